@@ -328,6 +328,126 @@ int kvg_decode_attn_noalloc(const kvg_cache* cache, const kvg_seqs* seqs, const 
                             const void* q_raw_dev, const void* k_raw_dev, const void* v_raw_dev,
                             float scale, float* out_dev, void* stream);
 
+/* ---------------------------------------------------------------------------------
+ * Packed sequences: batches whose sequences add different numbers of tokens (whole prompts,
+ * suffixes over restored blocks, single tokens, in one call), for models that norm their query
+ * and key heads, rotate part of a head, or scale the rotation for long contexts.
+ * kvg_norm_append writes the new tokens' keys and values to the cache and their queries, normed
+ * and rotated, to q_out; kvg_packed_attn attends over the cache from them.  The blocks deposited
+ * from such a cache graft like any other at their own position (a byte move); kvg_graft's
+ * relocation re-rotates keys with the header's base over the whole head, so it is right
+ * only for a rotary without scaling and with rotary_dim = head_dim. */
+
+/* How a rotary's frequencies follow from theta_i = base^(-2i/r), i in [0, r/2), r = rotary_dim,
+ * for a context `factor` times longer than the original_len tokens they were made for. */
+typedef enum {
+  KVG_ROTARY_PLAIN = 0,       /* theta_i                                                        */
+  KVG_ROTARY_LINEAR = 1,      /* theta_i / factor (position interpolation)                      */
+  KVG_ROTARY_BASE = 2,        /* with base factor^(r / (r - 2)) in the place of base             */
+  /* by turns n_i = original_len theta_i / (2 pi), g = (n_i - slow) / (fast - slow) clamped to [0, 1]:
+   * theta_i (g + (1 - g) / factor): frequencies of at least `fast` turns stay, those of at most
+   * `slow` are interpolated */
+  KVG_ROTARY_ROTATIONS = 3,
+  /* by index: c(n) = r ln(original_len / (2 pi n)) / (2 ln base), lo = max(floor c(fast), 0), hi =
+   * min(ceil c(slow), r - 1), g = (i - lo) / (hi - lo) clamped to [0, 1] (a step of 0.001 when hi <= lo):
+   * theta_i (1 - g) + theta_i / factor g */
+  KVG_ROTARY_INDEX = 4
+} kvg_rotary_scaling;
+
+/* A rotary embedding.  The first rotary_dim components of a head are rotated, in pairs i, i + r/2
+ * (HALF) or 2i, 2i + 1 (INTERLEAVED), by position * theta_i; the others are left as they are.  The
+ * rotated components are multiplied by `amplitude` as well (1: a rotation alone).  Angles, cosines and
+ * sines are taken in fp64 and rounded to fp32; the products are fp32. */
+typedef struct {
+  double base;            /* > 1 */
+  double factor;          /* >= 1; read with a scaling */
+  double original_len;    /* > 0; read by ROTATIONS and INDEX */
+  double fast, slow;      /* fast > slow > 0; read by ROTATIONS and INDEX */
+  double amplitude;       /* > 0 */
+  int32_t pairing;        /* kvg_rope_pairing */
+  int32_t scaling;        /* kvg_rotary_scaling */
+  int32_t rotary_dim;     /* a multiple of 16, at most head_dim; 0 = head_dim */
+  int32_t reserved;       /* must be 0 */
+} kvg_rotary;
+
+/* RMS norm of every query and key head: x <- x / sqrt(mean(x^2) + eps) * (weight + weight_offset), in
+ * fp32 over the head's head_dim components, before the rotation.  Weights: device
+ * [n_layers][head_dim] of the raw dtype for the layers of the call, or NULL: those heads are not
+ * normed. */
+typedef struct {
+  const void* q_weight;
+  const void* k_weight;
+  float eps;              /* >= 0 */
+  float weight_offset;    /* 0, or 1 for weights stored less one */
+} kvg_head_norm;
+
+/* The new tokens of a batch, one sequence after the other: rows [cu_tokens[b], cu_tokens[b + 1]) of the
+ * packed tensors are sequence b's tokens at logical indices ctx_lens[b] + 0, 1, ... (ctx_lens: the
+ * tokens cached before them).  A sequence may have none.  Rows below cu_tokens[0] and from
+ * cu_tokens[batch] on (a batch padded to a fixed size) are neither read nor written.  cu_tokens ascends; a
+ * sequence whose range descends, passes n_tokens or holds more than max_len tokens, whose ctx_lens is
+ * outside [0, max_ctx_len], or whose tokens pass its block table is skipped.
+ * Strides: elements from one token's row of the raw queries (keys, values) to the next one's,
+ * so that the three may be views into the rows of one projection; 0 = dense (heads * head_dim).
+ * Layers are n_tokens rows apart. */
+typedef struct {
+  int32_t n_tokens;             /* rows of the packed tensors, >= 0 */
+  int32_t max_len;              /* host-side upper bound of a sequence's tokens, >= 0 */
+  const int32_t* cu_tokens;     /* device [batch + 1] */
+  int64_t q_stride, k_stride, v_stride;
+} kvg_packed;
+
+/* The rotary's frequencies as the calls below use them: head_dim's rotary_dim / 2 values into
+ * theta_out (host).  Errors: KVG_E_INVAL, KVG_E_SHAPE (rotary_dim). */
+int kvg_rotary_frequencies(const kvg_rotary* rotary, int32_t head_dim, double* theta_out);
+
+/* Rotary positions of packed rows: y[t][h] = the rotation of x[t][h] at positions[t], for n_tokens rows
+ * of n_heads heads of head_dim (64, 128 or 256) components of `dtype` (KVG_F32 or KVG_BF16),
+ * computed in fp32 and rounded once.  x_stride, y_stride: elements from a token's row to the next (0 =
+ * dense).  y may be x itself with the same stride; otherwise they must not overlap.
+ * positions_dev: int64 [n_tokens], any sign.  Errors: KVG_E_INVAL, KVG_E_SHAPE, KVG_E_DTYPE, KVG_E_ALIGN
+ * (x, y or their rows not on 16 bytes), KVG_E_HIP. */
+int kvg_rotate(const kvg_rotary* rotary, int32_t dtype, int32_t head_dim, int32_t n_tokens, int32_t n_heads,
+               const int64_t* positions_dev, const void* x_dev, int64_t x_stride, void* y_dev, int64_t y_stride,
+               void* stream);
+
+/* Norm, rotation and append of packed tokens, in one pass: for every token at logical index t of
+ * sequence b, position p = start_pos[b] + t,
+ *   q_out <- round(R(p) norm(q_raw)),  cache K <- round(R(p) norm(k_raw)),  cache V <- round(v_raw)
+ * (fp32, rounded once; V is copied where the types are the same).  norm: NULL for none.  q_raw_dev:
+ * [n_layers][n_tokens][n_q_heads][head_dim] of the raw dtype (the cache's; bf16 for an fp8 cache) with
+ * the strides of `packed`, k_raw_dev and v_raw_dev alike; q_out_dev: the raw dtype, dense, not
+ * overlapping them except that it may be q_raw_dev itself when that is dense.  q_raw_dev and q_out_dev may both be NULL
+ * (keys and values alone).  Without norm, scaling and amplitude, and with rotary_dim = head_dim, the
+ * cache's bytes are kvg_append's.
+ * Errors: KVG_E_INVAL, KVG_E_SHAPE, KVG_E_DTYPE, KVG_E_CAPACITY (max_len or max_ctx_len tokens exceed the
+ * block table), KVG_E_ALIGN (pointers or strides not on 16 bytes), KVG_E_HIP. */
+int kvg_norm_append(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, const kvg_rotary* rotary,
+                    const kvg_head_norm* norm, int32_t layer0, int32_t n_layers, const void* q_raw_dev,
+                    const void* k_raw_dev, const void* v_raw_dev, void* q_out_dev, void* stream);
+
+/* Workspace bytes kvg_packed_attn needs for this batch (0 on bad args). */
+size_t kvg_packed_attn_workspace_bytes(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed,
+                                       int32_t n_layers);
+
+/* Causal attention of packed tokens over the paged cache, their own keys and values already in
+ * it (kvg_norm_append or kvg_append): for token i of sequence b, n = ctx_lens[b] + i, and each
+ * query head h,
+ *   out = softmax_j( (q_h . K_{h/group, j}) * scale ) V_{h/group, j},  j <= n
+ * (j > n - W as well in a layer with window W).  q_dev: [n_layers][n_tokens][n_q_heads][head_dim] of the raw
+ * dtype, rotated, token stride packed->q_stride; out_dev: the same, dense, of the raw dtype, not
+ * overlapping q_dev.  Softmax and sums in fp32, one rounding of the result; bf16 and fp8 caches multiply
+ * on the bf16 matrix cores, with the softmax weights rounded to bf16 (and summed as rounded).
+ * A row's bytes depend on its own query, keys and values alone: neither on how its sequence was cut
+ * into calls, nor on the other sequences or the pages.  A whole prompt and a suffix over its grafted
+ * prefix give the same bytes for the same token.  Inf and NaN among the keys and values reach
+ * the rows that see their token and no others.  seqs->start_pos is not read; seqs->shared_tokens is
+ * ignored.  ws_dev: kvg_packed_attn_workspace_bytes() bytes of scratch.
+ * Errors: as kvg_norm_append, and KVG_E_WORKSPACE. */
+int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, int32_t layer0,
+                    int32_t n_layers, const void* q_dev, float scale, void* out_dev, void* ws_dev, size_t ws_bytes,
+                    void* stream);
+
 /* ---- Content digests of an artifact (block digests, Sec. 4.11; the paper's deposit-side
  * hashing is closed, Sec. 3.1).  These calls work on any device buffer, typically a
  * deposited payload.  SHA-256 is FIPS 180-4.  All three launch on `stream`, clear their

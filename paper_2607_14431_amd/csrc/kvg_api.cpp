@@ -7,57 +7,18 @@
 #include <cstring>
 
 #include "kvg.h"
+#include "kvg_host.h"
 #include "kvg_launch.h"
 
 namespace {
 
-using kvg::kPage;
 using kvg::kSplit;
-
-constexpr size_t kAlign = 256;
-
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-
-size_t elem_bytes(const kvg_cache* c) { return c->dtype == KVG_BF16 ? 2 : c->dtype == KVG_FP8_E4M3 ? 1 : 4; }
-
-int check_cache(const kvg_cache* c) {
-  if (c == nullptr || c->k_pool == nullptr || c->v_pool == nullptr) return KVG_E_INVAL;
-  if (c->dtype != KVG_F32 && c->dtype != KVG_BF16 && c->dtype != KVG_FP8_E4M3) return KVG_E_DTYPE;
-  if (c->n_layers <= 0 || c->n_q_heads <= 0 || c->n_kv_heads <= 0 || c->n_pages <= 0) return KVG_E_SHAPE;
-  if (c->n_pages > INT32_MAX) return KVG_E_SHAPE;
-  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return KVG_E_SHAPE;
-  if (c->page_size != kPage) return KVG_E_SHAPE;
-  if (c->n_q_heads % c->n_kv_heads != 0) return KVG_E_SHAPE;
-  const int g = c->n_q_heads / c->n_kv_heads;
-  if (g != 1 && g != 2 && g != 4 && g != 8) return KVG_E_SHAPE;
-  if (c->layer_window != nullptr)
-    for (int l = 0; l < c->n_layers; ++l)
-      if (c->layer_window[l] < 0) return KVG_E_INVAL;
-  return KVG_OK;
-}
-
-// Windows of layers [layer0, layer0 + n_layers) as a launch carries them (all zero when none
-// is windowed); KVG_E_SHAPE when a windowed call spans more layers than a launch carries.
-int fill_windows(const kvg_cache* c, int32_t layer0, int32_t n_layers, int32_t* dst) {
-  std::memset(dst, 0, sizeof(int32_t) * kvg::kMaxWindowLayers);
-  if (c->layer_window == nullptr) return KVG_OK;
-  bool any = false;
-  for (int l = 0; l < n_layers; ++l) any = any || c->layer_window[layer0 + l] != 0;
-  if (!any) return KVG_OK;
-  if (n_layers > kvg::kMaxWindowLayers) return KVG_E_SHAPE;
-  for (int l = 0; l < n_layers; ++l) dst[l] = c->layer_window[layer0 + l];
-  return KVG_OK;
-}
+using namespace kvg::host;
 
 int check_rope(const kvg_rope* r) {
   if (r == nullptr || !(r->base > 0.0) || !std::isfinite(r->base)) return KVG_E_INVAL;
   if (r->pairing != KVG_ROPE_HALF && r->pairing != KVG_ROPE_INTERLEAVED) return KVG_E_INVAL;
   if (r->reserved != 0) return KVG_E_INVAL;
-  return KVG_OK;
-}
-
-int check_layers(const kvg_cache* c, int32_t layer0, int32_t n_layers) {
-  if (layer0 < 0 || n_layers <= 0 || layer0 + (int64_t)n_layers > c->n_layers) return KVG_E_SHAPE;
   return KVG_OK;
 }
 
@@ -69,10 +30,6 @@ int check_seqs(const kvg_cache* c, const kvg_seqs* s, int32_t chunk) {
     return KVG_E_INVAL;
   if ((int64_t)s->max_ctx_len + chunk > (int64_t)s->max_pages * c->page_size) return KVG_E_CAPACITY;
   return KVG_OK;
-}
-
-int64_t layer_elems(const kvg_cache* c) {
-  return c->n_pages * c->n_kv_heads * (int64_t)c->page_size * c->head_dim;
 }
 
 int n_split_max(const kvg_seqs* s, int32_t chunk) {
@@ -177,8 +134,6 @@ kvg::AppendArgs append_args(const kvg_cache* c, const kvg_seqs* s, const kvg_rop
   std::memcpy(a.theta, rope_theta(r->base, c->head_dim), sizeof(double) * (c->head_dim / 2));
   return a;
 }
-
-int hip_status(hipError_t e) { return e == hipSuccess ? KVG_OK : KVG_E_HIP; }
 
 // Every launch of a call is checked before the first one is enqueued.
 using kvg::fits_grid;

@@ -1,0 +1,235 @@
+// C ABI of the packed sequences' calls (declarations and contracts in include/kvg.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "kvg.h"
+#include "kvg_host.h"
+#include "kvg_launch.h"
+#include "kvg_packed.h"
+
+namespace {
+
+using namespace kvg::host;
+using kvg::fits_grid;
+
+constexpr double kTwoPi = 6.283185307179586476925;
+
+int rotary_dim(const kvg_rotary* r, int32_t head_dim) { return r->rotary_dim == 0 ? head_dim : r->rotary_dim; }
+
+bool positive(double x) { return x > 0.0 && std::isfinite(x); }
+
+int check_rotary(const kvg_rotary* r, int32_t head_dim) {
+  if (r == nullptr || !(r->base > 1.0) || !std::isfinite(r->base) || !positive(r->amplitude) || r->reserved != 0)
+    return KVG_E_INVAL;
+  if (r->pairing != KVG_ROPE_HALF && r->pairing != KVG_ROPE_INTERLEAVED) return KVG_E_INVAL;
+  if (r->scaling < KVG_ROTARY_PLAIN || r->scaling > KVG_ROTARY_INDEX) return KVG_E_INVAL;
+  if (r->scaling != KVG_ROTARY_PLAIN && (!(r->factor >= 1.0) || !std::isfinite(r->factor))) return KVG_E_INVAL;
+  if ((r->scaling == KVG_ROTARY_ROTATIONS || r->scaling == KVG_ROTARY_INDEX) &&
+      (!positive(r->original_len) || !positive(r->fast) || !positive(r->slow) || !(r->fast > r->slow)))
+    return KVG_E_INVAL;
+  if (r->rotary_dim < 0 || r->rotary_dim > head_dim || r->rotary_dim % 16 != 0) return KVG_E_SHAPE;
+  return KVG_OK;
+}
+
+void frequencies(const kvg_rotary* r, int dim, double* theta) {
+  const double base = r->scaling == KVG_ROTARY_BASE ? r->base * std::pow(r->factor, dim / (dim - 2.0)) : r->base;
+  double lo = 0.0, hi = 0.0;
+  if (r->scaling == KVG_ROTARY_INDEX) {
+    auto index = [&](double turns) { return dim * std::log(r->original_len / (kTwoPi * turns)) / (2.0 * std::log(r->base)); };
+    lo = std::max(std::floor(index(r->fast)), 0.0);
+    hi = std::min(std::ceil(index(r->slow)), dim - 1.0);
+  }
+  for (int i = 0; i < dim / 2; ++i) {
+    const double t = std::pow(base, -2.0 * i / dim);
+    double keep = 1.0;                                   // share of the unscaled frequency
+    if (r->scaling == KVG_ROTARY_LINEAR)
+      keep = 0.0;
+    else if (r->scaling == KVG_ROTARY_ROTATIONS)
+      keep = std::clamp((r->original_len * t / kTwoPi - r->slow) / (r->fast - r->slow), 0.0, 1.0);
+    else if (r->scaling == KVG_ROTARY_INDEX)
+      keep = 1.0 - std::clamp((i - lo) / std::max(hi - lo, 0.001), 0.0, 1.0);
+    theta[i] = keep == 1.0 ? t : t * keep + t / r->factor * (1.0 - keep);
+  }
+}
+
+// The rotary as a launch carries it.  Each thread keeps its last one: a model has one or two, and its powers
+// are a good part of a small call's time.
+void fill_rotary(const kvg_rotary* r, int32_t head_dim, kvg::RotaryArgs* out) {
+  thread_local kvg_rotary last = {};
+  thread_local int last_dim = 0;
+  thread_local kvg::RotaryArgs args;
+  const int dim = rotary_dim(r, head_dim);
+  if (dim != last_dim || std::memcmp(r, &last, sizeof(last)) != 0) {
+    args.pairing = r->pairing;
+    args.dim = dim;
+    args.amplitude = r->amplitude;
+    frequencies(r, dim, args.theta);
+    last = *r;
+    last_dim = dim;
+  }
+  out->pairing = args.pairing;
+  out->dim = dim;
+  out->amplitude = args.amplitude;
+  std::memcpy(out->theta, args.theta, sizeof(double) * (dim / 2));
+}
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+size_t raw_bytes(int32_t dtype) { return dtype == KVG_F32 ? 4 : 2; }
+
+// A token stride in elements: `dense` for 0; KVG_E_INVAL when rows overlap, KVG_E_ALIGN when they leave 16 bytes.
+int check_stride(int64_t stride, int64_t dense, size_t elem, int64_t* out) {
+  *out = stride == 0 ? dense : stride;
+  if (*out < dense) return KVG_E_INVAL;
+  return *out * (int64_t)elem % 16 == 0 ? KVG_OK : KVG_E_ALIGN;
+}
+
+int check_packed(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p) {
+  if (s == nullptr || s->block_tables == nullptr || s->ctx_lens == nullptr || s->start_pos == nullptr) return KVG_E_INVAL;
+  if (p == nullptr || p->cu_tokens == nullptr || p->n_tokens < 0 || p->max_len < 0) return KVG_E_INVAL;
+  if (s->batch <= 0 || s->max_pages <= 0 || s->max_ctx_len < 0) return KVG_E_INVAL;
+  const int64_t room = (int64_t)s->max_pages * c->page_size;
+  if (room > INT32_MAX) return KVG_E_SHAPE;
+  if (s->max_ctx_len > room || p->max_len > room) return KVG_E_CAPACITY;
+  return KVG_OK;
+}
+
+kvg::PackedSeqs packed_seqs(const kvg_seqs* s, const kvg_packed* p) {
+  return {p->cu_tokens, s->ctx_lens, s->block_tables, s->batch, p->n_tokens, p->max_len, s->max_ctx_len, s->max_pages};
+}
+
+}  // namespace
+
+extern "C" {
+
+int kvg_rotary_frequencies(const kvg_rotary* rotary, int32_t head_dim, double* theta_out) {
+  if (theta_out == nullptr) return KVG_E_INVAL;
+  if (head_dim != 64 && head_dim != 128 && head_dim != 256) return KVG_E_SHAPE;
+  const int st = check_rotary(rotary, head_dim);
+  if (st == KVG_OK) frequencies(rotary, rotary_dim(rotary, head_dim), theta_out);
+  return st;
+}
+
+int kvg_rotate(const kvg_rotary* rotary, int32_t dtype, int32_t head_dim, int32_t n_tokens, int32_t n_heads,
+               const int64_t* positions, const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream) {
+  if (dtype != KVG_F32 && dtype != KVG_BF16) return KVG_E_DTYPE;
+  if (head_dim != 64 && head_dim != 128 && head_dim != 256) return KVG_E_SHAPE;
+  int st = check_rotary(rotary, head_dim);
+  if (st != KVG_OK) return st;
+  if (n_tokens < 0 || n_heads <= 0 || (int64_t)n_heads * head_dim > INT32_MAX) return KVG_E_INVAL;
+  kvg::RotateArgs a;
+  const int64_t dense = (int64_t)n_heads * head_dim;
+  if ((st = check_stride(x_stride, dense, raw_bytes(dtype), &a.x_stride)) != KVG_OK) return st;
+  if ((st = check_stride(y_stride, dense, raw_bytes(dtype), &a.y_stride)) != KVG_OK) return st;
+  if (n_tokens == 0) return KVG_OK;
+  if (positions == nullptr || x == nullptr || y == nullptr) return KVG_E_INVAL;
+  if (x == y && a.x_stride != a.y_stride) return KVG_E_INVAL;
+  if (!aligned16(x) || !aligned16(y)) return KVG_E_ALIGN;
+  if (!fits_grid(n_tokens, 256)) return KVG_E_SHAPE;
+  a.x = x;
+  a.y = y;
+  a.positions = positions;
+  a.n_tokens = n_tokens;
+  a.n_heads = n_heads;
+  a.D = head_dim;
+  fill_rotary(rotary, head_dim, &a.rot);
+  return hip_status(kvg::launch_rotate(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int kvg_norm_append(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, const kvg_rotary* rotary,
+                    const kvg_head_norm* norm, int32_t layer0, int32_t n_layers, const void* q_raw, const void* k_raw,
+                    const void* v_raw, void* q_out, void* stream) {
+  int st = check_cache(cache);
+  if (st != KVG_OK) return st;
+  if ((st = check_rotary(rotary, cache->head_dim)) != KVG_OK) return st;
+  if ((st = check_layers(cache, layer0, n_layers)) != KVG_OK) return st;
+  if ((st = check_packed(cache, seqs, packed)) != KVG_OK) return st;
+  if (norm != nullptr && (!(norm->eps >= 0.0f) || !std::isfinite(norm->eps) || !std::isfinite(norm->weight_offset)))
+    return KVG_E_INVAL;
+  kvg::NormAppendArgs a;
+  std::memset(&a, 0, sizeof(a));
+  const size_t raw = raw_bytes(cache->dtype);
+  const int64_t q_dense = (int64_t)cache->n_q_heads * cache->head_dim, kv_dense = (int64_t)cache->n_kv_heads * cache->head_dim;
+  if ((st = check_stride(packed->q_stride, q_dense, raw, &a.q_stride)) != KVG_OK) return st;
+  if ((st = check_stride(packed->k_stride, kv_dense, raw, &a.k_stride)) != KVG_OK) return st;
+  if ((st = check_stride(packed->v_stride, kv_dense, raw, &a.v_stride)) != KVG_OK) return st;
+  if ((q_raw == nullptr) != (q_out == nullptr)) return KVG_E_INVAL;
+  if (packed->n_tokens == 0 || packed->max_len == 0) return KVG_OK;
+  if (k_raw == nullptr || v_raw == nullptr || (q_raw != nullptr && q_raw == q_out && a.q_stride != q_dense)) return KVG_E_INVAL;
+  const void* w_q = norm != nullptr ? norm->q_weight : nullptr;
+  const void* w_k = norm != nullptr ? norm->k_weight : nullptr;
+  if (!aligned16(q_raw) || !aligned16(k_raw) || !aligned16(v_raw) || !aligned16(q_out) || !aligned16(w_q) || !aligned16(w_k) ||
+      !aligned16(cache->k_pool) || !aligned16(cache->v_pool))
+    return KVG_E_ALIGN;
+  if (!fits_grid(packed->n_tokens, 256)) return KVG_E_SHAPE;
+  a.seqs = packed_seqs(seqs, packed);
+  a.start_pos = seqs->start_pos;
+  a.k_pool = cache->k_pool;
+  a.v_pool = cache->v_pool;
+  a.layer_elems = layer_elems(cache);
+  a.n_pages = cache->n_pages;
+  a.q_raw = q_raw;
+  a.k_raw = k_raw;
+  a.v_raw = v_raw;
+  a.q_out = q_out;
+  a.q_weight = w_q;
+  a.k_weight = w_k;
+  a.eps = norm != nullptr ? norm->eps : 0.0f;
+  a.weight_offset = norm != nullptr ? norm->weight_offset : 0.0f;
+  a.Hq = cache->n_q_heads;
+  a.Hkv = cache->n_kv_heads;
+  a.D = cache->head_dim;
+  a.layer0 = layer0;
+  a.n_layers = n_layers;
+  fill_rotary(rotary, cache->head_dim, &a.rot);
+  return hip_status(kvg::launch_norm_append(a, cache->dtype, static_cast<hipStream_t>(stream)));
+}
+
+size_t kvg_packed_attn_workspace_bytes(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed,
+                                       int32_t n_layers) {
+  if (check_cache(cache) != KVG_OK || check_packed(cache, seqs, packed) != KVG_OK || n_layers <= 0 ||
+      n_layers > cache->n_layers)
+    return 0;
+  return kAlign;
+}
+
+int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, int32_t layer0, int32_t n_layers,
+                    const void* q, float scale, void* out, void* ws, size_t ws_bytes, void* stream) {
+  int st = check_cache(cache);
+  if (st != KVG_OK) return st;
+  if ((st = check_layers(cache, layer0, n_layers)) != KVG_OK) return st;
+  if ((st = check_packed(cache, seqs, packed)) != KVG_OK) return st;
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return KVG_E_INVAL;
+  kvg::PackedAttnArgs a;
+  std::memset(&a, 0, sizeof(a));
+  if ((st = check_stride(packed->q_stride, (int64_t)cache->n_q_heads * cache->head_dim, raw_bytes(cache->dtype),
+                         &a.q_stride)) != KVG_OK)
+    return st;
+  if ((st = fill_windows(cache, layer0, n_layers, a.window)) != KVG_OK) return st;
+  if (ws == nullptr || ws_bytes < kvg_packed_attn_workspace_bytes(cache, seqs, packed, n_layers)) return KVG_E_WORKSPACE;
+  if (packed->n_tokens == 0 || packed->max_len == 0) return KVG_OK;
+  if (q == nullptr || out == nullptr || q == out) return KVG_E_INVAL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(ws) || !aligned16(cache->k_pool) || !aligned16(cache->v_pool))
+    return KVG_E_ALIGN;
+  if (!fits_grid((int64_t)packed->n_tokens * cache->n_q_heads * n_layers, 256)) return KVG_E_SHAPE;
+  a.seqs = packed_seqs(seqs, packed);
+  a.k_pool = cache->k_pool;
+  a.v_pool = cache->v_pool;
+  a.layer_elems = layer_elems(cache);
+  a.n_pages = cache->n_pages;
+  a.q = q;
+  a.out = out;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.Hq = cache->n_q_heads;
+  a.Hkv = cache->n_kv_heads;
+  a.D = cache->head_dim;
+  a.group = cache->n_q_heads / cache->n_kv_heads;
+  a.layer0 = layer0;
+  a.n_layers = n_layers;
+  return hip_status(kvg::launch_packed_attn(a, cache->dtype, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -22,6 +22,7 @@ _lib = ctypes.CDLL(LIB_PATH)
 KVG_F32, KVG_BF16, KVG_FP8_E4M3 = 0, 1, 2
 KVG_ROPE_HALF, KVG_ROPE_INTERLEAVED = 0, 1
 KVG_GRAFT_ALLOW_RELOCATE = 1
+KVG_ROTARY_PLAIN, KVG_ROTARY_LINEAR, KVG_ROTARY_BASE, KVG_ROTARY_ROTATIONS, KVG_ROTARY_INDEX = range(5)
 KVG_ARTIFACT_MAGIC = 0x4147564B
 KVG_ARTIFACT_VERSION = 2
 
@@ -53,6 +54,23 @@ class kvg_seqs(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("max_ctx_len", ctypes.c_int32),
                 ("shared_tokens", ctypes.c_int32), ("block_tables", ctypes.c_void_p), ("ctx_lens", ctypes.c_void_p),
                 ("start_pos", ctypes.c_void_p)]
+
+
+class kvg_rotary(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_double), ("factor", ctypes.c_double), ("original_len", ctypes.c_double),
+                ("fast", ctypes.c_double), ("slow", ctypes.c_double), ("amplitude", ctypes.c_double),
+                ("pairing", ctypes.c_int32), ("scaling", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class kvg_head_norm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("weight_offset", ctypes.c_float)]
+
+
+class kvg_packed(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int32), ("max_len", ctypes.c_int32), ("cu_tokens", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
 
 
 class kvg_artifact_hdr(ctypes.Structure):
@@ -87,6 +105,13 @@ _SIGS = {
                                        _f32, _vp, _vp, _sz, _vp]),
     "kvg_decode_attn_noalloc": (ctypes.c_int, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_rope), _i32, _i32, _vp, _vp, _vp,
                                                _f32, _vp, _vp]),
+    "kvg_rotary_frequencies": (ctypes.c_int, [_P(kvg_rotary), _i32, _P(ctypes.c_double)]),
+    "kvg_rotate": (ctypes.c_int, [_P(kvg_rotary), _i32, _i32, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "kvg_norm_append": (ctypes.c_int, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_packed), _P(kvg_rotary), _P(kvg_head_norm),
+                                       _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
+    "kvg_packed_attn_workspace_bytes": (_sz, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_packed), _i32]),
+    "kvg_packed_attn": (ctypes.c_int, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_packed), _i32, _i32, _vp, _f32, _vp, _vp, _sz,
+                                       _vp]),
     "kvg_leaf_digests": (ctypes.c_int, [_vp, _u64, ctypes.c_uint32, _vp, _vp]),
     "kvg_merkle_workspace_bytes": (_sz, [_u64]),
     "kvg_merkle_root": (ctypes.c_int, [_vp, _u64, _vp, _vp, _sz, _vp]),
@@ -323,6 +348,116 @@ def kvg_decode_attn_noalloc(cache: Cache, seqs: Seqs, rp: kvg_rope, layer0: int,
     _check(_lib.kvg_decode_attn_noalloc(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()), ctypes.byref(rp),
                                         layer0, n_layers, _ptr(q_raw), _ptr(k_raw), _ptr(v_raw), scale, _ptr(out),
                                         _stream(stream)), "kvg_decode_attn_noalloc")
+
+
+def rotary(base: float = 10000.0, pairing: int = KVG_ROPE_HALF, rotary_dim: int = 0, scaling: int = KVG_ROTARY_PLAIN,
+           factor: float = 1.0, original_len: float = 0.0, fast: float = 0.0, slow: float = 0.0,
+           amplitude: float = 1.0) -> kvg_rotary:
+    """A rotary embedding: pairing, rotated part of the head (0: all of it), scaling with its parameters (kvg.h)."""
+    return kvg_rotary(base, factor, original_len, fast, slow, amplitude, pairing, scaling, rotary_dim, 0)
+
+
+@dataclasses.dataclass
+class HeadNorm:
+    """RMS norm of query and key heads: weights [n_layers][head_dim] of the raw dtype (None: not normed)."""
+    q_weight: torch.Tensor | None
+    k_weight: torch.Tensor | None
+    eps: float
+    weight_offset: float = 0.0       # 1 for weights stored less one
+
+    def struct(self, cache: Cache, n_layers: int) -> kvg_head_norm:
+        dtype, n = cache.raw_dtype, n_layers * cache.head_dim
+        for w in (self.q_weight, self.k_weight):
+            assert w is None or (w.dtype is dtype and w.is_contiguous() and w.numel() == n), \
+                "norm weights: [n_layers][head_dim] of the cache's raw dtype, contiguous"
+        return kvg_head_norm(_ptr(self.q_weight), _ptr(self.k_weight), self.eps, self.weight_offset)
+
+
+@dataclasses.dataclass
+class Packed:
+    """New tokens of a batch, one sequence after the other: rows [cu_tokens[b], cu_tokens[b + 1]) (int32 [batch + 1],
+    device) of tensors of n_tokens rows are sequence b's; max_len: an upper bound of a sequence's tokens."""
+    cu_tokens: torch.Tensor
+    n_tokens: int
+    max_len: int
+
+    def struct(self, seqs: Seqs, q_stride: int = 0, k_stride: int = 0, v_stride: int = 0) -> kvg_packed:
+        cu = self.cu_tokens
+        assert cu.dtype is torch.int32 and cu.is_contiguous() and cu.numel() == seqs.block_tables.shape[0] + 1
+        return kvg_packed(self.n_tokens, self.max_len, cu.data_ptr(), q_stride, k_stride, v_stride)
+
+
+def _token_stride(t: torch.Tensor, n_layers: int, n_tokens: int, heads: int, head_dim: int, dtype: torch.dtype) -> int:
+    """Token stride of packed rows [n_layers][n_tokens][heads][head_dim], which may be a view into wider rows."""
+    if t.dtype is not dtype or t.shape != (n_layers, n_tokens, heads, head_dim):
+        raise ValueError(f"packed rows: {dtype} [{n_layers}][{n_tokens}][{heads}][{head_dim}], got {t.dtype} {tuple(t.shape)}")
+    sl, st, sh, sd = t.stride()
+    if n_tokens <= 1:                      # a token's rows are n_tokens strides from the next layer's
+        st = sl if n_layers > 1 and n_tokens else heads * head_dim
+    if sd != 1 or (heads > 1 and sh != head_dim) or st < heads * head_dim or (n_layers > 1 and n_tokens and sl != n_tokens * st):
+        raise ValueError("packed rows: heads dense, layers n_tokens rows apart")
+    return st
+
+
+def kvg_rotary_frequencies(rt: kvg_rotary, head_dim: int) -> list[float]:
+    theta = (ctypes.c_double * 128)()
+    _check(_lib.kvg_rotary_frequencies(ctypes.byref(rt), head_dim, theta), "kvg_rotary_frequencies")
+    return list(theta[: (rt.rotary_dim or head_dim) // 2])
+
+
+def kvg_rotate(rt: kvg_rotary, positions: torch.Tensor, x: torch.Tensor, y: torch.Tensor, stream=None):
+    """y[t][h] = x[t][h] rotated at positions[t] (int64); x, y: [n_tokens][n_heads][head_dim], fp32 or bf16, heads
+    dense, any token stride; y may be x."""
+    T, H, D = x.shape
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise KvgError(-3, "kvg_rotate")
+    assert positions.dtype is torch.int64 and positions.is_contiguous() and positions.numel() == T
+    sx = _token_stride(x[None], 1, T, H, D, x.dtype)
+    sy = _token_stride(y[None], 1, T, H, D, x.dtype)
+    _check(_lib.kvg_rotate(ctypes.byref(rt), _DTYPE_CODE[x.dtype], D, T, H, _ptr(positions), _ptr(x), sx, _ptr(y), sy,
+                           _stream(stream)), "kvg_rotate")
+
+
+def kvg_norm_append(cache: Cache, seqs: Seqs, packed: Packed, rt: kvg_rotary, norm: HeadNorm | None, layer0: int,
+                    n_layers: int, q_raw: torch.Tensor | None, k_raw: torch.Tensor, v_raw: torch.Tensor,
+                    q_out: torch.Tensor | None, stream=None):
+    """Norm, rotation and append of packed tokens.  q_raw, k_raw, v_raw: [n_layers][n_tokens][heads][head_dim] of the raw
+    dtype, views into wider rows allowed; q_out: dense (q_raw and q_out: both None for keys and values alone)."""
+    raw, T, D, Hkv = cache.raw_dtype, packed.n_tokens, cache.head_dim, cache.n_kv_heads
+    sq = 0
+    if q_raw is not None:
+        sq = _token_stride(q_raw, n_layers, T, cache.n_q_heads, D, raw)
+    if q_out is not None:
+        assert q_out.shape == (n_layers, T, cache.n_q_heads, D) and q_out.dtype is raw and q_out.is_contiguous()
+    sk, sv = (_token_stride(t, n_layers, T, Hkv, D, raw) for t in (k_raw, v_raw))
+    ns = None if norm is None else norm.struct(cache, n_layers)
+    _check(_lib.kvg_norm_append(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()),
+                                ctypes.byref(packed.struct(seqs, sq, sk, sv)), ctypes.byref(rt),
+                                None if ns is None else ctypes.byref(ns), layer0, n_layers, _ptr(q_raw), _ptr(k_raw),
+                                _ptr(v_raw), _ptr(q_out), _stream(stream)), "kvg_norm_append")
+
+
+def kvg_packed_attn_workspace_bytes(cache: Cache, seqs: Seqs, packed: Packed, n_layers: int) -> int:
+    return _lib.kvg_packed_attn_workspace_bytes(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()),
+                                                ctypes.byref(packed.struct(seqs)), n_layers)
+
+
+def packed_attn_workspace(cache: Cache, seqs: Seqs, packed: Packed, n_layers: int) -> torch.Tensor:
+    """Scratch for kvg_packed_attn calls of this batch's bounds."""
+    return torch.empty(max(kvg_packed_attn_workspace_bytes(cache, seqs, packed, n_layers), 256), dtype=torch.uint8,
+                       device=cache.k_pool.device)
+
+
+def kvg_packed_attn(cache: Cache, seqs: Seqs, packed: Packed, layer0: int, n_layers: int, q: torch.Tensor, scale: float,
+                    out: torch.Tensor, ws: torch.Tensor, stream=None):
+    """Causal attention of packed tokens over the cache.  q: [n_layers][n_tokens][n_q_heads][head_dim] of the raw dtype,
+    rotated, any token stride; out: the same, dense."""
+    raw, T, D, Hq = cache.raw_dtype, packed.n_tokens, cache.head_dim, cache.n_q_heads
+    sq = _token_stride(q, n_layers, T, Hq, D, raw)
+    assert out.shape == (n_layers, T, Hq, D) and out.dtype is raw and out.is_contiguous()
+    _check(_lib.kvg_packed_attn(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()),
+                                ctypes.byref(packed.struct(seqs, sq)), layer0, n_layers, _ptr(q), scale, _ptr(out),
+                                _ptr(ws), ws.nbytes, _stream(stream)), "kvg_packed_attn")
 
 
 def kvg_leaf_digests(data: torch.Tensor, leaf_bytes: int, digests: torch.Tensor, n_bytes: int | None = None,
