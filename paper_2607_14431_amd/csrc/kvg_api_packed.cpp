@@ -101,6 +101,32 @@ kvg::PackedSeqs packed_seqs(const kvg_seqs* s, const kvg_packed* p) {
   return {p->cu_tokens, s->ctx_lens, s->block_tables, s->batch, p->n_tokens, p->max_len, s->max_ctx_len, s->max_pages};
 }
 
+// How an attention call runs: tiles of the batch at most, segments of a launch split over keys (1: none), workspace.
+struct AttnPlan {
+  int64_t n_tiles;
+  int32_t n_seg;
+  size_t ml, acc;
+  size_t total() const { return std::max(ml + acc, kAlign); }
+};
+
+AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, int32_t n_layers) {
+  AttnPlan r = {0, 1, 0, 0};
+  if (c->dtype == KVG_F32 || p->n_tokens == 0 || p->max_len == 0) return r;
+  const int64_t group = c->n_q_heads / c->n_kv_heads, bm = kvg::packed_mfma_pairs(c->head_dim);
+  const int64_t len = std::min(p->max_len, p->n_tokens), per_seq = (len * group + bm - 1) / bm;
+  // each sequence's tiles round up
+  r.n_tiles = std::min(s->batch * per_seq, (p->n_tokens * group + (int64_t)std::min(s->batch, p->n_tokens) * (bm - 1)) / bm);
+  const int64_t keys = std::min((int64_t)s->max_ctx_len + p->max_len, (int64_t)s->max_pages * c->page_size);
+  const int64_t segs = (keys + kvg::kPackedSeg - 1) / kvg::kPackedSeg;
+  if (segs > 1 && r.n_tiles * c->n_kv_heads * n_layers < 512) {
+    r.n_seg = (int32_t)segs;
+    const size_t rows = (size_t)n_layers * p->n_tokens * c->n_q_heads * segs;
+    r.ml = align_up(rows * 2 * sizeof(float));
+    r.acc = align_up(rows * c->head_dim * sizeof(float));
+  }
+  return r;
+}
+
 }  // namespace
 
 extern "C" {
@@ -193,7 +219,7 @@ size_t kvg_packed_attn_workspace_bytes(const kvg_cache* cache, const kvg_seqs* s
   if (check_cache(cache) != KVG_OK || check_packed(cache, seqs, packed) != KVG_OK || n_layers <= 0 ||
       n_layers > cache->n_layers)
     return 0;
-  return kAlign;
+  return attn_plan(cache, seqs, packed, n_layers).total();
 }
 
 int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, int32_t layer0, int32_t n_layers,
@@ -209,7 +235,8 @@ int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_pack
                          &a.q_stride)) != KVG_OK)
     return st;
   if ((st = fill_windows(cache, layer0, n_layers, a.window)) != KVG_OK) return st;
-  if (ws == nullptr || ws_bytes < kvg_packed_attn_workspace_bytes(cache, seqs, packed, n_layers)) return KVG_E_WORKSPACE;
+  const AttnPlan plan = attn_plan(cache, seqs, packed, n_layers);
+  if (ws == nullptr || ws_bytes < plan.total()) return KVG_E_WORKSPACE;
   if (packed->n_tokens == 0 || packed->max_len == 0) return KVG_OK;
   if (q == nullptr || out == nullptr || q == out) return KVG_E_INVAL;
   if (!aligned16(q) || !aligned16(out) || !aligned16(ws) || !aligned16(cache->k_pool) || !aligned16(cache->v_pool))
@@ -229,6 +256,14 @@ int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_pack
   a.group = cache->n_q_heads / cache->n_kv_heads;
   a.layer0 = layer0;
   a.n_layers = n_layers;
+  if (cache->dtype != KVG_F32) {
+    a.n_tiles = (int32_t)std::min<int64_t>(plan.n_tiles, INT32_MAX);
+    a.n_seg = plan.n_seg;
+    a.part_ml = static_cast<float*>(ws);
+    a.part_acc = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.ml);
+    if (!fits_grid(kvg::packed_mfma_workgroups(a), 256)) return KVG_E_SHAPE;
+    return hip_status(kvg::launch_packed_mfma(a, cache->dtype, static_cast<hipStream_t>(stream)));
+  }
   return hip_status(kvg::launch_packed_attn(a, cache->dtype, static_cast<hipStream_t>(stream)));
 }
 

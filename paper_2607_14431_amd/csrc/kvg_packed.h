@@ -28,6 +28,58 @@ __device__ __forceinline__ SeqRange seq_range(const PackedSeqs& s, int b) {
   return {r0, ok ? (int)len : 0, ctx};
 }
 
+// A sequence, its range, and the place of a searched unit in it: unit `at` of its `count`; b -1: no sequence.
+struct SeqUnit {
+  int b, at, count;
+  SeqRange range;
+};
+
+// Unit `target` of the batch, whose sequences have count(range) units each.  All lanes of a wave search together, 64
+// sequences at a time, each lane reading one; the result is uniform.
+template <typename Count>
+__device__ __forceinline__ SeqUnit find_unit(const PackedSeqs& s, int target, Count count) {
+  const int lane = __lane_id();
+  for (int b0 = 0; b0 < s.batch; b0 += 64) {
+    const int b = b0 + lane;
+    const SeqRange r = b < s.batch ? seq_range(s, b) : SeqRange{0, 0, 0};
+    const int n = count(r);
+    int sum = n;                                           // of this lane's sequence and those before it
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int before = __shfl_up(sum, d);
+      sum += lane >= d ? before : 0;
+    }
+    const uint64_t past = __builtin_amdgcn_ballot_w64(sum > target);
+    if (past != 0) {
+      const int at = __builtin_ctzll(past);
+      const int c = __builtin_amdgcn_readlane(n, at);
+      return {b0 + at, target - (__builtin_amdgcn_readlane(sum, at) - c), c,
+              {__builtin_amdgcn_readlane(r.row0, at), __builtin_amdgcn_readlane(r.len, at), __builtin_amdgcn_readlane(r.ctx, at)}};
+    }
+    target -= __builtin_amdgcn_readlane(sum, 63);
+  }
+  return {-1, 0, 0, {0, 0, 0}};
+}
+
+// The sequence of packed row `tok` and its place there.
+__device__ __forceinline__ SeqUnit find_token(const PackedSeqs& s, int tok) {
+  const int lane = __lane_id();
+  for (int b0 = 0; b0 < s.batch; b0 += 64) {
+    const int b = b0 + lane;
+    const SeqRange r = b < s.batch ? seq_range(s, b) : SeqRange{0, 0, 0};
+    const uint64_t mine = __builtin_amdgcn_ballot_w64(tok >= r.row0 && tok - r.row0 < r.len);
+    if (mine != 0) {
+      const int at = __builtin_ctzll(mine);
+      const int row0 = __builtin_amdgcn_readlane(r.row0, at), len = __builtin_amdgcn_readlane(r.len, at);
+      return {b0 + at, tok - row0, len, {row0, len, __builtin_amdgcn_readlane(r.ctx, at)}};
+    }
+  }
+  return {-1, 0, 0, {0, 0, 0}};
+}
+
+// Keys of a segment of the attention's sums (absolute multiples of the logical index).
+constexpr int kPackedSeg = 512;
+
 // The rotation of a launch: frequencies and what cos and sin are multiplied with.
 struct RotaryArgs {
   int32_t pairing, dim;       // dim: components rotated
@@ -72,11 +124,19 @@ struct PackedAttnArgs {
   int64_t q_stride;
   float scale_log2;
   int32_t Hq, Hkv, D, group, layer0, n_layers;
+  int32_t n_tiles;            // bf16 and fp8: bound of the batch's tiles
+  int32_t n_seg;              // segments of a launch split over keys (1: not split)
+  float* part_acc;            // split: [n_layers][n_tokens][Hq][n_seg][D]
+  float* part_ml;             // [n_layers][n_tokens][Hq][n_seg][2] reference, sum
   int32_t window[kMaxWindowLayers];
 };
 
 hipError_t launch_rotate(const RotateArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_norm_append(const NormAppendArgs& a, int dtype, hipStream_t stream);
+// bf16 and fp8 caches: (row, query head) pairs of a tile, workgroups of the launch
+int packed_mfma_pairs(int D);
+inline int64_t packed_mfma_workgroups(const PackedAttnArgs& a) { return (int64_t)a.n_layers * a.n_seg * a.n_tiles * a.Hkv; }
+hipError_t launch_packed_mfma(const PackedAttnArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_packed_attn(const PackedAttnArgs& a, int dtype, hipStream_t stream);
 
 }  // namespace kvg
