@@ -101,30 +101,69 @@ kvg::PackedSeqs packed_seqs(const kvg_seqs* s, const kvg_packed* p) {
   return {p->cu_tokens, s->ctx_lens, s->block_tables, s->batch, p->n_tokens, p->max_len, s->max_ctx_len, s->max_pages};
 }
 
-// How an attention call runs: tiles of the batch at most, segments of a launch split over keys (1: none), workspace.
+// How a bf16 or fp8 attention call runs: rows of the few kernel and tiles at most, each launch's segments (1: not
+// split), and where their partials lie in the workspace.
 struct AttnPlan {
-  int64_t n_tiles;
-  int32_t n_seg;
-  size_t ml, acc;
-  size_t total() const { return std::max(ml + acc, kAlign); }
+  int64_t few_rows, n_tiles;
+  int32_t few_seg, tile_seg;
+  size_t few_ml, few_acc, tile_ml, tile_acc;
+  size_t total() const { return std::max(few_ml + few_acc + tile_ml + tile_acc, kAlign); }
 };
 
 AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, int32_t n_layers) {
-  AttnPlan r = {0, 1, 0, 0};
+  AttnPlan r = {0, 0, 1, 1, 0, 0, 0, 0};
   if (c->dtype == KVG_F32 || p->n_tokens == 0 || p->max_len == 0) return r;
-  const int64_t group = c->n_q_heads / c->n_kv_heads, bm = kvg::packed_mfma_pairs(c->head_dim);
-  const int64_t len = std::min(p->max_len, p->n_tokens), per_seq = (len * group + bm - 1) / bm;
-  // each sequence's tiles round up
-  r.n_tiles = std::min(s->batch * per_seq, (p->n_tokens * group + (int64_t)std::min(s->batch, p->n_tokens) * (bm - 1)) / bm);
+  const int64_t group = c->n_q_heads / c->n_kv_heads, bm = kvg::packed_tile_pairs(c->head_dim);
+  const int64_t len = std::min(p->max_len, p->n_tokens);
   const int64_t keys = std::min((int64_t)s->max_ctx_len + p->max_len, (int64_t)s->max_pages * c->page_size);
-  const int64_t segs = (keys + kvg::kPackedSeg - 1) / kvg::kPackedSeg;
-  if (segs > 1 && r.n_tiles * c->n_kv_heads * n_layers < 512) {
-    r.n_seg = (int32_t)segs;
-    const size_t rows = (size_t)n_layers * p->n_tokens * c->n_q_heads * segs;
-    r.ml = align_up(rows * 2 * sizeof(float));
-    r.acc = align_up(rows * c->head_dim * sizeof(float));
+  const int32_t segs = (int32_t)((keys + kvg::kPackedSeg - 1) / kvg::kPackedSeg);
+  // The lengths are the device's.  A single sequence that may be long goes in tiles whatever its length.
+  if (len * group <= kvg::kFewPairs || s->batch > 1) {
+    r.few_rows = std::min<int64_t>(p->n_tokens, s->batch * std::min<int64_t>(len, kvg::kFewPairs / group));
+    r.few_seg = segs;
   }
+  if (len * group > kvg::kFewPairs) {
+    const int64_t per_seq = (len * group + bm - 1) / bm;               // each sequence's tiles round up
+    r.n_tiles = std::min(s->batch * per_seq, (p->n_tokens * group + (int64_t)std::min(s->batch, p->n_tokens) * (bm - 1)) / bm);
+    if (r.n_tiles * c->n_kv_heads * n_layers < 512) r.tile_seg = segs;
+  }
+  auto bytes = [&](int64_t rows, int32_t n_seg, size_t values) {
+    return n_seg > 1 ? align_up((size_t)n_layers * rows * c->n_q_heads * n_seg * values * sizeof(float)) : 0;
+  };
+  r.few_ml = bytes(r.few_rows, r.few_seg, 2);
+  r.few_acc = bytes(r.few_rows, r.few_seg, c->head_dim);
+  r.tile_ml = bytes(p->n_tokens, r.tile_seg, 2);
+  r.tile_acc = bytes(p->n_tokens, r.tile_seg, c->head_dim);
   return r;
+}
+
+// The few kernel's launch, the tiles' launch, and the folds of those that are split.  Every launch is checked before the
+// first one is enqueued.
+int attn_mfma(kvg::PackedAttnArgs a, const AttnPlan& plan, int32_t dtype, char* ws, hipStream_t stream) {
+  if (plan.n_tiles > INT32_MAX) return KVG_E_SHAPE;
+  a.few_rows = (int32_t)plan.few_rows;
+  a.n_tiles = (int32_t)plan.n_tiles;
+  kvg::PackedAttnArgs few = a, tiles = a;
+  few.n_seg = plan.few_seg;
+  few.part_ml = reinterpret_cast<float*>(ws);
+  few.part_acc = reinterpret_cast<float*>(ws + plan.few_ml);
+  tiles.n_seg = plan.tile_seg;
+  tiles.part_ml = reinterpret_cast<float*>(ws + plan.few_ml + plan.few_acc);
+  tiles.part_acc = reinterpret_cast<float*>(ws + plan.few_ml + plan.few_acc + plan.tile_ml);
+  const int64_t row_heads = (int64_t)a.n_layers * a.seqs.n_tokens * a.Hq;
+  if (!fits_grid(kvg::packed_few_workgroups(few), 256) || !fits_grid(kvg::packed_tile_workgroups(tiles), 256) ||
+      !fits_grid(row_heads, 256))
+    return KVG_E_SHAPE;
+  int st = KVG_OK;
+  if (a.n_tiles > 0) {
+    st = hip_status(kvg::launch_packed_tiles(tiles, dtype, stream));
+    if (st == KVG_OK && plan.tile_seg > 1) st = hip_status(kvg::launch_packed_fold(tiles, false, stream));
+  }
+  if (st == KVG_OK && a.few_rows > 0) {
+    st = hip_status(kvg::launch_packed_few(few, dtype, stream));
+    if (st == KVG_OK && plan.few_seg > 1) st = hip_status(kvg::launch_packed_fold(few, true, stream));
+  }
+  return st;
 }
 
 }  // namespace
@@ -257,12 +296,7 @@ int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_pack
   a.layer0 = layer0;
   a.n_layers = n_layers;
   if (cache->dtype != KVG_F32) {
-    a.n_tiles = (int32_t)std::min<int64_t>(plan.n_tiles, INT32_MAX);
-    a.n_seg = plan.n_seg;
-    a.part_ml = static_cast<float*>(ws);
-    a.part_acc = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.ml);
-    if (!fits_grid(kvg::packed_mfma_workgroups(a), 256)) return KVG_E_SHAPE;
-    return hip_status(kvg::launch_packed_mfma(a, cache->dtype, static_cast<hipStream_t>(stream)));
+    return attn_mfma(a, plan, cache->dtype, static_cast<char*>(ws), static_cast<hipStream_t>(stream));
   }
   return hip_status(kvg::launch_packed_attn(a, cache->dtype, static_cast<hipStream_t>(stream)));
 }

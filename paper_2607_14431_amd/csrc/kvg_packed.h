@@ -124,19 +124,31 @@ struct PackedAttnArgs {
   int64_t q_stride;
   float scale_log2;
   int32_t Hq, Hkv, D, group, layer0, n_layers;
-  int32_t n_tiles;            // bf16 and fp8: bound of the batch's tiles
-  int32_t n_seg;              // segments of a launch split over keys (1: not split)
-  float* part_acc;            // split: [n_layers][n_tokens][Hq][n_seg][D]
-  float* part_ml;             // [n_layers][n_tokens][Hq][n_seg][2] reference, sum
+  // bf16 and fp8 caches: sequences of at most kFewPairs (row, query head) pairs per KV head are the few kernel's where
+  // it runs (few_rows > 0: a bound of their rows), the others go in tiles (n_tiles: a bound of the batch's).
+  // A launch over n_seg > 1 segments leaves partials [n_layers][rows][Hq][n_seg] (reference and sum, then D sums);
+  // rows: the launch's packed rows, the few kernel's counted over its own sequences.
+  int32_t few_rows, n_tiles;
+  int32_t n_seg;
+  float* part_acc;
+  float* part_ml;
   int32_t window[kMaxWindowLayers];
 };
 
 hipError_t launch_rotate(const RotateArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_norm_append(const NormAppendArgs& a, int dtype, hipStream_t stream);
-// bf16 and fp8 caches: (row, query head) pairs of a tile, workgroups of the launch
-int packed_mfma_pairs(int D);
-inline int64_t packed_mfma_workgroups(const PackedAttnArgs& a) { return (int64_t)a.n_layers * a.n_seg * a.n_tiles * a.Hkv; }
-hipError_t launch_packed_mfma(const PackedAttnArgs& a, int dtype, hipStream_t stream);
+// bf16 and fp8 caches: pairs of a tile, workgroups of the launches
+constexpr int kFewPairs = 32;
+__device__ __forceinline__ bool is_few(const PackedAttnArgs& a, const SeqRange& s) {
+  return a.few_rows > 0 && (int64_t)s.len * a.group <= kFewPairs;
+}
+int packed_tile_pairs(int D);
+inline int64_t packed_tile_workgroups(const PackedAttnArgs& a) { return (int64_t)a.n_layers * a.n_seg * a.n_tiles * a.Hkv; }
+inline int64_t packed_few_workgroups(const PackedAttnArgs& a) { return (int64_t)a.n_layers * a.n_seg * a.seqs.batch * a.Hkv; }
+hipError_t launch_packed_tiles(const PackedAttnArgs& a, int dtype, hipStream_t stream);
+hipError_t launch_packed_few(const PackedAttnArgs& a, int dtype, hipStream_t stream);
+// out = the rows' segments folded in order, of a tile launch and of the few kernel's
+hipError_t launch_packed_fold(const PackedAttnArgs& a, bool few, hipStream_t stream);
 hipError_t launch_packed_attn(const PackedAttnArgs& a, int dtype, hipStream_t stream);
 
 }  // namespace kvg

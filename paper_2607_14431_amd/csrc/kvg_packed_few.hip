@@ -1,0 +1,303 @@
+// Packed attention of sequences with few rows (single tokens, short chunks): a workgroup per (layer, sequence, KV head,
+// segment of kPackedSeg keys), up to kFewPairs (row, query head) pairs, and the fold of segments.
+//
+// The sums are those of the tile kernel (kvg_packed_mfma.hip), operation for operation: blocks of 32 keys, their
+// references and sums one after the other.  What can be done side by side without changing them is: the
+// scores of a unit's blocks (a block per wave), then the weights, then the weighted values (a part of
+// head_dim per wave, over all of the unit's blocks in order).  Through LDS go the blocks' largest scores,
+// the rounded weights (as MFMA operands) and their sums.
+//
+// What bounds it: HBM.  K and V of a unit have a buffer each: the next unit's K lands while this one's
+// weights and values are worked on, its V during the next unit's scores.
+#include "kvg_launch.h"
+#include "kvg_packed_mfma.h"
+
+#include <type_traits>
+
+namespace kvg {
+
+namespace {
+
+// s_waitcnt operand that waits for vmcnt <= n alone (gfx9 encoding: bits 3:0 and 15:14)
+constexpr int vm_wait(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
+constexpr int kLgkmWait = 0xC07F;      // lgkmcnt(0) alone
+constexpr int kStream = 2;             // buffer load policy: nontemporal (every row is read once)
+
+// kWaves: waves of a workgroup, a block of 32 keys and D / kWaves dimensions each
+template <typename T, int D, int kWaves>
+__global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAttnArgs a) {
+  constexpr bool kFp8 = sizeof(T) == 1;
+  constexpr int RB = D * (int)sizeof(T), NCH = RB / 16, NS = D / 16;
+  constexpr int NDW = D / 32 / kWaves;               // 32-wide blocks of head_dim per wave
+  constexpr int kUnitKeys = 32 * kWaves;
+  constexpr int kLoads = 2 * kPage * RB / 1024;      // direct loads of a wave's block, K or V
+  static_assert(D / 32 % kWaves == 0 && kPackedSeg % kUnitKeys == 0, "units");
+  using SW = SwzTile<RB, kFp8>;
+  __shared__ __attribute__((aligned(1024))) uint4 s_k[kUnitKeys * NCH];
+  __shared__ __attribute__((aligned(1024))) uint4 s_v[kUnitKeys * NCH];
+  __shared__ uint4 s_p[kWaves][2][64];
+  __shared__ float s_mx[kWaves][32], s_sum[kWaves][32];
+  __shared__ int s_bad;
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int lrow = lane & 31, half = lane >> 5;
+  const int lg = 31 - __builtin_clz(a.group);
+  // (layer, segment, sequence, KV head), the KV head fastest
+  uint32_t id = blockIdx.x;
+  const int g = (int)(id % (uint32_t)a.Hkv);
+  id /= (uint32_t)a.Hkv;
+  const int b = (int)(id % (uint32_t)a.seqs.batch);
+  id /= (uint32_t)a.seqs.batch;
+  const int seg = (int)(id % (uint32_t)a.n_seg);
+  const int l = (int)(id / (uint32_t)a.n_seg);
+  const int32_t* bt = a.seqs.tables + (int64_t)b * a.seqs.max_pages;
+  // page ids of the segment, one per lane (requested with the sequence's range)
+  const int32_t pg = bt[min(seg * (kPackedSeg / kPage) + (lane & 31), a.seqs.max_pages - 1)];
+  const SeqRange sq = seq_range(a.seqs, b);
+  if (sq.len == 0 || !is_few(a, sq)) return;
+  const int n_pairs = sq.len << lg;
+  const int W = layer_window(a, l);
+  const int first_n = sq.ctx, n_hi = sq.ctx + sq.len;        // the first row's index; keys [0, n_hi) are needed
+  const int first_lo = window_start(W, first_n + 1), mask_lo = window_start(W, n_hi);
+  const int k_end = min(n_hi, (seg + 1) * kPackedSeg);
+  const int k_begin = max(seg * kPackedSeg, first_lo & ~(kUnitKeys - 1));
+  if (k_begin >= k_end) return;
+  const int n_units = (k_end - k_begin + kUnitKeys - 1) / kUnitKeys;
+
+  const int pair = min(lrow, n_pairs - 1);
+  const bool pair_ok = lrow < n_pairs;
+  const int row = pair >> lg, head = g * a.group + (pair & (a.group - 1));
+  const int row_n = sq.ctx + row, row_lo = window_start(W, row_n + 1);
+
+  const int64_t lbase = (int64_t)(a.layer0 + l) * a.layer_elems;
+  const T* kpool = reinterpret_cast<const T*>(a.k_pool) + lbase;
+  const T* vpool = reinterpret_cast<const T*>(a.v_pool) + lbase;
+
+  // ---- loads of this wave's block of unit u (two pages, K or V); rows from k_end on read as zeros
+  constexpr int RPL = 64 / NCH;                      // rows per load
+  const int lr = lane / NCH;
+  const uint32_t k_off = lr * RB + 16 * ((lane % NCH) ^ SW::k(lr));
+  const uint32_t v_off = lr * RB + 16 * ((lane % NCH) ^ SW::v(lr));
+  auto issue = [&](const T* pool, uint4* dst, int u, bool is_v) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int key = k_begin + u * kUnitKeys + wave * 32 + p * kPage;
+      int32_t page = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_readlane(pg, (key / kPage) & 31));
+      page = (page >= 0 && page < a.n_pages) ? page : 0;
+      const int rows = __builtin_amdgcn_readfirstlane(min(max(k_end - key, 0), kPage));
+      const int64_t off = ((int64_t)page * a.Hkv + g) * kPage * D;
+      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(pool + off), 0, rows * RB, kBufferWord3);
+      lds_char* to = (lds_char*)(lds_void*)(dst + (wave * 32 + p * kPage) * NCH);
+#pragma unroll
+      for (int j = 0; j < kPage / RPL; ++j) {
+        const int r0 = j * RPL;
+        const uint32_t at = r0 * RB + (is_v ? v_off ^ (16 * SW::v(r0)) : k_off ^ (16 * SW::k(r0)));
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(to + r0 * RB), 16, at, 0, 0, kStream);
+      }
+    }
+  };
+  // queries (B operand of S^T = K Q^T), zeros past the pairs
+  uint4 qf[NS];
+  {
+    const int64_t tok = (int64_t)l * a.seqs.n_tokens + sq.row0 + row;
+    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + tok * a.q_stride + (int64_t)head * D;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) qf[s] = ld16(qp + (2 * s + half) * 8);
+  }
+  issue(kpool, s_k, 0, false);
+  issue(vpool, s_v, 0, true);
+  if (threadIdx.x == 0) s_bad = 0;                   // read and written behind the first unit's barriers
+#pragma unroll
+  for (int s = 0; s < NS; ++s) qf[s] = pair_ok ? qf[s] : make_uint4(0, 0, 0, 0);
+
+  const lds_char* kbase = (const lds_char*)(lds_void*)s_k + wave * 32 * RB;
+  const lds_char* vbase = (const lds_char*)(lds_void*)s_v;
+  const uint32_t k_lane = k_lane_base<RB, kFp8>(lane), v_lane = v_lane_base<RB, kFp8>(lane);
+  f32x16 o[NDW];
+#pragma unroll
+  for (int d = 0; d < NDW; ++d) o[d] = splat(0.0f);
+  float m = -INFINITY, lsum = 0.0f;
+
+  for (int u = 0; u < n_units; ++u) {
+    const int key0 = k_begin + u * kUnitKeys;
+    // ---- scores of this wave's block; its K has landed (V's loads may be in flight)
+    __builtin_amdgcn_s_waitcnt(vm_wait(kLoads));
+    asm volatile("" ::: "memory");
+    f32x16 s = splat(0.0f);
+#pragma unroll
+    for (int ss = 0; ss < NS; ++ss) s = mfma32(k_fragment<kFp8>(kbase, k_lane, ss), qf[ss], s);
+    __builtin_amdgcn_s_waitcnt(kLgkmWait);           // read: the buffer takes the next unit's
+    asm volatile("" ::: "memory");
+    issue(kpool, s_k, u + 1, false);
+    const int kb = key0 + 32 * wave;
+    if (kb + 31 > first_n || kb < mask_lo) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = kb + half * 4 + (r >> 2) * 8 + (r & 3);
+        s[r] = (key <= row_n && key >= row_lo) ? s[r] : -INFINITY;
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    const float2 mh = halves32(mx);
+    s_mx[wave][lrow] = fmaxf(mh.x, mh.y) * a.scale_log2;      // both halves of the wave, the same value
+    __syncthreads();
+    // ---- the references of the unit's blocks in order (every wave alike), this wave's weights
+    float alpha[kWaves], m_ref = 0.0f;
+    bool raised[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      alpha[w] = raise_reference(m, s_mx[w][lrow], raised[w]);
+      if (w == wave) m_ref = m == -INFINITY ? 0.0f : m;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -m_ref));
+    float psum = 0.0f;
+    s_p[wave][0][lane] = round_weights(s, 0, psum);
+    s_p[wave][1][lane] = round_weights(s, 1, psum);
+    const float2 ph = halves32(psum);
+    s_sum[wave][lrow] = ph.x + ph.y;
+    // V of the unit has landed (the next unit's K may be in flight)
+    __builtin_amdgcn_s_waitcnt(vm_wait(kLoads));
+    __syncthreads();
+    // a masked key weighs 0, and 0 times an Inf or NaN would reach rows that do not see it (see the tile kernel)
+    if (min(key0 + kUnitKeys, n_hi) - 1 > first_n || key0 < mask_lo) {
+      if (finite_rows<T, NCH>(s_v + wave * 32 * NCH, lane) | finite_rows<T, NCH>(s_v + (wave * 32 + kPage) * NCH, lane)) s_bad = 1;
+      __syncthreads();
+    }
+    // ---- this wave's dimensions over the unit's blocks
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      lsum = lsum * alpha[w] + s_sum[w][lrow];
+      if (__builtin_amdgcn_ballot_w64(raised[w]) != 0) {
+#pragma unroll
+        for (int d = 0; d < NDW; ++d) o[d] *= alpha[w];
+      }
+      const uint4 p0 = s_p[w][0][lane], p1 = s_p[w][1][lane];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int d = 0; d < NDW; ++d)
+          o[d] = mfma32(v_fragment<RB, kFp8>(vbase + (32 * w + 16 * ks) * RB, v_lane, wave * NDW + d), ks ? p1 : p0, o[d]);
+    }
+    __syncthreads();                                 // V, weights and sums are read: the next unit's may come
+    issue(vpool, s_v, u + 1, true);
+  }
+  __builtin_amdgcn_s_waitcnt(vm_wait(0));            // the empty loads past the last unit write LDS: none may outlive the workgroup
+
+  // ---- the segment's partial, or the result when there is one segment
+  const int rank = a.n_seg > 1 ? few_rows_before(a, b) : 0;
+  if (a.n_seg > 1 && rank + sq.len > a.few_rows) return;     // overlapping ranges hold more rows than there are
+  auto slot_of = [&](int p) -> int64_t {
+    const int h = g * a.group + (p & (a.group - 1));
+    if (a.n_seg > 1) return (((int64_t)l * a.few_rows + rank + (p >> lg)) * a.Hq + h) * a.n_seg + seg;
+    return ((int64_t)l * a.seqs.n_tokens + sq.row0 + (p >> lg)) * a.Hq + h;
+  };
+  if (pair_ok) {
+    const int64_t at = slot_of(pair);
+    if (a.n_seg > 1) {
+      float* op = a.part_acc + at * D + wave * NDW * 32;
+#pragma unroll
+      for (int d = 0; d < NDW; ++d)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4)
+          *reinterpret_cast<float4*>(op + d * 32 + r4 * 8 + half * 4) =
+              make_float4(o[d][r4 * 4], o[d][r4 * 4 + 1], o[d][r4 * 4 + 2], o[d][r4 * 4 + 3]);
+      if (wave == 0 && half == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(m, lsum);
+    } else {
+      const float inv = 1.0f / lsum;
+      uint16_t* op = static_cast<uint16_t*>(a.out) + at * D + wave * NDW * 32;
+#pragma unroll
+      for (int d = 0; d < NDW; ++d)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4)
+          *reinterpret_cast<uint2*>(op + d * 32 + r4 * 8 + half * 4) =
+              make_uint2(pack_bf16_rne(o[d][r4 * 4] * inv, o[d][r4 * 4 + 1] * inv),
+                         pack_bf16_rne(o[d][r4 * 4 + 2] * inv, o[d][r4 * 4 + 3] * inv));
+    }
+  }
+  if (s_bad != 0) {                                  // the values that are not finite, to the rows that see them
+    __builtin_amdgcn_s_waitcnt(vm_wait(0));
+    __syncthreads();
+    for (int key = k_begin + wave; key < k_end; key += kWaves) {
+      const int32_t page = bt[key / kPage];
+      const T* vr = vpool + (((int64_t)(page >= 0 && page < a.n_pages ? page : 0) * a.Hkv + g) * kPage + key % kPage) * D;
+      for (int x = lane; x < D; x += 64) {
+        const float v = load_value(vr + x);
+        if (fabsf(v) < INFINITY) continue;
+        for (int p = 0; p < n_pairs; ++p) {
+          const int n = sq.ctx + (p >> lg);
+          if (key > n || key < window_start(W, n + 1)) continue;
+          const int64_t at = slot_of(p);
+          if (a.n_seg > 1)
+            a.part_acc[at * D + x] = v;
+          else
+            static_cast<uint16_t*>(a.out)[at * D + x] = (uint16_t)(__float_as_uint(v) >> 16);
+        }
+      }
+    }
+  }
+}
+
+// out = the segments of a row and query head folded in ascending order: a workgroup of D lanes (a dimension each).
+template <int D, bool kFew>
+__global__ __launch_bounds__(D) void packed_fold_kernel(const PackedAttnArgs a) {
+  const int64_t id = blockIdx.x;                     // (layer, row of the launch, query head)
+  const int h = (int)(id % a.Hq);
+  const int rows = kFew ? a.few_rows : a.seqs.n_tokens;
+  const int t = (int)(id / a.Hq % rows), l = (int)(id / a.Hq / rows);
+  const SeqUnit u = kFew ? find_unit(a.seqs, t, [&](const SeqRange& s) { return is_few(a, s) ? s.len : 0; }) : find_token(a.seqs, t);
+  if (u.b < 0 || (!kFew && is_few(a, u.range))) return;
+  const int n = u.range.ctx + u.at;
+  const int s_lo = window_start(layer_window(a, l), n + 1) / kPackedSeg, s_hi = n / kPackedSeg;
+  const float* ml = a.part_ml + id * a.n_seg * 2;
+  const float* acc = a.part_acc + id * a.n_seg * D + threadIdx.x;
+  float m_run = -INFINITY, l_run = 0.0f, o_run = 0.0f;
+#pragma unroll 8
+  for (int s = s_lo; s <= s_hi; ++s) {
+    const float2 x = *reinterpret_cast<const float2*>(ml + 2 * s);
+    const FoldFactors f = fold_factors(m_run, l_run, x.x, x.y);
+    o_run = fmaf(acc[(int64_t)s * D], f.part, o_run * f.run);
+  }
+  const int64_t row = (int64_t)l * a.seqs.n_tokens + u.range.row0 + u.at;
+  static_cast<uint16_t*>(a.out)[(row * a.Hq + h) * D + threadIdx.x] = __builtin_bit_cast(uint16_t, (__bf16)(o_run * (1.0f / l_run)));
+}
+
+template <typename T>
+hipError_t launch_few_t(const PackedAttnArgs& a, hipStream_t stream) {
+  const unsigned grid = (unsigned)packed_few_workgroups(a);
+  switch (a.D) {
+    case 64: packed_few_kernel<T, 64, 2><<<grid, 128, 0, stream>>>(a); break;
+    case 128: packed_few_kernel<T, 128, 4><<<grid, 256, 0, stream>>>(a); break;
+    case 256: packed_few_kernel<T, 256, 4><<<grid, 256, 0, stream>>>(a); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+template <bool kFew>
+hipError_t launch_fold_t(const PackedAttnArgs& a, hipStream_t stream) {
+  const unsigned grid = (unsigned)((int64_t)a.n_layers * (kFew ? a.few_rows : a.seqs.n_tokens) * a.Hq);
+  switch (a.D) {
+    case 64: packed_fold_kernel<64, kFew><<<grid, 64, 0, stream>>>(a); break;
+    case 128: packed_fold_kernel<128, kFew><<<grid, 128, 0, stream>>>(a); break;
+    case 256: packed_fold_kernel<256, kFew><<<grid, 256, 0, stream>>>(a); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_packed_few(const PackedAttnArgs& a, int dtype, hipStream_t stream) {
+  if (dtype == kDtypeBf16) return launch_few_t<uint16_t>(a, stream);
+  if (dtype == kDtypeFp8) return launch_few_t<uint8_t>(a, stream);
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_packed_fold(const PackedAttnArgs& a, bool few, hipStream_t stream) {
+  return few ? launch_fold_t<true>(a, stream) : launch_fold_t<false>(a, stream);
+}
+
+}  // namespace kvg

@@ -7,7 +7,8 @@
 // A row's sums have one order, whatever the launch: keys in blocks of 32, an online softmax over the blocks of a
 // segment of kSeg keys (absolute multiples), and the segments' states folded in ascending order.  A
 // workgroup that walks all keys folds in registers; split launches leave one partial per segment for
-// packed_fold_kernel, which folds them with the same operations.
+// packed_fold_kernel (kvg_packed_few.hip), which folds them with the same operations.  Sequences of at most kFewPairs
+// pairs are left to packed_few_kernel, which takes the same operations too.
 //
 //   S^T = K Q^T    A = K rows from LDS, B = the pairs' queries in registers; a lane owns one pair (lane % 32) and 16
 //                  of a block's 32 keys, the other 16 are in lane ^ 32
@@ -17,9 +18,7 @@
 //                  gives its value exactly and rounding errors of the heavy weights cancel
 //   O^T += V^T P^T A = V^T fragments (ds_read_b64_tr), B = P straight from the S^T registers
 #include "kvg_launch.h"
-#include "kvg_mfma.h"
-#include "kvg_packed.h"
-#include "kvg_rows.h"
+#include "kvg_packed_mfma.h"
 
 #include <math.h>
 
@@ -32,70 +31,10 @@ namespace {
 constexpr int kTileKeys = 64;
 constexpr int kSegTiles = kPackedSeg / kTileKeys;
 constexpr int kWaves = 4;
-constexpr float kStep = 8.0f;          // grid of the references, log2 units
-
-// The reference that a largest score (log2 units) asks for.
-__device__ __forceinline__ float reference_of(float mx) { return ceilf(mx * (1.0f / kStep)) * kStep; }
-
-// LDS rows hold their 16-byte chunks at position chunk ^ swizzle(row), XOR-linear in the row bits.  K is read as one chunk
-// of 32 consecutive rows per lane half, V transposed (bf16: four rows x two or four chunks, fp8: rows
-// {0..3, 8..11} (+ 4) of a 16-row step).
-template <int RB, bool kFp8>
-struct SwzTile {
-  __device__ static __forceinline__ int k(int r) {
-    if constexpr (kFp8) return RB == 256 ? (r & 15) : RB == 128 ? ((r >> 1) & 7) : ((r >> 2) & 3);
-    return RB >= 256 ? (r & 15) : (r & 7);
-  }
-  __device__ static __forceinline__ int v(int r) {
-    if constexpr (kFp8)
-      return RB == 256 ? (r & 15) : RB == 128 ? (((r >> 1) & 1) | (((r >> 3) & 1) << 1)) : ((r >> 3) & 1);
-    return RB >= 256 ? ((0xCA60 >> (4 * (r & 3))) & 15) : 2 * (r & 3);
-  }
-};
-
-__device__ __forceinline__ float load_value(const uint16_t* p) { return bf16_bits_to_f32(*p); }
-__device__ __forceinline__ float load_value(const uint8_t* p) { return Elem<uint8_t>::get(make_uint4(*p, 0, 0, 0), 0); }
-
-// whether one of the values is Inf or NaN (bf16: all exponent bits set)
-__device__ __forceinline__ bool bad_values(const uint4& x, uint16_t) {
-  bool bad = false;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const uint32_t v = (&x.x)[w];
-    bad = bad || (v & 0x7F80u) == 0x7F80u || (v & 0x7F800000u) == 0x7F800000u;
-  }
-  return bad;
-}
-// fp8: NaN codes 0x7F and 0xFF
-__device__ __forceinline__ bool bad_values(const uint4& x, uint8_t) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) m |= ((&x.x)[w] & 0x7F7F7F7Fu) + 0x01010101u;
-  return (m & 0x80808080u) != 0;
-}
-
-// The page of value rows at p with every Inf and NaN set to 0; whether there was one.
-template <typename T, int NCH>
-__device__ __forceinline__ bool finite_rows(uint4* p, int lane) {
-  bool any = false;
-#pragma unroll 2
-  for (int i = lane; i < kPage * NCH; i += 64) {
-    uint4 x = p[i];
-    if (!bad_values(x, T{})) continue;
-    any = true;
-    T* v = reinterpret_cast<T*>(p + i);
-    for (int e = 0; e < (int)(16 / sizeof(T)); ++e)
-      if (!(fabsf(load_value(v + e)) < INFINITY)) v[e] = 0;
-  }
-  return __builtin_amdgcn_ballot_w64(any) != 0;
-}
-
-__device__ __forceinline__ f32x16 splat(float x) { return (f32x16)(x); }
-
 // T: cache storage (uint16_t bf16, uint8_t fp8 E4M3).  kBlocks: blocks of 32 pairs per wave.
 // kSplit: a workgroup takes one segment and leaves its partial.
 template <typename T, int D, int kBlocks, bool kSplitKeys>
-__global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_kernel(const PackedAttnArgs a) {
+__global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_kernel(const PackedAttnArgs a) {
   constexpr bool kFp8 = sizeof(T) == 1;
   constexpr int RB = D * (int)sizeof(T);   // bytes per cache row
   constexpr int NCH = RB / 16;             // 16-byte chunks per row
@@ -129,7 +68,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
     id /= (uint32_t)a.n_seg;
   }
   const int l = (int)id;
-  const SeqUnit u = find_unit(a.seqs, slot, [&](const SeqRange& s) { return (int)((((int64_t)s.len << lg) + BM - 1) / BM); });
+  const SeqUnit u = find_unit(a.seqs, slot, [&](const SeqRange& s) {
+    return is_few(a, s) ? 0 : (int)((((int64_t)s.len << lg) + BM - 1) / BM);
+  });
   if (u.b < 0) return;
   const SeqRange sq = u.range;
   const int tile_id = u.count - 1 - u.at;
@@ -225,22 +166,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
     }
   }
 
-  // ---- LDS addressing (row base and chunk; a constant XORed into the chunk bits permutes a row's chunks)
-  //   K step ss of block kb: row kb * 32 + lrow, chunk 2 ss + half (fp8: 8 bytes at 16 ss + 8 half)
-  //   V^T step (ks, d), 16 keys: 16-lane group tr_m = lane / 16, tr_k = lane % 16: bf16 rows 4 (tr_m / 2) + tr_k / 4 (and 8
-  //   further), 8 bytes at dim 32 d + 16 (tr_m % 2) + 4 (tr_k % 4); fp8 row 4 (tr_m / 2) + {0..3, 8..11}[tr_k / 2], 8 bytes
-  //   at dim 32 d + 16 (tr_m % 2) + 8 (tr_k % 2)
-  const int tr_k = lane & 15, tr_m = lane >> 4;
-  uint32_t k_lane, v_lane;
-  if constexpr (kFp8) {
-    const int kk = 4 * (tr_m >> 1) + ((tr_k >> 1) & 3) + 8 * (tr_k >> 3);
-    k_lane = lrow * RB + 16 * SW::k(lrow) + 8 * half;
-    v_lane = kk * RB + 16 * ((tr_m & 1) ^ SW::v(kk)) + 8 * (tr_k & 1);
-  } else {
-    const int rr = (tr_m >> 1) * 4 + (tr_k >> 2);
-    k_lane = lrow * RB + 16 * (half ^ SW::k(lrow));
-    v_lane = rr * RB + 8 * (tr_k & 1) + 16 * ((2 * (tr_m & 1) + ((tr_k & 3) >> 1)) ^ SW::v(rr));
-  }
+  const uint32_t k_lane = k_lane_base<RB, kFp8>(lane), v_lane = v_lane_base<RB, kFp8>(lane);
 
   if (tid == 0) s_bad = 0;              // read and written behind the first tile's barrier
   using Stage0 = std::integral_constant<int, 0>;
@@ -274,28 +200,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
     };
     const lds_char* kbase = (const lds_char*)(lds_void*)(ST ? sB_K1 : sB_K0);
     const lds_char* vbase = (const lds_char*)(lds_void*)(ST ? sA_V1 : sA_V0);
-    auto kread = [&](int f) -> uint4 {    // fragment f = kb * NS + ss
-      const int kb = f / NS, ss = f % NS;
-      if constexpr (kFp8) {
-        const u32x2 w = *reinterpret_cast<const lds_u32x2*>(kbase + (k_lane ^ (uint32_t)(16 * ss)) + kb * 32 * RB);
-        return widen_fp8x8(w.x, w.y);
-      } else {
-        return __builtin_bit_cast(uint4, *reinterpret_cast<const lds_u32x4*>(kbase + (k_lane ^ (uint32_t)(32 * ss)) + kb * 32 * RB));
-      }
-    };
-    auto vread = [&](int t) -> uint4 {    // fragment t = ks * ND + d
-      const int ks = t / ND, d = t % ND;
-      if constexpr (kFp8) {
-        const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vbase + (v_lane ^ (uint32_t)(32 * d)) + ks * 16 * RB));
-        return widen_fp8x8((uint32_t)w.x, (uint32_t)w.y);
-      } else {
-        const uint32_t at = (v_lane ^ (uint32_t)(64 * d)) + ks * 16 * RB;
-        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vbase + at));
-        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vbase + at + 8 * RB));
-        const uint2 lo2 = __builtin_bit_cast(uint2, lo), hi2 = __builtin_bit_cast(uint2, hi);
-        return make_uint4(lo2.x, lo2.y, hi2.x, hi2.y);
-      }
-    };
+    auto kread = [&](int f) { return k_fragment<kFp8>(kbase + f / NS * 32 * RB, k_lane, f % NS); };        // f = block * NS + step
+    auto vread = [&](int t) { return v_fragment<RB, kFp8>(vbase + t / ND * 16 * RB, v_lane, t % ND); };     // t = 16-key step * ND + d
 
     f32x16 s[2][kBlocks];
     if constexpr (D > 128) {
@@ -330,11 +236,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
         for (int r = 4 * j; r < 4 * j + 4; ++r) x.mx = fmaxf(x.mx, s[kb][rb][r]);
       } else if (j == 4) {
         const float2 mh = halves32(x.mx);
-        const float mx = fmaxf(mh.x, mh.y) * a.scale_log2;
-        x.raised = mx > m[rb];
-        const float up = reference_of(mx);
-        x.alpha = x.raised ? __builtin_amdgcn_exp2f(m[rb] - up) : 1.0f;
-        m[rb] = x.raised ? up : m[rb];
+        x.alpha = raise_reference(m[rb], fmaxf(mh.x, mh.y) * a.scale_log2, x.raised);
         x.m_ref = m[rb] == -INFINITY ? 0.0f : m[rb];      // no key seen yet: every weight is 0
         x.psum = 0.0f;
       } else if (j < 13) {
@@ -342,14 +244,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
         for (int r = 2 * (j - 5); r < 2 * (j - 5) + 2; ++r)
           s[kb][rb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][rb][r], a.scale_log2, -x.m_ref));
       } else if (j < 15) {
-        const int hs = j - 13;
-        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-        uint4& f = pf[kb][rb][hs];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          (&f.x)[w] = pack_bf16_rne(s[kb][rb][8 * hs + 2 * w], s[kb][rb][8 * hs + 2 * w + 1]);
-          x.psum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (&f.x)[w]), ones, x.psum, false);
-        }
+        pf[kb][rb][j - 13] = round_weights(s[kb][rb], j - 13, x.psum);
       } else {
         const float2 ph = halves32(x.psum);
         lsum[rb] = lsum[rb] * x.alpha + (ph.x + ph.y);
@@ -363,10 +258,6 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
           for (int d = 0; d < ND; ++d) o[rb][d] *= st[rb].alpha;
         }
     };
-    auto mfma = [](const uint4& x, const uint4& y, const f32x16& c) {
-      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), as_bf16x8(y), c, 0, 0, 0);
-    };
-
     // K fragments of both blocks form one stream read LK ahead of their MFMAs, V^T fragments one read LV ahead, whose first
     // LV are issued with block 1's scores
     if constexpr (D <= 128) {
@@ -382,7 +273,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
           if (ss + LF < NS) kf[(ss + LF) % RF] = kread(kb * NS + ss + LF);
           issue_step(kb * NS + ss);
 #pragma unroll
-          for (int rb = 0; rb < kBlocks; ++rb) s[0][rb] = ss ? mfma(kf[ss % RF], qf[rb][ss], s[0][rb]) : mfma(kf[0], qf[rb][0], splat(0.0f));
+          for (int rb = 0; rb < kBlocks; ++rb) s[0][rb] = ss ? mfma32(kf[ss % RF], qf[rb][ss], s[0][rb]) : mfma32(kf[0], qf[rb][0], splat(0.0f));
         }
         mask_block(kb);
         auto vget = [&](int t) { return vread(kb * 2 * ND + t); };
@@ -397,7 +288,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
         for (int t = 0; t < 2 * ND; ++t) {
           if (t + LF < 2 * ND) vf[(t + LF) % RF] = vget(t + LF);
 #pragma unroll
-          for (int rb = 0; rb < kBlocks; ++rb) o[rb][t % ND] = mfma(vf[t % RF], pf[0][rb][t / ND], o[rb][t % ND]);
+          for (int rb = 0; rb < kBlocks; ++rb) o[rb][t % ND] = mfma32(vf[t % RF], pf[0][rb][t / ND], o[rb][t % ND]);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -424,7 +315,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
       issue_step(ss);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int rb = 0; rb < kBlocks; ++rb) s[0][rb] = mfma(kf[ss % RK], qf[rb][ss], s[0][rb]);
+      for (int rb = 0; rb < kBlocks; ++rb) s[0][rb] = mfma32(kf[ss % RK], qf[rb][ss], s[0][rb]);
       __builtin_amdgcn_sched_barrier(0);
     }
     mask_block(0);
@@ -438,7 +329,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
       issue_step(NS + ss);
       if (ss >= NS - LV) vfetch(ss - (NS - LV));
 #pragma unroll
-      for (int rb = 0; rb < kBlocks; ++rb) s[1][rb] = mfma(kf[f % RK], qf[rb][ss], s[1][rb]);
+      for (int rb = 0; rb < kBlocks; ++rb) s[1][rb] = mfma32(kf[f % RK], qf[rb][ss], s[1][rb]);
 #pragma unroll
       for (int j = ss * kPieces / NS; j < (ss + 1) * kPieces / NS; ++j) soft_piece(0, j % kBlocks, j / kBlocks);
       __builtin_amdgcn_sched_barrier(0);
@@ -450,7 +341,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
     for (int t = 0; t < 2 * ND; ++t) {
       vfetch(t + LV);
 #pragma unroll
-      for (int rb = 0; rb < kBlocks; ++rb) o[rb][t % ND] = mfma(vf[t % RV], pf[0][rb][t / ND], o[rb][t % ND]);
+      for (int rb = 0; rb < kBlocks; ++rb) o[rb][t % ND] = mfma32(vf[t % RV], pf[0][rb][t / ND], o[rb][t % ND]);
 #pragma unroll
       for (int j = t * kPieces / (2 * ND); j < (t + 1) * kPieces / (2 * ND); ++j) soft_piece(1, j % kBlocks, j / kBlocks);
       __builtin_amdgcn_sched_barrier(0);
@@ -461,7 +352,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
       vfetch(t + LV);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int rb = 0; rb < kBlocks; ++rb) o[rb][t % ND] = mfma(vf[t % RV], pf[1][rb][t / ND - 2], o[rb][t % ND]);
+      for (int rb = 0; rb < kBlocks; ++rb) o[rb][t % ND] = mfma32(vf[t % RV], pf[1][rb][t / ND - 2], o[rb][t % ND]);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -470,16 +361,13 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
     if constexpr (!kSplitKeys) {
 #pragma unroll
       for (int rb = 0; rb < kBlocks; ++rb) {
-        const float m_new = fmaxf(m_run[rb], m[rb]);
-        const float f_run = merge_factor(m_run[rb], m_new), f = merge_factor(m[rb], m_new);
-        m_run[rb] = m_new;
-        l_run[rb] = fmaf(lsum[rb], f, l_run[rb] * f_run);
-        if (__builtin_amdgcn_ballot_w64(f_run != 1.0f || f != 1.0f) == 0) {
+        const FoldFactors f = fold_factors(m_run[rb], l_run[rb], m[rb], lsum[rb]);
+        if (__builtin_amdgcn_ballot_w64(f.run != 1.0f || f.part != 1.0f) == 0) {
 #pragma unroll
           for (int d = 0; d < ND; ++d) o_run[rb][d] += o[rb][d];
         } else {
 #pragma unroll
-          for (int d = 0; d < ND; ++d) o_run[rb][d] = __builtin_elementwise_fma(o[rb][d], splat(f), o_run[rb][d] * f_run);
+          for (int d = 0; d < ND; ++d) o_run[rb][d] = __builtin_elementwise_fma(o[rb][d], splat(f.part), o_run[rb][d] * f.run);
         }
         m[rb] = -INFINITY;
         lsum[rb] = 0.0f;
@@ -559,45 +447,13 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_mfma_ker
   }
 }
 
-// out = the rows' segments folded in ascending order, a wave per (layer, token, query head).
-template <int D>
-__global__ __launch_bounds__(256) void packed_fold_kernel(const PackedAttnArgs a) {
-  constexpr int N = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (id >= (int64_t)a.n_layers * a.seqs.n_tokens * a.Hq) return;
-  const int64_t tok = id / a.Hq;
-  const int l = (int)(tok / a.seqs.n_tokens), t = (int)(tok % a.seqs.n_tokens);
-  const SeqUnit u = find_token(a.seqs, t);
-  if (u.b < 0) return;
-  const int n = u.range.ctx + u.at;
-  const int s_lo = window_start(layer_window(a, l), n + 1) / kPackedSeg, s_hi = n / kPackedSeg;
-  float m_run = -INFINITY, l_run = 0.0f, o_run[N] = {};
-  for (int s = s_lo; s <= s_hi; ++s) {
-    const int64_t at = id * a.n_seg + s;
-    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
-    const float m_new = fmaxf(m_run, ml.x);
-    const float f_run = merge_factor(m_run, m_new), f = merge_factor(ml.x, m_new);
-    m_run = m_new;
-    l_run = fmaf(ml.y, f, l_run * f_run);
-#pragma unroll
-    for (int x = 0; x < N; ++x) o_run[x] = fmaf(a.part_acc[at * D + lane * N + x], f, o_run[x] * f_run);
-  }
-  const float inv = 1.0f / l_run;
-  uint16_t* op = static_cast<uint16_t*>(a.out) + id * D + lane * N;
-#pragma unroll
-  for (int x = 0; x < N; ++x) op[x] = __builtin_bit_cast(uint16_t, (__bf16)(o_run[x] * inv));
-}
-
 template <typename T, int D, int kBlocks>
 hipError_t launch_d(const PackedAttnArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)packed_mfma_workgroups(a));
+  const dim3 grid((unsigned)packed_tile_workgroups(a));
   if (a.n_seg > 1)
-    packed_mfma_kernel<T, D, kBlocks, true><<<grid, 64 * kWaves, 0, stream>>>(a);
+    packed_tiles_kernel<T, D, kBlocks, true><<<grid, 64 * kWaves, 0, stream>>>(a);
   else
-    packed_mfma_kernel<T, D, kBlocks, false><<<grid, 64 * kWaves, 0, stream>>>(a);
-  if (a.n_seg > 1)
-    packed_fold_kernel<D><<<(unsigned)(((int64_t)a.n_layers * a.seqs.n_tokens * a.Hq + 3) / 4), 256, 0, stream>>>(a);
+    packed_tiles_kernel<T, D, kBlocks, false><<<grid, 64 * kWaves, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -613,9 +469,9 @@ hipError_t launch_t(const PackedAttnArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-int packed_mfma_pairs(int D) { return 32 * kWaves * (D == 64 ? 2 : 1); }
+int packed_tile_pairs(int D) { return 32 * kWaves * (D == 64 ? 2 : 1); }
 
-hipError_t launch_packed_mfma(const PackedAttnArgs& a, int dtype, hipStream_t stream) {
+hipError_t launch_packed_tiles(const PackedAttnArgs& a, int dtype, hipStream_t stream) {
   if (dtype == kDtypeBf16) return launch_t<uint16_t>(a, stream);
   if (dtype == kDtypeFp8) return launch_t<uint8_t>(a, stream);
   return hipErrorInvalidValue;
