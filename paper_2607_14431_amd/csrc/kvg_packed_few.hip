@@ -27,14 +27,15 @@ constexpr int kStream = 2;             // buffer load policy: nontemporal (every
 template <typename T, int D, int kWaves>
 __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAttnArgs a) {
   constexpr bool kFp8 = sizeof(T) == 1;
-  constexpr int RB = D * (int)sizeof(T), NCH = RB / 16, NS = D / 16;
+  constexpr int RB = D * (int)sizeof(T), NS = D / 16;
   constexpr int NDW = D / 32 / kWaves;               // 32-wide blocks of head_dim per wave
   constexpr int kUnitKeys = 32 * kWaves;
-  constexpr int kLoads = 2 * kPage * RB / 1024;      // direct loads of a wave's block, K or V
+  using KR = KRows<RB>;
+  using VR = VRows<RB>;
+  constexpr int kLoads = 2 * KR::kPageLoads;         // direct loads of a wave's block, K or V
   static_assert(D / 32 % kWaves == 0 && kPackedSeg % kUnitKeys == 0, "units");
-  using SW = SwzTile<RB, kFp8>;
-  __shared__ __attribute__((aligned(1024))) uint4 s_k[kUnitKeys * NCH];
-  __shared__ __attribute__((aligned(1024))) uint4 s_v[kUnitKeys * NCH];
+  __shared__ __attribute__((aligned(1024))) char s_k[2 * kWaves * KR::kPageBytes];
+  __shared__ __attribute__((aligned(1024))) char s_v[2 * kWaves * VR::kPageBytes];
   __shared__ uint4 s_p[kWaves][2][64];
   __shared__ float s_mx[kWaves][32], s_sum[kWaves][32];
   __shared__ int s_bad;
@@ -42,14 +43,15 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int lrow = lane & 31, half = lane >> 5;
   const int lg = 31 - __builtin_clz(a.group);
-  // (layer, segment, sequence, KV head), the KV head fastest
+  // (layer, sequence, segment, KV head), the KV head fastest: workgroups without work come in runs (see the tile kernel)
   uint32_t id = blockIdx.x;
   const int g = (int)(id % (uint32_t)a.Hkv);
   id /= (uint32_t)a.Hkv;
+  int seg = (int)(id % (uint32_t)a.n_seg);
+  id /= (uint32_t)a.n_seg;
   const int b = (int)(id % (uint32_t)a.seqs.batch);
-  id /= (uint32_t)a.seqs.batch;
-  const int seg = (int)(id % (uint32_t)a.n_seg);
-  const int l = (int)(id / (uint32_t)a.n_seg);
+  const int l = (int)(id / (uint32_t)a.seqs.batch);
+  seg = (int)((uint32_t)(seg + b) % (uint32_t)a.n_seg);
   const int32_t* bt = a.seqs.tables + (int64_t)b * a.seqs.max_pages;
   // page ids of the segment, one per lane (requested with the sequence's range)
   const int32_t pg = bt[min(seg * (kPackedSeg / kPage) + (lane & 31), a.seqs.max_pages - 1)];
@@ -74,26 +76,16 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
   const T* vpool = reinterpret_cast<const T*>(a.v_pool) + lbase;
 
   // ---- loads of this wave's block of unit u (two pages, K or V); rows from k_end on read as zeros
-  constexpr int RPL = 64 / NCH;                      // rows per load
-  const int lr = lane / NCH;
-  const uint32_t k_off = lr * RB + 16 * ((lane % NCH) ^ SW::k(lr));
-  const uint32_t v_off = lr * RB + 16 * ((lane % NCH) ^ SW::v(lr));
-  auto issue = [&](const T* pool, uint4* dst, int u, bool is_v) {
+  const int source = KR::source(lane);               // the same for V
+  auto issue = [&](auto rows_type, const T* pool, char* dst, int u) {
+    using R = decltype(rows_type);
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const int key = k_begin + u * kUnitKeys + wave * 32 + p * kPage;
       int32_t page = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_readlane(pg, (key / kPage) & 31));
       page = (page >= 0 && page < a.n_pages) ? page : 0;
-      const int rows = __builtin_amdgcn_readfirstlane(min(max(k_end - key, 0), kPage));
-      const int64_t off = ((int64_t)page * a.Hkv + g) * kPage * D;
-      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(pool + off), 0, rows * RB, kBufferWord3);
-      lds_char* to = (lds_char*)(lds_void*)(dst + (wave * 32 + p * kPage) * NCH);
-#pragma unroll
-      for (int j = 0; j < kPage / RPL; ++j) {
-        const int r0 = j * RPL;
-        const uint32_t at = r0 * RB + (is_v ? v_off ^ (16 * SW::v(r0)) : k_off ^ (16 * SW::k(r0)));
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(to + r0 * RB), 16, at, 0, 0, kStream);
-      }
+      load_page<R, kStream>(pool + ((int64_t)page * a.Hkv + g) * kPage * D, __builtin_amdgcn_readfirstlane(min(max(k_end - key, 0), kPage)),
+                            (lds_char*)(lds_void*)(dst + (2 * wave + p) * R::kPageBytes), source);
     }
   };
   // queries (B operand of S^T = K Q^T), zeros past the pairs
@@ -104,15 +96,14 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
 #pragma unroll
     for (int s = 0; s < NS; ++s) qf[s] = ld16(qp + (2 * s + half) * 8);
   }
-  issue(kpool, s_k, 0, false);
-  issue(vpool, s_v, 0, true);
+  issue(KR{}, kpool, s_k, 0);
+  issue(VR{}, vpool, s_v, 0);
   if (threadIdx.x == 0) s_bad = 0;                   // read and written behind the first unit's barriers
 #pragma unroll
   for (int s = 0; s < NS; ++s) qf[s] = pair_ok ? qf[s] : make_uint4(0, 0, 0, 0);
 
-  const lds_char* kbase = (const lds_char*)(lds_void*)s_k + wave * 32 * RB;
-  const lds_char* vbase = (const lds_char*)(lds_void*)s_v;
-  const uint32_t k_lane = k_lane_base<RB, kFp8>(lane), v_lane = v_lane_base<RB, kFp8>(lane);
+  const lds_char* kbase = (const lds_char*)(lds_void*)s_k + 2 * wave * KR::kPageBytes + k_lane_base<RB, kFp8>(lane);
+  const lds_char* vbase = (const lds_char*)(lds_void*)s_v + wave * VR::at(0, D * (int)sizeof(T) / 16 / kWaves) + v_lane_base<RB, kFp8>(lane);
   f32x16 o[NDW];
 #pragma unroll
   for (int d = 0; d < NDW; ++d) o[d] = splat(0.0f);
@@ -125,10 +116,10 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
     asm volatile("" ::: "memory");
     f32x16 s = splat(0.0f);
 #pragma unroll
-    for (int ss = 0; ss < NS; ++ss) s = mfma32(k_fragment<kFp8>(kbase, k_lane, ss), qf[ss], s);
+    for (int ss = 0; ss < NS; ++ss) s = mfma32(k_fragment<RB, kFp8>(kbase, ss), qf[ss], s);
     __builtin_amdgcn_s_waitcnt(kLgkmWait);           // read: the buffer takes the next unit's
     asm volatile("" ::: "memory");
-    issue(kpool, s_k, u + 1, false);
+    issue(KR{}, kpool, s_k, u + 1);
     const int kb = key0 + 32 * wave;
     if (kb + 31 > first_n || kb < mask_lo) {
 #pragma unroll
@@ -163,14 +154,14 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
     __syncthreads();
     // a masked key weighs 0, and 0 times an Inf or NaN would reach rows that do not see it (see the tile kernel)
     if (min(key0 + kUnitKeys, n_hi) - 1 > first_n || key0 < mask_lo) {
-      if (finite_rows<T, NCH>(s_v + wave * 32 * NCH, lane) | finite_rows<T, NCH>(s_v + (wave * 32 + kPage) * NCH, lane)) s_bad = 1;
+      if (finite_page<T, VR>(s_v + 2 * wave * VR::kPageBytes, lane) | finite_page<T, VR>(s_v + (2 * wave + 1) * VR::kPageBytes, lane)) s_bad = 1;
       __syncthreads();
     }
     // ---- this wave's dimensions over the unit's blocks
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       lsum = lsum * alpha[w] + s_sum[w][lrow];
-      if (__builtin_amdgcn_ballot_w64(raised[w]) != 0) {
+      if ((u > 0 || w > 0) && __builtin_amdgcn_ballot_w64(raised[w]) != 0) {      // O is 0 before the first block
 #pragma unroll
         for (int d = 0; d < NDW; ++d) o[d] *= alpha[w];
       }
@@ -179,10 +170,10 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int d = 0; d < NDW; ++d)
-          o[d] = mfma32(v_fragment<RB, kFp8>(vbase + (32 * w + 16 * ks) * RB, v_lane, wave * NDW + d), ks ? p1 : p0, o[d]);
+          o[d] = mfma32(v_fragment<RB, kFp8>(vbase + (2 * w + ks) * VR::kPageBytes, d), ks ? p1 : p0, o[d]);
     }
     __syncthreads();                                 // V, weights and sums are read: the next unit's may come
-    issue(vpool, s_v, u + 1, true);
+    issue(VR{}, vpool, s_v, u + 1);
   }
   __builtin_amdgcn_s_waitcnt(vm_wait(0));            // the empty loads past the last unit write LDS: none may outlive the workgroup
 
@@ -270,7 +261,7 @@ hipError_t launch_few_t(const PackedAttnArgs& a, hipStream_t stream) {
   switch (a.D) {
     case 64: packed_few_kernel<T, 64, 2><<<grid, 128, 0, stream>>>(a); break;
     case 128: packed_few_kernel<T, 128, 4><<<grid, 256, 0, stream>>>(a); break;
-    case 256: packed_few_kernel<T, 256, 4><<<grid, 256, 0, stream>>>(a); break;
+    case 256: packed_few_kernel<T, 256, 2><<<grid, 128, 0, stream>>>(a); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();

@@ -12,26 +12,45 @@ namespace kvg {
 
 namespace {
 
-constexpr float kStep = 8.0f;          // grid of the references, log2 units
+constexpr float kStep = 16.0f;         // grid of the references, log2 units
 
 // The reference that a largest score (log2 units) asks for.
 __device__ __forceinline__ float reference_of(float mx) { return ceilf(mx * (1.0f / kStep)) * kStep; }
 
-// LDS rows hold their 16-byte chunks at position chunk ^ swizzle(row), XOR-linear in the row bits.  K is read as one chunk
-// of 32 consecutive rows per lane half, V transposed (bf16: four rows x two or four chunks, fp8: rows
-// {0..3, 8..11} (+ 4) of a 16-row step).
-template <int RB, bool kFp8>
-struct SwzTile {
-  __device__ static __forceinline__ int k(int r) {
-    if constexpr (kFp8) return RB == 256 ? (r & 15) : RB == 128 ? ((r >> 1) & 7) : ((r >> 2) & 3);
-    return RB >= 256 ? (r & 15) : (r & 7);
+// LDS layout of cache rows of RB bytes.  One direct load brings 1 KiB, kRows = 1024 / RB rows, whose 16-byte units its lanes
+// may place in any order: units of the same chunk (16 bytes of a row) of consecutive rows lie side by side, so that
+// what a fragment read's lanes take is consecutive, and every read of a kernel is one lane base plus a
+// constant.  Loads lie 1024 + PAD bytes apart, which spreads the rows of different loads over the banks.
+template <int RB, int PAD>
+struct Rows {
+  static constexpr int kRows = 1024 / RB;
+  static constexpr int kLoad = 1024 + PAD;
+  static constexpr int kPageLoads = kPage / kRows;
+  static constexpr int kPageBytes = kPageLoads * kLoad;
+  // byte offset of a row's chunk; with eight rows a load, four rows x two chunks together
+  __host__ __device__ static constexpr int at(int row, int chunk) {
+    return row / kRows * kLoad + (kRows == 8 ? (chunk / 2 * 2 + row / 4 % 2) * 128 + chunk % 2 * 64 + row % 4 * 16
+                                             : (chunk * kRows + row % kRows) * 16);
   }
-  __device__ static __forceinline__ int v(int r) {
-    if constexpr (kFp8)
-      return RB == 256 ? (r & 15) : RB == 128 ? (((r >> 1) & 1) | (((r >> 3) & 1) << 1)) : ((r >> 3) & 1);
-    return RB >= 256 ? ((0xCA60 >> (4 * (r & 3))) & 15) : 2 * (r & 3);
+  // what lane `lane` of a load brings: byte offset in the load's rows
+  __device__ static __forceinline__ int source(int lane) {
+    if constexpr (kRows == 8)
+      return (lane / 8 % 2 * 4 + lane % 4) * RB + (lane / 16 * 2 + lane / 4 % 2) * 16;
+    else
+      return lane % kRows * RB + lane / kRows * 16;
   }
 };
+template <int RB> using KRows = Rows<RB, RB == 512 ? 32 : 64>;
+template <int RB> using VRows = Rows<RB, RB == 512 ? 128 : 64>;
+
+// A page (16 rows of the pool at `slab`, the first `rows` of them; zeros past them) into LDS.
+template <typename R, int POLICY>
+__device__ __forceinline__ void load_page(const void* slab, int rows, lds_char* to, int source, int j0 = 0, int j1 = R::kPageLoads) {
+  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(slab), 0, rows * (1024 / R::kRows), kBufferWord3);
+#pragma unroll
+  for (int j = j0; j < j1; ++j)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(to + j * R::kLoad), 16, source, 1024 * j, 0, POLICY);
+}
 
 __device__ __forceinline__ float load_value(const uint16_t* p) { return bf16_bits_to_f32(*p); }
 __device__ __forceinline__ float load_value(const uint8_t* p) { return Elem<uint8_t>::get(make_uint4(*p, 0, 0, 0), 0); }
@@ -55,15 +74,15 @@ __device__ __forceinline__ bool bad_values(const uint4& x, uint8_t) {
 }
 
 // The page of value rows at p with every Inf and NaN set to 0; whether there was one.
-template <typename T, int NCH>
-__device__ __forceinline__ bool finite_rows(uint4* p, int lane) {
+template <typename T, typename R>
+__device__ __forceinline__ bool finite_page(char* p, int lane) {
   bool any = false;
-#pragma unroll 2
-  for (int i = lane; i < kPage * NCH; i += 64) {
-    uint4 x = p[i];
-    if (!bad_values(x, T{})) continue;
+#pragma unroll 1
+  for (int j = 0; j < R::kPageLoads; ++j) {
+    T* v = reinterpret_cast<T*>(p + j * R::kLoad + lane * 16);
+    if (!bad_values(*reinterpret_cast<const uint4*>(v), T{})) continue;
     any = true;
-    T* v = reinterpret_cast<T*>(p + i);
+#pragma unroll 1
     for (int e = 0; e < (int)(16 / sizeof(T)); ++e)
       if (!(fabsf(load_value(v + e)) < INFINITY)) v[e] = 0;
   }
@@ -76,26 +95,25 @@ __device__ __forceinline__ f32x16 mfma32(const uint4& x, const uint4& y, const f
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), as_bf16x8(y), c, 0, 0, 0);
 }
 
-// K fragment ss of 32 rows whose lane base is `lane`: eight values of head_dim for each lane's row (fp8 widened).
-template <bool kFp8>
-__device__ __forceinline__ uint4 k_fragment(const lds_char* rows, uint32_t lane, int ss) {
+// K fragment of step ss (32 rows x 16 dims; eight values of head_dim for each lane's row, fp8 widened) at the lane's base.
+template <int RB, bool kFp8>
+__device__ __forceinline__ uint4 k_fragment(const lds_char* lane_base, int ss) {
   if constexpr (kFp8) {
-    const u32x2 w = *reinterpret_cast<const lds_u32x2*>(rows + (lane ^ (uint32_t)(16 * ss)));
+    const u32x2 w = *reinterpret_cast<const lds_u32x2*>(lane_base + KRows<RB>::at(0, ss));
     return widen_fp8x8(w.x, w.y);
   } else {
-    return __builtin_bit_cast(uint4, *reinterpret_cast<const lds_u32x4*>(rows + (lane ^ (uint32_t)(32 * ss))));
+    return __builtin_bit_cast(uint4, *reinterpret_cast<const lds_u32x4*>(lane_base + KRows<RB>::at(0, 2 * ss)));
   }
 }
 // V^T fragment of 16 rows, dims 32 d .. 32 d + 31.
 template <int RB, bool kFp8>
-__device__ __forceinline__ uint4 v_fragment(const lds_char* rows, uint32_t lane, int d) {
+__device__ __forceinline__ uint4 v_fragment(const lds_char* lane_base, int d) {
   if constexpr (kFp8) {
-    const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(rows + (lane ^ (uint32_t)(32 * d))));
+    const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(lane_base + VRows<RB>::at(0, 2 * d)));
     return widen_fp8x8((uint32_t)w.x, (uint32_t)w.y);
   } else {
-    const uint32_t at = lane ^ (uint32_t)(64 * d);
-    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(rows + at));
-    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(rows + at + 8 * RB));
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lane_base + VRows<RB>::at(0, 4 * d)));
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lane_base + VRows<RB>::at(8, 4 * d)));
     const uint2 lo2 = __builtin_bit_cast(uint2, lo), hi2 = __builtin_bit_cast(uint2, hi);
     return make_uint4(lo2.x, lo2.y, hi2.x, hi2.y);
   }
@@ -106,22 +124,14 @@ __device__ __forceinline__ uint4 v_fragment(const lds_char* rows, uint32_t lane,
 //      32 d + 16 (tr_m % 2) + 4 (tr_k % 4); fp8 row 4 (tr_m / 2) + {0..3, 8..11}[tr_k / 2], 8 bytes at dim
 //      32 d + 16 (tr_m % 2) + 8 (tr_k % 2)
 template <int RB, bool kFp8>
-__device__ __forceinline__ uint32_t k_lane_base(int lane) {
-  using SW = SwzTile<RB, kFp8>;
-  const int r = lane & 31, half = lane >> 5;
-  return kFp8 ? r * RB + 16 * SW::k(r) + 8 * half : r * RB + 16 * (half ^ SW::k(r));
+__device__ __forceinline__ int k_lane_base(int lane) {
+  return kFp8 ? KRows<RB>::at(lane & 31, 0) + 8 * (lane >> 5) : KRows<RB>::at(lane & 31, lane >> 5);
 }
 template <int RB, bool kFp8>
-__device__ __forceinline__ uint32_t v_lane_base(int lane) {
-  using SW = SwzTile<RB, kFp8>;
+__device__ __forceinline__ int v_lane_base(int lane) {
   const int tr_k = lane & 15, tr_m = lane >> 4;
-  if constexpr (kFp8) {
-    const int kk = 4 * (tr_m >> 1) + ((tr_k >> 1) & 3) + 8 * (tr_k >> 3);
-    return kk * RB + 16 * ((tr_m & 1) ^ SW::v(kk)) + 8 * (tr_k & 1);
-  } else {
-    const int rr = (tr_m >> 1) * 4 + (tr_k >> 2);
-    return rr * RB + 8 * (tr_k & 1) + 16 * ((2 * (tr_m & 1) + ((tr_k & 3) >> 1)) ^ SW::v(rr));
-  }
+  return kFp8 ? VRows<RB>::at(4 * (tr_m >> 1) + ((tr_k >> 1) & 3) + 8 * (tr_k >> 3), tr_m & 1) + 8 * (tr_k & 1)
+              : VRows<RB>::at((tr_m >> 1) * 4 + (tr_k >> 2), 2 * (tr_m & 1) + ((tr_k & 3) >> 1)) + 8 * (tr_k & 1);
 }
 
 // Softmax state of a segment's blocks of 32 keys; the operations of one block, in the order every kernel takes them.

@@ -37,17 +37,18 @@ template <typename T, int D, int kBlocks, bool kSplitKeys>
 __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_kernel(const PackedAttnArgs a) {
   constexpr bool kFp8 = sizeof(T) == 1;
   constexpr int RB = D * (int)sizeof(T);   // bytes per cache row
-  constexpr int NCH = RB / 16;             // 16-byte chunks per row
   constexpr int NS = D / 16;               // MFMA steps over head_dim
   constexpr int ND = D / 32;               // 32-wide blocks of head_dim
-  constexpr int kTileChunks = kTileKeys * NCH;
-  constexpr int kLoads = NCH / kWaves;     // direct loads per lane and operand: a wave brings one page of the tile
   constexpr int BM = 32 * kBlocks * kWaves;
-  using SW = SwzTile<RB, kFp8>;
-  __shared__ __attribute__((aligned(1024))) uint4 sA_V0[kTileChunks];
-  __shared__ __attribute__((aligned(1024))) uint4 sA_V1[kTileChunks];
-  __shared__ __attribute__((aligned(1024))) uint4 sB_K0[kTileChunks];
-  __shared__ __attribute__((aligned(1024))) uint4 sB_K1[kTileChunks];
+  constexpr int kRing = kSplitKeys || D == 64 ? NS : 6;
+  constexpr bool kSpread = D == 256;       // a tile's loads among the matrix steps, or all at its start
+  using KR = KRows<RB>;
+  using VR = VRows<RB>;
+  // a wave brings one page of a tile; the V stages first, where an LDS instruction's immediate offset reaches
+  __shared__ __attribute__((aligned(1024))) char sA_V0[kWaves * VR::kPageBytes];
+  __shared__ __attribute__((aligned(1024))) char sA_V1[kWaves * VR::kPageBytes];
+  __shared__ __attribute__((aligned(1024))) char sB_K0[kWaves * KR::kPageBytes];
+  __shared__ __attribute__((aligned(1024))) char sB_K1[kWaves * KR::kPageBytes];
   __shared__ int s_bad;
 
   const int tid = threadIdx.x;
@@ -56,18 +57,20 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
   const int lrow = lane & 31, half = lane >> 5;
   const int lg = 31 - __builtin_clz(a.group);            // 1, 2, 4 or 8 query heads per KV head
 
-  // ---- (layer, segment, tile, KV head), the KV head fastest; late tiles, which have the most keys, first
+  // ---- (tile, layer, segment, KV head), the KV head fastest (an XCD's workgroups share few heads); late tiles, which have
+  // the most keys, first.  Workgroups without work come in runs: an XCD's go to its four shader engines in turn, and with
+  // the tile before the segment one in four had work, all on the same engine: 35 rows over 32k keys (fp8), 69 -> 205 us.
   uint32_t id = blockIdx.x;
   const int g = (int)(id % (uint32_t)a.Hkv);
   id /= (uint32_t)a.Hkv;
-  const int slot = (int)(id % (uint32_t)a.n_tiles);
-  id /= (uint32_t)a.n_tiles;
   int seg = 0;
   if constexpr (kSplitKeys) {
     seg = (int)(id % (uint32_t)a.n_seg);
     id /= (uint32_t)a.n_seg;
   }
-  const int l = (int)id;
+  const int l = (int)(id % (uint32_t)a.n_layers);
+  const int slot = (int)(id / (uint32_t)a.n_layers);
+  if constexpr (kSplitKeys) seg = (int)((uint32_t)(seg + slot) % (uint32_t)a.n_seg);      // a segment not always on the same XCD
   const SeqUnit u = find_unit(a.seqs, slot, [&](const SeqRange& s) {
     return is_few(a, s) ? 0 : (int)((((int64_t)s.len << lg) + BM - 1) / BM);
   });
@@ -108,38 +111,26 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
   const T* kpool = reinterpret_cast<const T*>(a.k_pool) + lbase;
   const T* vpool = reinterpret_cast<const T*>(a.v_pool) + lbase;
 
-  // ---- loads: wave w brings page w of tile kt (rows 16 w ..).  Instruction i covers slots [64 i, 64 i + 64) of the page's
-  // rows: row (64 i + lane) / NCH, position (64 i + lane) % NCH.  The resource over a (page, head) slab ends
-  // at the last row the workgroup needs: rows past it read as zeros.
-  constexpr int kRowsPerLoad = 64 / NCH;
-  const int lrow0 = lane / NCH;
-  const uint32_t k_off0 = lrow0 * RB + 16 * ((lane % NCH) ^ SW::k(lrow0));
-  const uint32_t v_off0 = lrow0 * RB + 16 * ((lane % NCH) ^ SW::v(lrow0));
+  // ---- loads: wave w brings page w of tile kt; rows past the last one the workgroup needs read as zeros
+  const int source = KR::source(lane);     // the same for V
   auto page_slot = [&](int kt) { return kt * (kTileKeys / kPage) + wave; };
   auto page_of_tile = [&](int kt) -> int32_t { return bt[min(page_slot(kt), last_page)]; };
-  auto tile_rsrc = [&](const T* pool, int kt, int32_t page) {
+  struct PageSource {
+    int64_t off;
+    int rows;
+  };
+  auto tile_source = [&](int kt, int32_t page) -> PageSource {
     page = __builtin_amdgcn_readfirstlane(page);
     page = (page >= 0 && page < a.n_pages) ? page : 0;
-    const int64_t poff = ((int64_t)page * a.Hkv + g) * kPage * D;
-    const int rows = __builtin_amdgcn_readfirstlane(min(max(n_hi - page_slot(kt) * kPage, 0), kPage));
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(pool + poff), 0, rows * RB, kBufferWord3);
+    return {((int64_t)page * a.Hkv + g) * kPage * D, __builtin_amdgcn_readfirstlane(min(max(n_hi - page_slot(kt) * kPage, 0), kPage))};
   };
-  constexpr int kTileLoads = 2 * kLoads;
-  auto issue = [&](__amdgpu_buffer_rsrc_t rk, __amdgpu_buffer_rsrc_t rv, auto dst_stage, int j0, int j1) {
+  constexpr int kTileLoads = 2 * KR::kPageLoads;       // of a wave: K and V alternate
+  auto issue = [&](const PageSource& src, auto dst_stage, int j0, int j1) {
     constexpr int DS = decltype(dst_stage)::value;
-    lds_char* dk = (lds_char*)(lds_void*)&(DS ? sB_K1 : sB_K0)[wave * kPage * NCH];
-    lds_char* dv = (lds_char*)(lds_void*)&(DS ? sA_V1 : sA_V0)[wave * kPage * NCH];
-#pragma unroll
-    for (int j = j0; j < j1; ++j) {
-      const int i = j >> 1;
-      if (j & 1) {
-        const uint32_t ov = 1024 * i + (v_off0 ^ (16 * SW::v(i * kRowsPerLoad)));
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(dv + 1024 * i), 16, ov, 0, 0, 0);
-      } else {
-        const uint32_t ok = 1024 * i + (k_off0 ^ (16 * SW::k(i * kRowsPerLoad)));
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)(dk + 1024 * i), 16, ok, 0, 0, 0);
-      }
-    }
+    lds_char* dk = (lds_char*)(lds_void*)((DS ? sB_K1 : sB_K0) + wave * KR::kPageBytes);
+    lds_char* dv = (lds_char*)(lds_void*)((DS ? sA_V1 : sA_V0) + wave * VR::kPageBytes);
+    load_page<KR, 0>(kpool + src.off, src.rows, dk, source, (j0 + 1) / 2, (j1 + 1) / 2);
+    load_page<VR, 0>(vpool + src.off, src.rows, dv, source, j0 / 2, j1 / 2);
   };
 
   // ---- queries (B operand of S^T), zeros past the rows
@@ -166,15 +157,16 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
     }
   }
 
-  const uint32_t k_lane = k_lane_base<RB, kFp8>(lane), v_lane = v_lane_base<RB, kFp8>(lane);
+  const int k_lane = k_lane_base<RB, kFp8>(lane), v_lane = v_lane_base<RB, kFp8>(lane);
 
   if (tid == 0) s_bad = 0;              // read and written behind the first tile's barrier
   using Stage0 = std::integral_constant<int, 0>;
   using Stage1 = std::integral_constant<int, 1>;
   int32_t pg_next = page_of_tile(kt_begin);
-  issue(tile_rsrc(kpool, kt_begin, pg_next), tile_rsrc(vpool, kt_begin, pg_next), Stage0{}, 0, kTileLoads);
+  issue(tile_source(kt_begin, pg_next), Stage0{}, 0, kTileLoads);
   pg_next = page_of_tile(kt_begin + 1);
 
+  bool fresh = true;                      // no block of the segment yet
   auto tile = [&](auto stage, int kt) __attribute__((always_inline)) {
     constexpr int ST = decltype(stage)::value;
     using Next = std::integral_constant<int, 1 - ST>;
@@ -185,23 +177,23 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
     // keys that some row of the workgroup does not see (the diagonal's, a window's lower edge; keys past n_hi
     // are zeros) such values are set to 0, and the rows that see them are given them at the end.
     if (min(key0 + kTileKeys, n_hi) - 1 > tile_first || key0 < tile_mask_lo) {
-      if (finite_rows<T, NCH>((ST ? sA_V1 : sA_V0) + wave * kPage * NCH, lane)) s_bad = 1;
+      if (finite_page<T, VR>((ST ? sA_V1 : sA_V0) + wave * VR::kPageBytes, lane)) s_bad = 1;
       __syncthreads();
     }
-    const __amdgpu_buffer_rsrc_t nk = tile_rsrc(kpool, kt + 1, pg_next), nv = tile_rsrc(vpool, kt + 1, pg_next);
+    const PageSource next = tile_source(kt + 1, pg_next);
     pg_next = page_of_tile(kt + 2);
-    if (key0 > wave_last || key0 + kTileKeys <= wave_lo) {       // no row of this wave sees the tile
-      issue(nk, nv, Next{}, 0, kTileLoads);
-      return;
-    }
+    const bool unseen = key0 > wave_last || key0 + kTileKeys <= wave_lo;       // by this wave's rows
+    if (!kSpread || unseen) issue(next, Next{}, 0, kTileLoads);
+    if (unseen) return;
     // loads of step t (0 <= t < 2 NS over phases A and B)
     auto issue_step = [&](int t) {
-      issue(nk, nv, Next{}, t * kTileLoads / (2 * NS), (t + 1) * kTileLoads / (2 * NS));
+      if constexpr (!kSpread) return;
+      issue(next, Next{}, t * kTileLoads / (2 * NS), (t + 1) * kTileLoads / (2 * NS));
     };
-    const lds_char* kbase = (const lds_char*)(lds_void*)(ST ? sB_K1 : sB_K0);
-    const lds_char* vbase = (const lds_char*)(lds_void*)(ST ? sA_V1 : sA_V0);
-    auto kread = [&](int f) { return k_fragment<kFp8>(kbase + f / NS * 32 * RB, k_lane, f % NS); };        // f = block * NS + step
-    auto vread = [&](int t) { return v_fragment<RB, kFp8>(vbase + t / ND * 16 * RB, v_lane, t % ND); };     // t = 16-key step * ND + d
+    const lds_char* kbase = (const lds_char*)(lds_void*)(ST ? sB_K1 : sB_K0) + k_lane;
+    const lds_char* vbase = (const lds_char*)(lds_void*)(ST ? sA_V1 : sA_V0) + v_lane;
+    auto kread = [&](int f) { return k_fragment<RB, kFp8>(kbase + KR::at(32 * (f / NS), 0), f % NS); };        // f = block * NS + step
+    auto vread = [&](int t) { return v_fragment<RB, kFp8>(vbase + VR::at(16 * (t / ND), 0), t % ND); };        // t = 16-key step * ND + d
 
     f32x16 s[2][kBlocks];
     if constexpr (D > 128) {
@@ -215,9 +207,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
         for (int rb = 0; rb < kBlocks; ++rb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int key = key0 + kb * 32 + half * 4 + (r >> 2) * 8 + (r & 3);
+            // key - row_lo as unsigned: keys below the window wrap round
+            const uint32_t key = key0 + kb * 32 + half * 4 - row_lo[rb] + (r >> 2) * 8 + (r & 3);
             const int at = D <= 128 ? 0 : kb;
-            s[at][rb][r] = (key <= row_n[rb] && key >= row_lo[rb]) ? s[at][rb][r] : -INFINITY;
+            s[at][rb][r] = key <= (uint32_t)(row_n[rb] - row_lo[rb]) ? s[at][rb][r] : -INFINITY;
           }
       }
     };
@@ -250,47 +243,54 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
         lsum[rb] = lsum[rb] * x.alpha + (ph.x + ph.y);
       }
     };
+    // O of a segment's first block is still 0
     auto rescale_o = [&]() {
 #pragma unroll
       for (int rb = 0; rb < kBlocks; ++rb)
-        if (__builtin_amdgcn_ballot_w64(st[rb].raised) != 0) {
+        if (!fresh && __builtin_amdgcn_ballot_w64(st[rb].raised) != 0) {
 #pragma unroll
           for (int d = 0; d < ND; ++d) o[rb][d] *= st[rb].alpha;
         }
+      fresh = false;
     };
     // K fragments of both blocks form one stream read LK ahead of their MFMAs, V^T fragments one read LV ahead, whose first
     // LV are issued with block 1's scores
     if constexpr (D <= 128) {
-      // two waves a SIMD: one's softmax runs beside the other's matrix steps
-      constexpr int LF = 2, RF = LF + 1;
+      // Two waves a SIMD: one's softmax runs beside the other's matrix steps.  The tile's K and V^T fragments, in the order of
+      // their use, pass through one ring: a fragment's place is refilled with the one LR steps on.
+      static_assert(NS == 2 * ND, "as many K as V^T fragments a block");
+      constexpr int LR = kRing;
+      uint4 ring[LR];
+      auto fetch = [&](int t) {
+        if (t < 4 * NS) ring[t % LR] = (t / NS) % 2 == 0 ? kread(t / (2 * NS) * NS + t % NS) : vread(t / (2 * NS) * NS + t % NS);
+      };
+#pragma unroll
+      for (int t = 0; t < LR; ++t) fetch(t);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        uint4 kf[RF], vf[RF];
-#pragma unroll
-        for (int f = 0; f < LF; ++f) kf[f] = kread(kb * NS + f);
 #pragma unroll
         for (int ss = 0; ss < NS; ++ss) {
-          if (ss + LF < NS) kf[(ss + LF) % RF] = kread(kb * NS + ss + LF);
-          issue_step(kb * NS + ss);
+          const int t = 2 * kb * NS + ss;
 #pragma unroll
-          for (int rb = 0; rb < kBlocks; ++rb) s[0][rb] = ss ? mfma32(kf[ss % RF], qf[rb][ss], s[0][rb]) : mfma32(kf[0], qf[rb][0], splat(0.0f));
+          for (int rb = 0; rb < kBlocks; ++rb) s[0][rb] = mfma32(ring[t % LR], qf[rb][ss], ss ? s[0][rb] : splat(0.0f));
+          fetch(t + LR);
+          issue_step(kb * NS + ss);
+          __builtin_amdgcn_sched_barrier(0);
         }
         mask_block(kb);
-        auto vget = [&](int t) { return vread(kb * 2 * ND + t); };
-#pragma unroll
-        for (int f = 0; f < LF; ++f) vf[f] = vget(f);
 #pragma unroll
         for (int rb = 0; rb < kBlocks; ++rb)
 #pragma unroll
           for (int j = 0; j < 16; ++j) soft_piece(0, rb, j);
         rescale_o();
 #pragma unroll
-        for (int t = 0; t < 2 * ND; ++t) {
-          if (t + LF < 2 * ND) vf[(t + LF) % RF] = vget(t + LF);
+        for (int i = 0; i < NS; ++i) {
+          const int t = (2 * kb + 1) * NS + i;
 #pragma unroll
-          for (int rb = 0; rb < kBlocks; ++rb) o[rb][t % ND] = mfma32(vf[t % RF], pf[0][rb][t / ND], o[rb][t % ND]);
+          for (int rb = 0; rb < kBlocks; ++rb) o[rb][i % ND] = mfma32(ring[t % LR], pf[0][rb][i / ND], o[rb][i % ND]);
+          fetch(t + LR);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
       }
       return;
     }
@@ -374,6 +374,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
 #pragma unroll
         for (int d = 0; d < ND; ++d) o[rb][d] = splat(0.0f);
       }
+      fresh = true;
     }
   };
   auto step = [&](auto stage, int kt) __attribute__((always_inline)) {
