@@ -101,7 +101,7 @@ kvg::PackedSeqs packed_seqs(const kvg_seqs* s, const kvg_packed* p) {
   return {p->cu_tokens, s->ctx_lens, s->block_tables, s->batch, p->n_tokens, p->max_len, s->max_ctx_len, s->max_pages};
 }
 
-// How a bf16 or fp8 attention call runs: rows of the few kernel and tiles at most, each launch's segments (1: not
+// How an attention call runs: rows of the few kernel and tiles at most, each launch's segments (1: not
 // split), and where their partials lie in the workspace.
 struct AttnPlan {
   int64_t few_rows, n_tiles;
@@ -112,17 +112,18 @@ struct AttnPlan {
 
 AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, int32_t n_layers) {
   AttnPlan r = {0, 0, 1, 1, 0, 0, 0, 0};
-  if (c->dtype == KVG_F32 || p->n_tokens == 0 || p->max_len == 0) return r;
-  const int64_t group = c->n_q_heads / c->n_kv_heads, bm = kvg::packed_tile_pairs(c->head_dim);
+  if (p->n_tokens == 0 || p->max_len == 0) return r;
+  const bool f32 = c->dtype == KVG_F32;
+  const int64_t group = c->n_q_heads / c->n_kv_heads, bm = f32 ? kvg::kF32Pairs : kvg::packed_tile_pairs(c->head_dim);
   const int64_t len = std::min(p->max_len, p->n_tokens);
   const int64_t keys = std::min((int64_t)s->max_ctx_len + p->max_len, (int64_t)s->max_pages * c->page_size);
   const int32_t segs = (int32_t)((keys + kvg::kPackedSeg - 1) / kvg::kPackedSeg);
   // The lengths are the device's.  A single sequence that may be long goes in tiles whatever its length.
-  if (len * group <= kvg::kFewPairs || s->batch > 1) {
+  if (!f32 && (len * group <= kvg::kFewPairs || s->batch > 1)) {
     r.few_rows = std::min<int64_t>(p->n_tokens, s->batch * std::min<int64_t>(len, kvg::kFewPairs / group));
     r.few_seg = segs;
   }
-  if (len * group > kvg::kFewPairs) {
+  if (f32 || len * group > kvg::kFewPairs) {
     const int64_t per_seq = (len * group + bm - 1) / bm;               // each sequence's tiles round up
     r.n_tiles = std::min(s->batch * per_seq, (p->n_tokens * group + (int64_t)std::min(s->batch, p->n_tokens) * (bm - 1)) / bm);
     if (r.n_tiles * c->n_kv_heads * n_layers < 512) r.tile_seg = segs;
@@ -139,7 +140,7 @@ AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, i
 
 // The few kernel's launch, the tiles' launch, and the folds of those that are split.  Every launch is checked before the
 // first one is enqueued.
-int attn_mfma(kvg::PackedAttnArgs a, const AttnPlan& plan, int32_t dtype, char* ws, hipStream_t stream) {
+int attn_launch(kvg::PackedAttnArgs a, const AttnPlan& plan, int32_t dtype, char* ws, hipStream_t stream) {
   if (plan.n_tiles > INT32_MAX) return KVG_E_SHAPE;
   a.few_rows = (int32_t)plan.few_rows;
   a.n_tiles = (int32_t)plan.n_tiles;
@@ -156,12 +157,12 @@ int attn_mfma(kvg::PackedAttnArgs a, const AttnPlan& plan, int32_t dtype, char* 
     return KVG_E_SHAPE;
   int st = KVG_OK;
   if (a.n_tiles > 0) {
-    st = hip_status(kvg::launch_packed_tiles(tiles, dtype, stream));
-    if (st == KVG_OK && plan.tile_seg > 1) st = hip_status(kvg::launch_packed_fold(tiles, false, stream));
+    st = hip_status(dtype == KVG_F32 ? kvg::launch_packed_f32(tiles, stream) : kvg::launch_packed_tiles(tiles, dtype, stream));
+    if (st == KVG_OK && plan.tile_seg > 1) st = hip_status(kvg::launch_packed_fold(tiles, dtype, false, stream));
   }
   if (st == KVG_OK && a.few_rows > 0) {
     st = hip_status(kvg::launch_packed_few(few, dtype, stream));
-    if (st == KVG_OK && plan.few_seg > 1) st = hip_status(kvg::launch_packed_fold(few, true, stream));
+    if (st == KVG_OK && plan.few_seg > 1) st = hip_status(kvg::launch_packed_fold(few, dtype, true, stream));
   }
   return st;
 }
@@ -295,10 +296,7 @@ int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_pack
   a.group = cache->n_q_heads / cache->n_kv_heads;
   a.layer0 = layer0;
   a.n_layers = n_layers;
-  if (cache->dtype != KVG_F32) {
-    return attn_mfma(a, plan, cache->dtype, static_cast<char*>(ws), static_cast<hipStream_t>(stream));
-  }
-  return hip_status(kvg::launch_packed_attn(a, cache->dtype, static_cast<hipStream_t>(stream)));
+  return attn_launch(a, plan, cache->dtype, static_cast<char*>(ws), static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

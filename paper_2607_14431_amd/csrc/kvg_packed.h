@@ -124,8 +124,8 @@ struct PackedAttnArgs {
   int64_t q_stride;
   float scale_log2;
   int32_t Hq, Hkv, D, group, layer0, n_layers;
-  // bf16 and fp8 caches: sequences of at most kFewPairs (row, query head) pairs per KV head are the few kernel's where
-  // it runs (few_rows > 0: a bound of their rows), the others go in tiles (n_tiles: a bound of the batch's).
+  // Sequences go in tiles of (row, query head) pairs of a KV head (n_tiles: a bound of the batch's); in bf16 and fp8 caches
+  // those of at most kFewPairs pairs are the few kernel's where it runs (few_rows > 0: a bound of their rows).
   // A launch over n_seg > 1 segments leaves partials [n_layers][rows][Hq][n_seg] (reference and sum, then D sums);
   // rows: the launch's packed rows, the few kernel's counted over its own sequences.
   int32_t few_rows, n_tiles;
@@ -148,7 +148,9 @@ inline int64_t packed_few_workgroups(const PackedAttnArgs& a) { return (int64_t)
 hipError_t launch_packed_tiles(const PackedAttnArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_packed_few(const PackedAttnArgs& a, int dtype, hipStream_t stream);
 // out = the rows' segments folded in order, of a tile launch and of the few kernel's
-hipError_t launch_packed_fold(const PackedAttnArgs& a, bool few, hipStream_t stream);
-hipError_t launch_packed_attn(const PackedAttnArgs& a, int dtype, hipStream_t stream);
+hipError_t launch_packed_fold(const PackedAttnArgs& a, int dtype, bool few, hipStream_t stream);
+// fp32 caches: tiles of kF32Pairs pairs
+constexpr int kF32Pairs = 32;
+hipError_t launch_packed_f32(const PackedAttnArgs& a, hipStream_t stream);
 
 }  // namespace kvg

@@ -211,28 +211,19 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
   if (s_bad != 0) {                                  // the values that are not finite, to the rows that see them
     __builtin_amdgcn_s_waitcnt(vm_wait(0));
     __syncthreads();
-    for (int key = k_begin + wave; key < k_end; key += kWaves) {
-      const int32_t page = bt[key / kPage];
-      const T* vr = vpool + (((int64_t)(page >= 0 && page < a.n_pages ? page : 0) * a.Hkv + g) * kPage + key % kPage) * D;
-      for (int x = lane; x < D; x += 64) {
-        const float v = load_value(vr + x);
-        if (fabsf(v) < INFINITY) continue;
-        for (int p = 0; p < n_pairs; ++p) {
-          const int n = sq.ctx + (p >> lg);
-          if (key > n || key < window_start(W, n + 1)) continue;
-          const int64_t at = slot_of(p);
-          if (a.n_seg > 1)
-            a.part_acc[at * D + x] = v;
-          else
-            static_cast<uint16_t*>(a.out)[at * D + x] = (uint16_t)(__float_as_uint(v) >> 16);
-        }
-      }
-    }
+    put_bad_values(a, vpool, bt, g, k_begin + wave, k_end, kWaves, W, sq.ctx, lg, 0, n_pairs, [&](int p, int x, float v) {
+      const int64_t at = slot_of(p) * D + x;
+      if (a.n_seg > 1)
+        a.part_acc[at] = v;
+      else
+        static_cast<uint16_t*>(a.out)[at] = (uint16_t)(__float_as_uint(v) >> 16);
+    });
   }
 }
 
 // out = the segments of a row and query head folded in ascending order: a workgroup of D lanes (a dimension each).
-template <int D, bool kFew>
+// T: type of the result.
+template <typename T, int D, bool kFew>
 __global__ __launch_bounds__(D) void packed_fold_kernel(const PackedAttnArgs a) {
   const int64_t id = blockIdx.x;                     // (layer, row of the launch, query head)
   const int h = (int)(id % a.Hq);
@@ -252,7 +243,7 @@ __global__ __launch_bounds__(D) void packed_fold_kernel(const PackedAttnArgs a) 
     o_run = fmaf(acc[(int64_t)s * D], f.part, o_run * f.run);
   }
   const int64_t row = (int64_t)l * a.seqs.n_tokens + u.range.row0 + u.at;
-  static_cast<uint16_t*>(a.out)[(row * a.Hq + h) * D + threadIdx.x] = __builtin_bit_cast(uint16_t, (__bf16)(o_run * (1.0f / l_run)));
+  static_cast<T*>(a.out)[(row * a.Hq + h) * D + threadIdx.x] = (T)(o_run * (1.0f / l_run));
 }
 
 template <typename T>
@@ -267,13 +258,13 @@ hipError_t launch_few_t(const PackedAttnArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <bool kFew>
+template <typename T, bool kFew>
 hipError_t launch_fold_t(const PackedAttnArgs& a, hipStream_t stream) {
   const unsigned grid = (unsigned)((int64_t)a.n_layers * (kFew ? a.few_rows : a.seqs.n_tokens) * a.Hq);
   switch (a.D) {
-    case 64: packed_fold_kernel<64, kFew><<<grid, 64, 0, stream>>>(a); break;
-    case 128: packed_fold_kernel<128, kFew><<<grid, 128, 0, stream>>>(a); break;
-    case 256: packed_fold_kernel<256, kFew><<<grid, 256, 0, stream>>>(a); break;
+    case 64: packed_fold_kernel<T, 64, kFew><<<grid, 64, 0, stream>>>(a); break;
+    case 128: packed_fold_kernel<T, 128, kFew><<<grid, 128, 0, stream>>>(a); break;
+    case 256: packed_fold_kernel<T, 256, kFew><<<grid, 256, 0, stream>>>(a); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
@@ -287,8 +278,9 @@ hipError_t launch_packed_few(const PackedAttnArgs& a, int dtype, hipStream_t str
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_packed_fold(const PackedAttnArgs& a, bool few, hipStream_t stream) {
-  return few ? launch_fold_t<true>(a, stream) : launch_fold_t<false>(a, stream);
+hipError_t launch_packed_fold(const PackedAttnArgs& a, int dtype, bool few, hipStream_t stream) {
+  if (dtype == kDtypeF32) return few ? hipErrorInvalidValue : launch_fold_t<float, false>(a, stream);
+  return few ? launch_fold_t<__bf16, true>(a, stream) : launch_fold_t<__bf16, false>(a, stream);
 }
 
 }  // namespace kvg

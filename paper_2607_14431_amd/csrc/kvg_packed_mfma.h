@@ -52,6 +52,7 @@ __device__ __forceinline__ void load_page(const void* slab, int rows, lds_char* 
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(to + j * R::kLoad), 16, source, 1024 * j, 0, POLICY);
 }
 
+__device__ __forceinline__ float load_value(const float* p) { return *p; }
 __device__ __forceinline__ float load_value(const uint16_t* p) { return bf16_bits_to_f32(*p); }
 __device__ __forceinline__ float load_value(const uint8_t* p) { return Elem<uint8_t>::get(make_uint4(*p, 0, 0, 0), 0); }
 
@@ -155,6 +156,25 @@ __device__ __forceinline__ uint4 round_weights(const f32x16& p, int h, float& ps
   }
   return f;
 }
+// The values of keys key0, key0 + step, .. (below key1) that are not finite, to those of the pairs [pair0, pair0 + pairs) of a
+// sequence that see them: put(pair - pair0, dimension, value), a dimension per lane.  For the keys a kernel has left out.
+template <typename T, typename Put>
+__device__ __forceinline__ void put_bad_values(const PackedAttnArgs& a, const T* vpool, const int32_t* table, int g, int key0, int key1, int step,
+                                            int W, int ctx, int lg, int pair0, int pairs, Put put) {
+  for (int key = key0; key < key1; key += step) {
+    const int32_t page = table[key / kPage];
+    const T* vr = vpool + (((int64_t)(page >= 0 && page < a.n_pages ? page : 0) * a.Hkv + g) * kPage + key % kPage) * a.D;
+    for (int x = __lane_id(); x < a.D; x += 64) {
+      const float v = load_value(vr + x);
+      if (fabsf(v) < INFINITY) continue;
+      for (int p = 0; p < pairs; ++p) {
+        const int n = ctx + ((pair0 + p) >> lg);
+        if (key <= n && key >= window_start(W, n + 1)) put(p, x, v);
+      }
+    }
+  }
+}
+
 // Rows of the few kernel's sequences before sequence b (a wave's lanes together).
 __device__ __forceinline__ int few_rows_before(const PackedAttnArgs& a, int b) {
   int rows = 0;

@@ -419,7 +419,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
                          pack_bf16_rne(o_run[rb][d][r4 * 4 + 2] * inv, o_run[rb][d][r4 * 4 + 3] * inv));
     }
   }
-  // ---- the values that are not finite, to the rows that see them (a dimension per lane)
+  // ---- the values that are not finite, to the rows that see them
   __syncthreads();
   if (s_bad != 0 && !idle) {
     __builtin_amdgcn_s_waitcnt(0x0F70);
@@ -427,23 +427,14 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
     for (int kt = kt_begin; kt < n_tiles; ++kt) {
       const int key0 = kt * kTileKeys;
       if (!(min(key0 + kTileKeys, n_hi) - 1 > tile_first || key0 < tile_mask_lo)) continue;
-      for (int key = max(key0, wave_lo); key < min(key0 + kTileKeys, wave_last + 1); ++key) {
-        const int32_t page = bt[key / kPage];
-        const T* vr = vpool + (((int64_t)(page >= 0 && page < a.n_pages ? page : 0) * a.Hkv + g) * kPage + key % kPage) * D;
-        for (int x = lane; x < D; x += 64) {
-          const float v = load_value(vr + x);
-          if (fabsf(v) < INFINITY) continue;
-          for (int i = 0; i < pairs; ++i) {
-            const int n = ctx + ((pair0 + i) >> lg);
-            if (key > n || key < window_start(W, n + 1)) continue;
-            const int64_t at = slot_of(pair0 + i);
-            if constexpr (kSplitKeys)
-              a.part_acc[at * D + x] = v;
-            else
-              static_cast<uint16_t*>(a.out)[at * D + x] = (uint16_t)(__float_as_uint(v) >> 16);
-          }
-        }
-      }
+      put_bad_values(a, vpool, bt, g, max(key0, wave_lo), min(key0 + kTileKeys, wave_last + 1), 1, W, ctx, lg, pair0, pairs,
+                     [&](int p, int x, float v) {
+                       const int64_t at = slot_of(pair0 + p) * D + x;
+                       if constexpr (kSplitKeys)
+                         a.part_acc[at] = v;
+                       else
+                         static_cast<uint16_t*>(a.out)[at] = (uint16_t)(__float_as_uint(v) >> 16);
+                     });
     }
   }
 }
