@@ -93,6 +93,7 @@ struct RotateArgs {
   int64_t x_stride, y_stride;
   const int64_t* positions;
   int32_t n_tokens, n_heads, D;
+  int32_t steps;              // of a workgroup (set by the launcher)
   RotaryArgs rot;
 };
 
@@ -110,7 +111,8 @@ struct NormAppendArgs {
   const void* q_weight;       // or null: no norm
   const void* k_weight;
   float eps, weight_offset;
-  int32_t Hq, Hkv, D, layer0, n_layers, layers_per_block;
+  int32_t Hq, Hkv, D, layer0, n_layers;
+  int32_t layers_per_block, steps;      // of a workgroup (set by the launcher)
   RotaryArgs rot;
 };
 

@@ -394,7 +394,8 @@ def _token_stride(t: torch.Tensor, n_layers: int, n_tokens: int, heads: int, hea
     sl, st, sh, sd = t.stride()
     if n_tokens <= 1:                      # a token's rows are n_tokens strides from the next layer's
         st = sl if n_layers > 1 and n_tokens else heads * head_dim
-    if sd != 1 or (heads > 1 and sh != head_dim) or st < heads * head_dim or (n_layers > 1 and n_tokens and sl != n_tokens * st):
+    if (sd != 1 or sh != head_dim and heads > 1 or st < heads * head_dim or
+            n_layers > 1 and n_tokens and sl != n_tokens * st):
         raise ValueError("packed rows: heads dense, layers n_tokens rows apart")
     return st
 
@@ -408,14 +409,19 @@ def kvg_rotary_frequencies(rt: kvg_rotary, head_dim: int) -> list[float]:
 def kvg_rotate(rt: kvg_rotary, positions: torch.Tensor, x: torch.Tensor, y: torch.Tensor, stream=None):
     """y[t][h] = x[t][h] rotated at positions[t] (int64); x, y: [n_tokens][n_heads][head_dim], fp32 or bf16, heads
     dense, any token stride; y may be x."""
-    T, H, D = x.shape
-    if x.dtype not in (torch.float32, torch.bfloat16):
+    shape, dtype = x.shape, x.dtype
+    T, H, D = shape
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise KvgError(-3, "kvg_rotate")
+    sx, hx, dx = x.stride()
+    sy, hy, dy = y.stride()
+    if y.dtype is not dtype or y.shape != shape or dx != 1 or dy != 1 or H > 1 and (hx != D or hy != D):
+        raise ValueError("kvg_rotate: x and y alike, heads dense")
+    if T <= 1:
+        sx = sy = 0
     assert positions.dtype is torch.int64 and positions.is_contiguous() and positions.numel() == T
-    sx = _token_stride(x[None], 1, T, H, D, x.dtype)
-    sy = _token_stride(y[None], 1, T, H, D, x.dtype)
-    _check(_lib.kvg_rotate(ctypes.byref(rt), _DTYPE_CODE[x.dtype], D, T, H, _ptr(positions), _ptr(x), sx, _ptr(y), sy,
-                           _stream(stream)), "kvg_rotate")
+    _check(_lib.kvg_rotate(ctypes.byref(rt), 1 if dtype is torch.bfloat16 else 0, D, T, H, positions.data_ptr(), x.data_ptr(), sx,
+                           y.data_ptr(), sy, _stream(stream)), "kvg_rotate")
 
 
 def kvg_norm_append(cache: Cache, seqs: Seqs, packed: Packed, rt: kvg_rotary, norm: HeadNorm | None, layer0: int,
