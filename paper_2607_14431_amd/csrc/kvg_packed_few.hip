@@ -160,7 +160,7 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
     // ---- this wave's dimensions over the unit's blocks
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      lsum = lsum * alpha[w] + s_sum[w][lrow];
+      lsum = fmaf(lsum, alpha[w], s_sum[w][lrow]);
       if ((u > 0 || w > 0) && __builtin_amdgcn_ballot_w64(raised[w]) != 0) {      // O is 0 before the first block
 #pragma unroll
         for (int d = 0; d < NDW; ++d) o[d] *= alpha[w];
@@ -246,13 +246,25 @@ __global__ __launch_bounds__(D) void packed_fold_kernel(const PackedAttnArgs a) 
   static_cast<T*>(a.out)[(row * a.Hq + h) * D + threadIdx.x] = (T)(o_run * (1.0f / l_run));
 }
 
+// Waves of a workgroup: four take a segment of a launch that leaves CUs idle soonest (one token over 4.6k keys at head_dim 256,
+// 80 workgroups: 19 us; two waves 27), two leave room for more workgroups on a CU, whose starts and ends then
+// overlap (16 tokens over 33k keys: 650 us with four waves, 521 with two).
+constexpr unsigned kFewGrid = 256;
+template <typename T, int D>
+void launch_few_d(const PackedAttnArgs& a, hipStream_t stream) {
+  const unsigned grid = (unsigned)packed_few_workgroups(a);
+  if (D > 64 && grid <= kFewGrid)
+    packed_few_kernel<T, D, D == 64 ? 2 : 4><<<grid, 64 * 4, 0, stream>>>(a);
+  else
+    packed_few_kernel<T, D, 2><<<grid, 64 * 2, 0, stream>>>(a);
+}
+
 template <typename T>
 hipError_t launch_few_t(const PackedAttnArgs& a, hipStream_t stream) {
-  const unsigned grid = (unsigned)packed_few_workgroups(a);
   switch (a.D) {
-    case 64: packed_few_kernel<T, 64, 2><<<grid, 128, 0, stream>>>(a); break;
-    case 128: packed_few_kernel<T, 128, 4><<<grid, 256, 0, stream>>>(a); break;
-    case 256: packed_few_kernel<T, 256, 2><<<grid, 128, 0, stream>>>(a); break;
+    case 64: launch_few_d<T, 64>(a, stream); break;
+    case 128: launch_few_d<T, 128>(a, stream); break;
+    case 256: launch_few_d<T, 256>(a, stream); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();

@@ -240,7 +240,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
         pf[kb][rb][j - 13] = round_weights(s[kb][rb], j - 13, x.psum);
       } else {
         const float2 ph = halves32(x.psum);
-        lsum[rb] = lsum[rb] * x.alpha + (ph.x + ph.y);
+        lsum[rb] = fmaf(lsum[rb], x.alpha, ph.x + ph.y);
       }
     };
     // O of a segment's first block is still 0
