@@ -101,6 +101,14 @@ kvg::PackedSeqs packed_seqs(const kvg_seqs* s, const kvg_packed* p) {
   return {p->cu_tokens, s->ctx_lens, s->block_tables, s->batch, p->n_tokens, p->max_len, s->max_ctx_len, s->max_pages};
 }
 
+// A tile launch is split over segments when its workgroups are few beside the segments that each would walk: splitting
+// shortens the walk, but every (row, segment) leaves D sums that the fold reads.  Measured, unsplit against split
+// with its fold, us, at workgroups x segments.  bf16 and fp8: 16 x 3 52 / 31 (head_dim 256), 32 x 9 173 / 34 (256),
+// 104 x 3 48 / 72 (256), 160 x 2 31 / 53, 184 x 12 135 / 108-139 (with and without windows), 192 x 4 37 / 67, 242 x 8
+// 165 / 91 (64), 250 x 4 53 / 79, 314 x 5 69 / 90, 388 x 12 167 / 182 (128 where not said).  fp32, whose tiles have fewer
+// rows to a workgroup: 32 x 2 26 / 21, 104 x 3 35 / 32, 184 x 3 45 / 36, 216 x 2 31 / 34, 256 x 5 69 / 82, 528 x 3 191 / 195.
+constexpr int64_t kSplitPerSegment = 48, kSplitPerSegmentF32 = 96, kSplitBelow = 256;
+
 // How an attention call runs: rows of the few kernel and tiles at most, each launch's segments (1: not
 // split), and where their partials lie in the workspace.
 struct AttnPlan {
@@ -110,7 +118,8 @@ struct AttnPlan {
   size_t total() const { return std::max(few_ml + few_acc + tile_ml + tile_acc, kAlign); }
 };
 
-AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, int32_t n_layers) {
+// window: the layers' windows, or null: as if they had none, which needs the most.
+AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, int32_t n_layers, const int32_t* window) {
   AttnPlan r = {0, 0, 1, 1, 0, 0, 0, 0};
   if (p->n_tokens == 0 || p->max_len == 0) return r;
   const bool f32 = c->dtype == KVG_F32;
@@ -126,7 +135,13 @@ AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, i
   if (f32 || len * group > kvg::kFewPairs) {
     const int64_t per_seq = (len * group + bm - 1) / bm;               // each sequence's tiles round up
     r.n_tiles = std::min(s->batch * per_seq, (p->n_tokens * group + (int64_t)std::min(s->batch, p->n_tokens) * (bm - 1)) / bm);
-    if (r.n_tiles * c->n_kv_heads * n_layers < 512) r.tile_seg = segs;
+    int64_t walked = 0;                                                // segments of a tile, about
+    for (int l = 0; l < n_layers; ++l) {
+      const int64_t W = window != nullptr ? window[l] : 0;
+      walked = std::max(walked, W > 0 ? std::min<int64_t>(segs, (W + bm / group) / kvg::kPackedSeg + 1) : segs);
+    }
+    const int64_t per_segment = f32 ? kSplitPerSegmentF32 : kSplitPerSegment;
+    if (r.n_tiles * c->n_kv_heads * n_layers < std::min(kSplitBelow, per_segment * (walked - 1))) r.tile_seg = segs;
   }
   auto bytes = [&](int64_t rows, int32_t n_seg, size_t values) {
     return n_seg > 1 ? align_up((size_t)n_layers * rows * c->n_q_heads * n_seg * values * sizeof(float)) : 0;
@@ -259,7 +274,7 @@ size_t kvg_packed_attn_workspace_bytes(const kvg_cache* cache, const kvg_seqs* s
   if (check_cache(cache) != KVG_OK || check_packed(cache, seqs, packed) != KVG_OK || n_layers <= 0 ||
       n_layers > cache->n_layers)
     return 0;
-  return attn_plan(cache, seqs, packed, n_layers).total();
+  return attn_plan(cache, seqs, packed, n_layers, nullptr).total();
 }
 
 int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, int32_t layer0, int32_t n_layers,
@@ -275,7 +290,7 @@ int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_pack
                          &a.q_stride)) != KVG_OK)
     return st;
   if ((st = fill_windows(cache, layer0, n_layers, a.window)) != KVG_OK) return st;
-  const AttnPlan plan = attn_plan(cache, seqs, packed, n_layers);
+  const AttnPlan plan = attn_plan(cache, seqs, packed, n_layers, a.window);
   if (ws == nullptr || ws_bytes < plan.total()) return KVG_E_WORKSPACE;
   if (packed->n_tokens == 0 || packed->max_len == 0) return KVG_OK;
   if (q == nullptr || out == nullptr || q == out) return KVG_E_INVAL;
