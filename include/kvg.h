@@ -426,7 +426,9 @@ int kvg_norm_append(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_pack
                     const kvg_head_norm* norm, int32_t layer0, int32_t n_layers, const void* q_raw_dev,
                     const void* k_raw_dev, const void* v_raw_dev, void* q_out_dev, void* stream);
 
-/* Workspace bytes kvg_packed_attn needs for this batch (0 on bad args). */
+/* Workspace bytes kvg_packed_attn needs for this batch, whichever n_layers layers it is called for (0 on bad
+ * args).  They follow from the bounds alone (n_tokens, max_len, max_ctx_len, batch, max_pages) and do not always grow with
+ * them: a smaller batch may be split over its keys where a larger one is not. */
 size_t kvg_packed_attn_workspace_bytes(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed,
                                        int32_t n_layers);
 

@@ -101,13 +101,19 @@ kvg::PackedSeqs packed_seqs(const kvg_seqs* s, const kvg_packed* p) {
   return {p->cu_tokens, s->ctx_lens, s->block_tables, s->batch, p->n_tokens, p->max_len, s->max_ctx_len, s->max_pages};
 }
 
-// A tile launch is split over segments when its workgroups are few beside the segments that each would walk: splitting
-// shortens the walk, but every (row, segment) leaves D sums that the fold reads.  Measured, unsplit against split
-// with its fold, us, at workgroups x segments.  bf16 and fp8: 16 x 3 52 / 31 (head_dim 256), 32 x 9 173 / 34 (256),
-// 104 x 3 48 / 72 (256), 160 x 2 31 / 53, 184 x 12 135 / 108-139 (with and without windows), 192 x 4 37 / 67, 242 x 8
-// 165 / 91 (64), 250 x 4 53 / 79, 314 x 5 69 / 90, 388 x 12 167 / 182 (128 where not said).  fp32, whose tiles have fewer
-// rows to a workgroup: 32 x 2 26 / 21, 104 x 3 35 / 32, 184 x 3 45 / 36, 216 x 2 31 / 34, 256 x 5 69 / 82, 528 x 3 191 / 195.
-constexpr int64_t kSplitPerSegment = 48, kSplitPerSegmentF32 = 96, kSplitBelow = 256;
+// A tile launch is split over segments when its workgroups (in units of the longest walk, `segs` segments) are few beside
+// the chip and beside the segments: splitting shortens the walk, but every (row, segment) leaves D sums that are written
+// and read again, cheaply only while the last-level cache holds them.  Measured, unsplit against split with its
+// fold, us, at workgroups x segments.  bf16 and fp8, head_dim 256: 16 x 3 52 / 31, 40 x 9 116 / 53, 64 x 33 445 / 302,
+// 96 x 34 447 / 453, 104 x 3 46 / 53, 128 x 10 144 / 136, 128 x 34 456 / 571; 128: 64 x 33 334 / 134, 128 x 9 99 / 78,
+// 128 x 33 357 / 294, 160 x 2 33 / 41, 184 x 12 128-134 / 96-122 (with and without windows), 192 x 4 35 / 51, 192 x 9
+// 109 / 110, 192 x 34 363 / 442, 242 x 12 166 / 143, 250 x 4 51 / 60, 314 x 5 65 / 67, 388 x 12 167 / 189; 64: 46 x 13 229 / 55,
+// 126 x 40 756 / 292, 242 x 8 165 / 91.  fp32, more work on fewer rows to a workgroup: 32 x 2 26 / 21, 104 x 3 35 / 32,
+// 184 x 3 45 / 34, 216 x 2 31 / 34, 256 x 5 73 / 81, 528 x 3 191 / 195.
+bool split_tiles(bool f32, int64_t head_dim, int64_t workgroups, int64_t segs) {
+  if (f32) return workgroups < std::min<int64_t>(256, 96 * (segs - 1));
+  return workgroups < std::min<int64_t>(256, 48 * (segs - 1)) && workgroups * segs < 576000 / head_dim;
+}
 
 // How an attention call runs: rows of the few kernel and tiles at most, each launch's segments (1: not
 // split), and where their partials lie in the workspace.
@@ -115,12 +121,13 @@ struct AttnPlan {
   int64_t few_rows, n_tiles;
   int32_t few_seg, tile_seg;
   size_t few_ml, few_acc, tile_ml, tile_acc;
+  bool fits;                  // the launches, into a grid
   size_t total() const { return std::max(few_ml + few_acc + tile_ml + tile_acc, kAlign); }
 };
 
-// window: the layers' windows, or null: as if they had none, which needs the most.
+// window: the layers' windows, or null.
 AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, int32_t n_layers, const int32_t* window) {
-  AttnPlan r = {0, 0, 1, 1, 0, 0, 0, 0};
+  AttnPlan r = {0, 0, 1, 1, 0, 0, 0, 0, true};
   if (p->n_tokens == 0 || p->max_len == 0) return r;
   const bool f32 = c->dtype == KVG_F32;
   const int64_t group = c->n_q_heads / c->n_kv_heads, bm = f32 ? kvg::kF32Pairs : kvg::packed_tile_pairs(c->head_dim);
@@ -135,28 +142,33 @@ AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, i
   if (f32 || len * group > kvg::kFewPairs) {
     const int64_t per_seq = (len * group + bm - 1) / bm;               // each sequence's tiles round up
     r.n_tiles = std::min(s->batch * per_seq, (p->n_tokens * group + (int64_t)std::min(s->batch, p->n_tokens) * (bm - 1)) / bm);
-    int64_t walked = 0;                                                // segments of a tile, about
+    int64_t longest = 0, sum = 0;                                      // segments of a layer's tile, about
     for (int l = 0; l < n_layers; ++l) {
       const int64_t W = window != nullptr ? window[l] : 0;
-      walked = std::max(walked, W > 0 ? std::min<int64_t>(segs, (W + bm / group) / kvg::kPackedSeg + 1) : segs);
+      const int64_t walk = W > 0 ? std::min<int64_t>(segs, (W + bm / group) / kvg::kPackedSeg + 1) : segs;
+      longest = std::max(longest, walk);
+      sum += walk;
     }
-    const int64_t per_segment = f32 ? kSplitPerSegmentF32 : kSplitPerSegment;
-    if (r.n_tiles * c->n_kv_heads * n_layers < std::min(kSplitBelow, per_segment * (walked - 1))) r.tile_seg = segs;
+    if (split_tiles(f32, c->head_dim, r.n_tiles * c->n_kv_heads * sum / longest, longest)) r.tile_seg = segs;
   }
-  auto bytes = [&](int64_t rows, int32_t n_seg, size_t values) {
-    return n_seg > 1 ? align_up((size_t)n_layers * rows * c->n_q_heads * n_seg * values * sizeof(float)) : 0;
+  const int64_t tile_grid = n_layers * r.n_tiles * c->n_kv_heads, fold_grid = (bm / 32) * (c->head_dim / 32);
+  r.fits = fits_grid((int64_t)n_layers * r.few_seg * (r.few_rows > 0 ? s->batch : 0) * c->n_kv_heads, 256) &&
+           fits_grid(n_layers * r.few_rows * c->n_q_heads, 256) &&
+           fits_grid(tile_grid * std::max<int64_t>(r.tile_seg, r.tile_seg > 1 ? fold_grid : 1), 256);
+  if (!r.fits) return r;
+  auto bytes = [&](int64_t row_heads, int32_t n_seg, size_t values) {
+    return n_seg > 1 ? align_up((size_t)n_layers * row_heads * n_seg * values * sizeof(float)) : 0;
   };
-  r.few_ml = bytes(r.few_rows, r.few_seg, 2);
-  r.few_acc = bytes(r.few_rows, r.few_seg, c->head_dim);
-  r.tile_ml = bytes(p->n_tokens, r.tile_seg, 2);
-  r.tile_acc = bytes(p->n_tokens, r.tile_seg, c->head_dim);
+  const int64_t few = r.few_rows * c->n_q_heads, tiles = r.n_tiles * c->n_kv_heads * bm;
+  r.few_ml = bytes(few, r.few_seg, 2);
+  r.few_acc = bytes(few, r.few_seg, c->head_dim);
+  r.tile_ml = bytes(tiles, r.tile_seg, 2);
+  r.tile_acc = bytes(tiles, r.tile_seg, c->head_dim);
   return r;
 }
 
-// The few kernel's launch, the tiles' launch, and the folds of those that are split.  Every launch is checked before the
-// first one is enqueued.
+// The tiles' launch, the few kernel's, and the folds of those that are split.
 int attn_launch(kvg::PackedAttnArgs a, const AttnPlan& plan, int32_t dtype, char* ws, hipStream_t stream) {
-  if (plan.n_tiles > INT32_MAX) return KVG_E_SHAPE;
   a.few_rows = (int32_t)plan.few_rows;
   a.n_tiles = (int32_t)plan.n_tiles;
   kvg::PackedAttnArgs few = a, tiles = a;
@@ -166,18 +178,14 @@ int attn_launch(kvg::PackedAttnArgs a, const AttnPlan& plan, int32_t dtype, char
   tiles.n_seg = plan.tile_seg;
   tiles.part_ml = reinterpret_cast<float*>(ws + plan.few_ml + plan.few_acc);
   tiles.part_acc = reinterpret_cast<float*>(ws + plan.few_ml + plan.few_acc + plan.tile_ml);
-  const int64_t row_heads = (int64_t)a.n_layers * a.seqs.n_tokens * a.Hq;
-  if (!fits_grid(kvg::packed_few_workgroups(few), 256) || !fits_grid(kvg::packed_tile_workgroups(tiles), 256) ||
-      !fits_grid(row_heads, 256))
-    return KVG_E_SHAPE;
   int st = KVG_OK;
   if (a.n_tiles > 0) {
     st = hip_status(dtype == KVG_F32 ? kvg::launch_packed_f32(tiles, stream) : kvg::launch_packed_tiles(tiles, dtype, stream));
-    if (st == KVG_OK && plan.tile_seg > 1) st = hip_status(kvg::launch_packed_fold(tiles, dtype, false, stream));
+    if (st == KVG_OK && plan.tile_seg > 1) st = hip_status(kvg::launch_packed_fold(tiles, dtype, stream));
   }
   if (st == KVG_OK && a.few_rows > 0) {
     st = hip_status(kvg::launch_packed_few(few, dtype, stream));
-    if (st == KVG_OK && plan.few_seg > 1) st = hip_status(kvg::launch_packed_fold(few, dtype, true, stream));
+    if (st == KVG_OK && plan.few_seg > 1) st = hip_status(kvg::launch_packed_few_fold(few, stream));
   }
   return st;
 }
@@ -274,7 +282,15 @@ size_t kvg_packed_attn_workspace_bytes(const kvg_cache* cache, const kvg_seqs* s
   if (check_cache(cache) != KVG_OK || check_packed(cache, seqs, packed) != KVG_OK || n_layers <= 0 ||
       n_layers > cache->n_layers)
     return 0;
-  return attn_plan(cache, seqs, packed, n_layers, nullptr).total();
+  // whichever layers the call is for
+  size_t most = 0;
+  const bool windowed = cache->layer_window != nullptr;
+  for (int32_t l = 0; l <= (windowed ? cache->n_layers - n_layers : 0); ++l) {
+    const AttnPlan plan = attn_plan(cache, seqs, packed, n_layers, windowed ? cache->layer_window + l : nullptr);
+    if (!plan.fits) return 0;
+    most = std::max(most, plan.total());
+  }
+  return most;
 }
 
 int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, int32_t layer0, int32_t n_layers,
@@ -291,12 +307,12 @@ int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_pack
     return st;
   if ((st = fill_windows(cache, layer0, n_layers, a.window)) != KVG_OK) return st;
   const AttnPlan plan = attn_plan(cache, seqs, packed, n_layers, a.window);
+  if (!plan.fits || !fits_grid(packed->n_tokens, 256)) return KVG_E_SHAPE;
   if (ws == nullptr || ws_bytes < plan.total()) return KVG_E_WORKSPACE;
   if (packed->n_tokens == 0 || packed->max_len == 0) return KVG_OK;
   if (q == nullptr || out == nullptr || q == out) return KVG_E_INVAL;
   if (!aligned16(q) || !aligned16(out) || !aligned16(ws) || !aligned16(cache->k_pool) || !aligned16(cache->v_pool))
     return KVG_E_ALIGN;
-  if (!fits_grid((int64_t)packed->n_tokens * cache->n_q_heads * n_layers, 256)) return KVG_E_SHAPE;
   a.seqs = packed_seqs(seqs, packed);
   a.k_pool = cache->k_pool;
   a.v_pool = cache->v_pool;

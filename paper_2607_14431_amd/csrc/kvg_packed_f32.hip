@@ -266,24 +266,24 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_f32_kernel(const Packed
   }
 
   // ---- the partial, or the result
-  auto slot_of = [&](int p) -> int64_t {
+  const int64_t block = part_block(a, l, slot, g, 1, 0, seg);
+  auto row_of = [&](int p) -> int64_t {
     const int64_t tok = (int64_t)l * a.seqs.n_tokens + sq.row0 + ((pair0 + p) >> lg);
-    const int64_t at = tok * a.Hq + g * a.group + ((pair0 + p) & (a.group - 1));
-    return kSplitKeys ? at * a.n_seg + seg : at;
+    return tok * a.Hq + g * a.group + ((pair0 + p) & (a.group - 1));
   };
-  float* dst = kSplitKeys ? a.part_acc : static_cast<float*>(a.out);
   const int pairs = min(32, (sq.len << lg) - pair0);
   if (f_pair < pairs) {
-    const int64_t at = slot_of(f_pair);
     const float inv = kSplitKeys ? 1.0f : 1.0f / l_run;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      Floats<ND> v;
+    for (int j = 0; j < ND; ++j) {            // dims ND f_i + 4 j + 0..3
+      Floats<4> v;
 #pragma unroll
-      for (int d = 0; d < ND; ++d) v.x[d] = kSplitKeys ? run[d][e] : run[d][e] * inv;
-      *reinterpret_cast<Floats<ND>*>(dst + at * D + ND * (f_i + e)) = v;
+      for (int i = 0; i < 4; ++i) v.x[i] = kSplitKeys ? run[(4 * j + i) % ND][(4 * j + i) / ND] : run[(4 * j + i) % ND][(4 * j + i) / ND] * inv;
+      const int x = ND * f_i + 4 * j;
+      float* dst = kSplitKeys ? a.part_acc + block * (32 * D) + part_at(f_pair, x) : static_cast<float*>(a.out) + row_of(f_pair) * D + x;
+      *reinterpret_cast<Floats<4>*>(dst) = v;
     }
-    if (kSplitKeys && (threadIdx.x & 7) == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(m_run, l_run);
+    if (kSplitKeys && (threadIdx.x & 7) == 0) *reinterpret_cast<float2*>(a.part_ml + (block * 32 + f_pair) * 2) = make_float2(m_run, l_run);
   }
   if (__builtin_amdgcn_ballot_w64(any_bad) != 0) s_bad = 1;
   __syncthreads();
@@ -291,7 +291,12 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_f32_kernel(const Packed
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __syncthreads();
     put_bad_values(a, vpool, bt, g, max(seg_begin * kPackedSeg, tile_lo) + wave, min(seg_end * kPackedSeg, tile_hi), kWaves, W, sq.ctx, lg,
-                   pair0, pairs, [&](int p, int x, float v) { dst[slot_of(p) * D + x] = v; });
+                   pair0, pairs, [&](int p, int x, float v) {
+                     if constexpr (kSplitKeys)
+                       a.part_acc[block * (32 * D) + part_at(p, x)] = v;
+                     else
+                       static_cast<float*>(a.out)[row_of(p) * D + x] = v;
+                   });
   }
 }
 

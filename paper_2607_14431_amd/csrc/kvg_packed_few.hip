@@ -221,16 +221,15 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
   }
 }
 
-// out = the segments of a row and query head folded in ascending order: a workgroup of D lanes (a dimension each).
-// T: type of the result.
-template <typename T, int D, bool kFew>
-__global__ __launch_bounds__(D) void packed_fold_kernel(const PackedAttnArgs a) {
+// out = the segments of a row and query head of the few kernel's, folded in ascending order: a workgroup of D lanes (a
+// dimension each).
+template <int D>
+__global__ __launch_bounds__(D) void packed_few_fold_kernel(const PackedAttnArgs a) {
   const int64_t id = blockIdx.x;                     // (layer, row of the launch, query head)
   const int h = (int)(id % a.Hq);
-  const int rows = kFew ? a.few_rows : a.seqs.n_tokens;
-  const int t = (int)(id / a.Hq % rows), l = (int)(id / a.Hq / rows);
-  const SeqUnit u = kFew ? find_unit(a.seqs, t, [&](const SeqRange& s) { return is_few(a, s) ? s.len : 0; }) : find_token(a.seqs, t);
-  if (u.b < 0 || (!kFew && is_few(a, u.range))) return;
+  const int t = (int)(id / a.Hq % a.few_rows), l = (int)(id / a.Hq / a.few_rows);
+  const SeqUnit u = find_unit(a.seqs, t, [&](const SeqRange& s) { return is_few(a, s) ? s.len : 0; });
+  if (u.b < 0) return;
   const int n = u.range.ctx + u.at;
   const int s_lo = window_start(layer_window(a, l), n + 1) / kPackedSeg, s_hi = n / kPackedSeg;
   const float* ml = a.part_ml + id * a.n_seg * 2;
@@ -243,7 +242,65 @@ __global__ __launch_bounds__(D) void packed_fold_kernel(const PackedAttnArgs a) 
     o_run = fmaf(acc[(int64_t)s * D], f.part, o_run * f.run);
   }
   const int64_t row = (int64_t)l * a.seqs.n_tokens + u.range.row0 + u.at;
-  static_cast<T*>(a.out)[(row * a.Hq + h) * D + threadIdx.x] = (T)(o_run * (1.0f / l_run));
+  static_cast<__bf16*>(a.out)[(row * a.Hq + h) * D + threadIdx.x] = (__bf16)(o_run * (1.0f / l_run));
+}
+
+// out = the segments of a split tile launch folded in ascending order.  A workgroup takes 32 dims of a block of 32 pairs, a wave
+// 8 of them: a lane a pair and 4 dims.  Segments that the block's other rows see but the lane's row does not have weight 0 there.
+// T: type of the result.  kPairs: pairs of a tile.
+template <typename T, int D, int kPairs>
+__global__ __launch_bounds__(256) void packed_fold_kernel(const PackedAttnArgs a) {
+  constexpr int kBlocks = kPairs / 32, kAhead = 8;   // kAhead: segments requested at a time
+  uint32_t id = blockIdx.x;                          // (layer, tile, KV head, block, 32 dims)
+  const int chunk = (int)(id % (D / 32)) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  id /= D / 32;
+  const int i = (int)(id % kBlocks);
+  id /= kBlocks;
+  const int g = (int)(id % (uint32_t)a.Hkv);
+  id /= (uint32_t)a.Hkv;
+  const int slot = (int)(id % (uint32_t)a.n_tiles), l = (int)(id / (uint32_t)a.n_tiles);
+  const int lg = 31 - __builtin_clz(a.group);
+  const SeqUnit u = find_unit(a.seqs, slot, [&](const SeqRange& s) {
+    return is_few(a, s) ? 0 : (int)((((int64_t)s.len << lg) + kPairs - 1) / kPairs);
+  });
+  if (u.b < 0) return;
+  const int pair0 = (u.count - 1 - u.at) * kPairs + 32 * i;
+  const int first = pair0 >> lg, last = min((pair0 + 31) >> lg, u.range.len - 1);
+  if (first >= u.range.len) return;
+  const int s_lo = window_start(layer_window(a, l), u.range.ctx + first + 1) / kPackedSeg, s_hi = (u.range.ctx + last) / kPackedSeg;
+  const int lane = threadIdx.x & 63;
+  const int64_t block = part_block(a, l, slot, g, kBlocks, i, 0);
+  const float* ml = a.part_ml + (block * 32 + (lane & 31)) * 2;
+  const float* acc = a.part_acc + block * (32 * D) + (chunk * 64 + lane) * 4;
+  float m_run = -INFINITY, l_run = 0.0f, o_run[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s0 = s_lo; s0 <= s_hi; s0 += kAhead) {
+    float2 x[kAhead];
+    float4 v[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int s = min(s0 + j, s_hi);
+      x[j] = *reinterpret_cast<const float2*>(ml + s * 64);
+      v[j] = *reinterpret_cast<const float4*>(acc + (int64_t)s * (32 * D));
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (s0 + j <= s_hi) {
+        const FoldFactors f = fold_factors(m_run, l_run, x[j].x, x[j].y);
+        o_run[0] = fmaf(v[j].x, f.part, o_run[0] * f.run);
+        o_run[1] = fmaf(v[j].y, f.part, o_run[1] * f.run);
+        o_run[2] = fmaf(v[j].z, f.part, o_run[2] * f.run);
+        o_run[3] = fmaf(v[j].w, f.part, o_run[3] * f.run);
+      }
+  }
+  const int p = pair0 + (lane & 31);
+  if ((p >> lg) >= u.range.len) return;
+  const int64_t row = ((int64_t)l * a.seqs.n_tokens + u.range.row0 + (p >> lg)) * a.Hq + g * a.group + (p & (a.group - 1));
+  const float inv = 1.0f / l_run;
+  struct alignas(4 * sizeof(T)) Four {
+    T x[4];
+  };
+  *reinterpret_cast<Four*>(static_cast<T*>(a.out) + row * D + chunk * 8 + (lane >> 5) * 4) = {
+      {(T)(o_run[0] * inv), (T)(o_run[1] * inv), (T)(o_run[2] * inv), (T)(o_run[3] * inv)}};
 }
 
 // Waves of a workgroup: four take a segment of a launch that leaves CUs idle soonest (one token over 4.6k keys at head_dim 256,
@@ -253,8 +310,9 @@ constexpr unsigned kFewGrid = 256;
 template <typename T, int D>
 void launch_few_d(const PackedAttnArgs& a, hipStream_t stream) {
   const unsigned grid = (unsigned)packed_few_workgroups(a);
-  if (D > 64 && grid <= kFewGrid)
-    packed_few_kernel<T, D, D == 64 ? 2 : 4><<<grid, 64 * 4, 0, stream>>>(a);
+  constexpr int kMost = D == 64 ? 2 : 4;
+  if (grid <= kFewGrid)
+    packed_few_kernel<T, D, kMost><<<grid, 64 * kMost, 0, stream>>>(a);
   else
     packed_few_kernel<T, D, 2><<<grid, 64 * 2, 0, stream>>>(a);
 }
@@ -270,15 +328,9 @@ hipError_t launch_few_t(const PackedAttnArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <typename T, bool kFew>
-hipError_t launch_fold_t(const PackedAttnArgs& a, hipStream_t stream) {
-  const unsigned grid = (unsigned)((int64_t)a.n_layers * (kFew ? a.few_rows : a.seqs.n_tokens) * a.Hq);
-  switch (a.D) {
-    case 64: packed_fold_kernel<T, 64, kFew><<<grid, 64, 0, stream>>>(a); break;
-    case 128: packed_fold_kernel<T, 128, kFew><<<grid, 128, 0, stream>>>(a); break;
-    case 256: packed_fold_kernel<T, 256, kFew><<<grid, 256, 0, stream>>>(a); break;
-    default: return hipErrorInvalidValue;
-  }
+template <typename T, int D, int kPairs>
+hipError_t launch_fold_d(const PackedAttnArgs& a, hipStream_t stream) {
+  packed_fold_kernel<T, D, kPairs><<<(unsigned)packed_fold_workgroups(a, kPairs), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -290,9 +342,25 @@ hipError_t launch_packed_few(const PackedAttnArgs& a, int dtype, hipStream_t str
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_packed_fold(const PackedAttnArgs& a, int dtype, bool few, hipStream_t stream) {
-  if (dtype == kDtypeF32) return few ? hipErrorInvalidValue : launch_fold_t<float, false>(a, stream);
-  return few ? launch_fold_t<__bf16, true>(a, stream) : launch_fold_t<__bf16, false>(a, stream);
+hipError_t launch_packed_few_fold(const PackedAttnArgs& a, hipStream_t stream) {
+  const unsigned grid = (unsigned)packed_few_fold_workgroups(a);
+  switch (a.D) {
+    case 64: packed_few_fold_kernel<64><<<grid, 64, 0, stream>>>(a); break;
+    case 128: packed_few_fold_kernel<128><<<grid, 128, 0, stream>>>(a); break;
+    case 256: packed_few_fold_kernel<256><<<grid, 256, 0, stream>>>(a); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_packed_fold(const PackedAttnArgs& a, int dtype, hipStream_t stream) {
+  const bool f32 = dtype == kDtypeF32;
+  switch (a.D) {
+    case 64: return f32 ? launch_fold_d<float, 64, kF32Pairs>(a, stream) : launch_fold_d<__bf16, 64, packed_tile_pairs(64)>(a, stream);
+    case 128: return f32 ? launch_fold_d<float, 128, kF32Pairs>(a, stream) : launch_fold_d<__bf16, 128, packed_tile_pairs(128)>(a, stream);
+    case 256: return f32 ? launch_fold_d<float, 256, kF32Pairs>(a, stream) : launch_fold_d<__bf16, 256, packed_tile_pairs(256)>(a, stream);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 }  // namespace kvg

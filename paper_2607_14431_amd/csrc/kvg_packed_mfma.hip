@@ -40,6 +40,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
   constexpr int NS = D / 16;               // MFMA steps over head_dim
   constexpr int ND = D / 32;               // 32-wide blocks of head_dim
   constexpr int BM = 32 * kBlocks * kWaves;
+  static_assert(BM == packed_tile_pairs(D), "the host's tiles");
   constexpr int kRing = kSplitKeys || D == 64 ? NS : 6;
   constexpr bool kSpread = D == 256;       // a tile's loads among the matrix steps, or all at its start
   using KR = KRows<RB>;
@@ -387,29 +388,30 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);     // the empty loads past the last tile write LDS: none may outlive the workgroup
 
-  // where a pair's result goes: its partial, or its row of the output
-  auto slot_of = [&](int p) -> int64_t {
+  // where a pair's results go: its block's partial, or its row of the output
+  auto block_of = [&](int rb) { return part_block(a, l, slot, g, kWaves * kBlocks, wave * kBlocks + rb, seg); };
+  auto row_of = [&](int p) -> int64_t {
     const int64_t tok = (int64_t)l * a.seqs.n_tokens + sq.row0 + (p >> lg);
-    const int64_t at = tok * a.Hq + g * a.group + (p & (a.group - 1));
-    return kSplitKeys ? at * a.n_seg + seg : at;
+    return tok * a.Hq + g * a.group + (p & (a.group - 1));
   };
   if constexpr (!kSplitKeys) fold();
 #pragma unroll
   for (int rb = 0; rb < kBlocks; ++rb) {
-    if (!row_ok[rb]) continue;
-    const int64_t at = slot_of(pair0 + 32 * rb + lrow);
     if constexpr (kSplitKeys) {
-      float* op = a.part_acc + at * D;
+      if (idle) break;
+      const int64_t block = block_of(rb);
+      float* op = a.part_acc + block * (32 * D) + lane * 4;
 #pragma unroll
       for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4)
-          *reinterpret_cast<float4*>(op + d * 32 + r4 * 8 + half * 4) =
+          *reinterpret_cast<float4*>(op + (d * 4 + r4) * 256) =
               make_float4(o[rb][d][r4 * 4], o[rb][d][r4 * 4 + 1], o[rb][d][r4 * 4 + 2], o[rb][d][r4 * 4 + 3]);
-      if (half == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(m[rb], lsum[rb]);
+      if (half == 0) *reinterpret_cast<float2*>(a.part_ml + (block * 32 + lrow) * 2) = make_float2(m[rb], lsum[rb]);
     } else {
+      if (!row_ok[rb]) continue;
       const float inv = 1.0f / l_run[rb];
-      uint16_t* op = static_cast<uint16_t*>(a.out) + at * D;
+      uint16_t* op = static_cast<uint16_t*>(a.out) + row_of(pair0 + 32 * rb + lrow) * D;
 #pragma unroll
       for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -429,11 +431,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
       if (!(min(key0 + kTileKeys, n_hi) - 1 > tile_first || key0 < tile_mask_lo)) continue;
       put_bad_values(a, vpool, bt, g, max(key0, wave_lo), min(key0 + kTileKeys, wave_last + 1), 1, W, ctx, lg, pair0, pairs,
                      [&](int p, int x, float v) {
-                       const int64_t at = slot_of(pair0 + p) * D + x;
                        if constexpr (kSplitKeys)
-                         a.part_acc[at] = v;
+                         a.part_acc[block_of(p >> 5) * (32 * D) + part_at(p & 31, x)] = v;
                        else
-                         static_cast<uint16_t*>(a.out)[at] = (uint16_t)(__float_as_uint(v) >> 16);
+                         static_cast<uint16_t*>(a.out)[row_of(pair0 + p) * D + x] = (uint16_t)(__float_as_uint(v) >> 16);
                      });
     }
   }
@@ -460,8 +461,6 @@ hipError_t launch_t(const PackedAttnArgs& a, hipStream_t stream) {
 }
 
 }  // namespace
-
-int packed_tile_pairs(int D) { return 32 * kWaves * (D == 64 ? 2 : 1); }
 
 hipError_t launch_packed_tiles(const PackedAttnArgs& a, int dtype, hipStream_t stream) {
   if (dtype == kDtypeBf16) return launch_t<uint16_t>(a, stream);
