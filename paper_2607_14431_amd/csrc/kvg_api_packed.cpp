@@ -153,8 +153,8 @@ AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, i
   }
   const int64_t tile_grid = n_layers * r.n_tiles * c->n_kv_heads, fold_grid = (bm / 32) * (c->head_dim / 32);
   r.fits = fits_grid((int64_t)n_layers * r.few_seg * (r.few_rows > 0 ? s->batch : 0) * c->n_kv_heads, 256) &&
-           fits_grid(n_layers * r.few_rows * c->n_q_heads, 256) &&
-           fits_grid(tile_grid * std::max<int64_t>(r.tile_seg, r.tile_seg > 1 ? fold_grid : 1), 256);
+           fits_grid(tile_grid * r.tile_seg, 256) &&
+           fits_grid(n_layers * r.few_rows * c->n_q_heads + (r.tile_seg > 1 ? tile_grid * fold_grid : 0), 256);
   if (!r.fits) return r;
   auto bytes = [&](int64_t row_heads, int32_t n_seg, size_t values) {
     return n_seg > 1 ? align_up((size_t)n_layers * row_heads * n_seg * values * sizeof(float)) : 0;
@@ -167,26 +167,20 @@ AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, i
   return r;
 }
 
-// The tiles' launch, the few kernel's, and the folds of those that are split.
+// The tiles' launch, the few kernel's, and the fold of those that are split.
 int attn_launch(kvg::PackedAttnArgs a, const AttnPlan& plan, int32_t dtype, char* ws, hipStream_t stream) {
   a.few_rows = (int32_t)plan.few_rows;
   a.n_tiles = (int32_t)plan.n_tiles;
   kvg::PackedAttnArgs few = a, tiles = a;
-  few.n_seg = plan.few_seg;
-  few.part_ml = reinterpret_cast<float*>(ws);
-  few.part_acc = reinterpret_cast<float*>(ws + plan.few_ml);
-  tiles.n_seg = plan.tile_seg;
-  tiles.part_ml = reinterpret_cast<float*>(ws + plan.few_ml + plan.few_acc);
-  tiles.part_acc = reinterpret_cast<float*>(ws + plan.few_ml + plan.few_acc + plan.tile_ml);
+  few.part = {reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + plan.few_ml), plan.few_seg};
+  ws += plan.few_ml + plan.few_acc;
+  tiles.part = {reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + plan.tile_ml), plan.tile_seg};
   int st = KVG_OK;
-  if (a.n_tiles > 0) {
+  if (a.n_tiles > 0)
     st = hip_status(dtype == KVG_F32 ? kvg::launch_packed_f32(tiles, stream) : kvg::launch_packed_tiles(tiles, dtype, stream));
-    if (st == KVG_OK && plan.tile_seg > 1) st = hip_status(kvg::launch_packed_fold(tiles, dtype, stream));
-  }
-  if (st == KVG_OK && a.few_rows > 0) {
-    st = hip_status(kvg::launch_packed_few(few, dtype, stream));
-    if (st == KVG_OK && plan.few_seg > 1) st = hip_status(kvg::launch_packed_few_fold(few, stream));
-  }
+  if (st == KVG_OK && a.few_rows > 0) st = hip_status(kvg::launch_packed_few(few, dtype, stream));
+  if (st == KVG_OK && (plan.tile_seg > 1 || plan.few_seg > 1))
+    st = hip_status(kvg::launch_packed_fold(tiles, few.part, dtype, stream));
   return st;
 }
 

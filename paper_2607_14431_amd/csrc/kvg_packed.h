@@ -116,6 +116,13 @@ struct NormAppendArgs {
   RotaryArgs rot;
 };
 
+// Partials of a launch over n_seg segments: a (reference, sum) and D sums per pair and segment.
+struct PackedPartials {
+  float* ml;
+  float* acc;
+  int32_t n_seg;              // 1: the launch is not split
+};
+
 struct PackedAttnArgs {
   PackedSeqs seqs;
   const void* k_pool;
@@ -128,12 +135,10 @@ struct PackedAttnArgs {
   int32_t Hq, Hkv, D, group, layer0, n_layers;
   // Sequences go in tiles of (row, query head) pairs of a KV head (n_tiles: a bound of the batch's); in bf16 and fp8 caches
   // those of at most kFewPairs pairs are the few kernel's where it runs (few_rows > 0: a bound of their rows).
-  // A launch over n_seg > 1 segments leaves partials (reference and sum, then D sums): the few kernel
-  // [n_layers][rows][Hq][n_seg], rows counted over its own sequences; tiles in blocks of 32 pairs (part_block).
+  // Where a split launch leaves its partials: the few kernel [n_layers][rows][Hq][n_seg], rows counted over its own
+  // sequences; tiles in blocks of 32 pairs (part_block).
   int32_t few_rows, n_tiles;
-  int32_t n_seg;
-  float* part_acc;
-  float* part_ml;
+  PackedPartials part;
   int32_t window[kMaxWindowLayers];
 };
 
@@ -145,17 +150,15 @@ __device__ __forceinline__ bool is_few(const PackedAttnArgs& a, const SeqRange& 
   return a.few_rows > 0 && (int64_t)s.len * a.group <= kFewPairs;
 }
 constexpr int packed_tile_pairs(int D) { return D == 64 ? 256 : 128; }
-inline int64_t packed_tile_workgroups(const PackedAttnArgs& a) { return (int64_t)a.n_layers * a.n_seg * a.n_tiles * a.Hkv; }
-inline int64_t packed_few_workgroups(const PackedAttnArgs& a) { return (int64_t)a.n_layers * a.n_seg * a.seqs.batch * a.Hkv; }
+inline int64_t packed_tile_workgroups(const PackedAttnArgs& a) { return (int64_t)a.n_layers * a.part.n_seg * a.n_tiles * a.Hkv; }
+inline int64_t packed_few_workgroups(const PackedAttnArgs& a) { return (int64_t)a.n_layers * a.part.n_seg * a.seqs.batch * a.Hkv; }
 hipError_t launch_packed_tiles(const PackedAttnArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_packed_few(const PackedAttnArgs& a, int dtype, hipStream_t stream);
-// out = the segments of a split launch, folded in order
-inline int64_t packed_few_fold_workgroups(const PackedAttnArgs& a) { return (int64_t)a.n_layers * a.few_rows * a.Hq; }
+// out = the segments of the split launches, folded in order: of the tiles (a.part) and of the few kernel
 inline int64_t packed_fold_workgroups(const PackedAttnArgs& a, int pairs) {
   return (int64_t)a.n_layers * a.n_tiles * a.Hkv * (pairs / 32) * (a.D / 32);
 }
-hipError_t launch_packed_few_fold(const PackedAttnArgs& a, hipStream_t stream);
-hipError_t launch_packed_fold(const PackedAttnArgs& a, int dtype, hipStream_t stream);
+hipError_t launch_packed_fold(const PackedAttnArgs& a, const PackedPartials& few, int dtype, hipStream_t stream);
 // fp32 caches: tiles of kF32Pairs pairs
 constexpr int kF32Pairs = 32;
 hipError_t launch_packed_f32(const PackedAttnArgs& a, hipStream_t stream);

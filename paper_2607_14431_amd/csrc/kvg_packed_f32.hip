@@ -60,12 +60,12 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_f32_kernel(const Packed
   id /= (uint32_t)a.Hkv;
   int seg = 0;
   if constexpr (kSplitKeys) {
-    seg = (int)(id % (uint32_t)a.n_seg);
-    id /= (uint32_t)a.n_seg;
+    seg = (int)(id % (uint32_t)a.part.n_seg);
+    id /= (uint32_t)a.part.n_seg;
   }
   const int l = (int)(id % (uint32_t)a.n_layers);
   const int slot = (int)(id / (uint32_t)a.n_layers);
-  if constexpr (kSplitKeys) seg = (int)((uint32_t)(seg + slot) % (uint32_t)a.n_seg);
+  if constexpr (kSplitKeys) seg = (int)((uint32_t)(seg + slot) % (uint32_t)a.part.n_seg);
   const SeqUnit u = find_unit(a.seqs, slot, [&](const SeqRange& s) { return (int)((((int64_t)s.len << lg) + 31) / 32); });
   if (u.b < 0) return;
   const SeqRange sq = u.range;
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_f32_kernel(const Packed
   }
 
   // ---- the partial, or the result
-  const int64_t block = part_block(a, l, slot, g, 1, 0, seg);
+  const int64_t block = part_block(a, a.part.n_seg, l, slot, g, 1, 0, seg);
   auto row_of = [&](int p) -> int64_t {
     const int64_t tok = (int64_t)l * a.seqs.n_tokens + sq.row0 + ((pair0 + p) >> lg);
     return tok * a.Hq + g * a.group + ((pair0 + p) & (a.group - 1));
@@ -280,10 +280,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_f32_kernel(const Packed
 #pragma unroll
       for (int i = 0; i < 4; ++i) v.x[i] = kSplitKeys ? run[(4 * j + i) % ND][(4 * j + i) / ND] : run[(4 * j + i) % ND][(4 * j + i) / ND] * inv;
       const int x = ND * f_i + 4 * j;
-      float* dst = kSplitKeys ? a.part_acc + block * (32 * D) + part_at(f_pair, x) : static_cast<float*>(a.out) + row_of(f_pair) * D + x;
+      float* dst = kSplitKeys ? a.part.acc + block * (32 * D) + part_at(f_pair, x) : static_cast<float*>(a.out) + row_of(f_pair) * D + x;
       *reinterpret_cast<Floats<4>*>(dst) = v;
     }
-    if (kSplitKeys && (threadIdx.x & 7) == 0) *reinterpret_cast<float2*>(a.part_ml + (block * 32 + f_pair) * 2) = make_float2(m_run, l_run);
+    if (kSplitKeys && (threadIdx.x & 7) == 0) *reinterpret_cast<float2*>(a.part.ml + (block * 32 + f_pair) * 2) = make_float2(m_run, l_run);
   }
   if (__builtin_amdgcn_ballot_w64(any_bad) != 0) s_bad = 1;
   __syncthreads();
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_f32_kernel(const Packed
     put_bad_values(a, vpool, bt, g, max(seg_begin * kPackedSeg, tile_lo) + wave, min(seg_end * kPackedSeg, tile_hi), kWaves, W, sq.ctx, lg,
                    pair0, pairs, [&](int p, int x, float v) {
                      if constexpr (kSplitKeys)
-                       a.part_acc[block * (32 * D) + part_at(p, x)] = v;
+                       a.part.acc[block * (32 * D) + part_at(p, x)] = v;
                      else
                        static_cast<float*>(a.out)[row_of(p) * D + x] = v;
                    });
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_f32_kernel(const Packed
 template <int D>
 hipError_t launch_f32_d(const PackedAttnArgs& a, hipStream_t stream) {
   const unsigned grid = (unsigned)packed_tile_workgroups(a);
-  if (a.n_seg > 1)
+  if (a.part.n_seg > 1)
     packed_f32_kernel<D, true><<<grid, 64 * kWaves, 0, stream>>>(a);
   else
     packed_f32_kernel<D, false><<<grid, 64 * kWaves, 0, stream>>>(a);

@@ -47,11 +47,11 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
   uint32_t id = blockIdx.x;
   const int g = (int)(id % (uint32_t)a.Hkv);
   id /= (uint32_t)a.Hkv;
-  int seg = (int)(id % (uint32_t)a.n_seg);
-  id /= (uint32_t)a.n_seg;
+  int seg = (int)(id % (uint32_t)a.part.n_seg);
+  id /= (uint32_t)a.part.n_seg;
   const int b = (int)(id % (uint32_t)a.seqs.batch);
   const int l = (int)(id / (uint32_t)a.seqs.batch);
-  seg = (int)((uint32_t)(seg + b) % (uint32_t)a.n_seg);
+  seg = (int)((uint32_t)(seg + b) % (uint32_t)a.part.n_seg);
   const int32_t* bt = a.seqs.tables + (int64_t)b * a.seqs.max_pages;
   // page ids of the segment, one per lane (requested with the sequence's range)
   const int32_t pg = bt[min(seg * (kPackedSeg / kPage) + (lane & 31), a.seqs.max_pages - 1)];
@@ -178,24 +178,24 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
   __builtin_amdgcn_s_waitcnt(vm_wait(0));            // the empty loads past the last unit write LDS: none may outlive the workgroup
 
   // ---- the segment's partial, or the result when there is one segment
-  const int rank = a.n_seg > 1 ? few_rows_before(a, b) : 0;
-  if (a.n_seg > 1 && rank + sq.len > a.few_rows) return;     // overlapping ranges hold more rows than there are
+  const int rank = a.part.n_seg > 1 ? few_rows_before(a, b) : 0;
+  if (a.part.n_seg > 1 && rank + sq.len > a.few_rows) return;     // overlapping ranges hold more rows than there are
   auto slot_of = [&](int p) -> int64_t {
     const int h = g * a.group + (p & (a.group - 1));
-    if (a.n_seg > 1) return (((int64_t)l * a.few_rows + rank + (p >> lg)) * a.Hq + h) * a.n_seg + seg;
+    if (a.part.n_seg > 1) return (((int64_t)l * a.few_rows + rank + (p >> lg)) * a.Hq + h) * a.part.n_seg + seg;
     return ((int64_t)l * a.seqs.n_tokens + sq.row0 + (p >> lg)) * a.Hq + h;
   };
   if (pair_ok) {
     const int64_t at = slot_of(pair);
-    if (a.n_seg > 1) {
-      float* op = a.part_acc + at * D + wave * NDW * 32;
+    if (a.part.n_seg > 1) {
+      float* op = a.part.acc + at * D + wave * NDW * 32;
 #pragma unroll
       for (int d = 0; d < NDW; ++d)
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4)
           *reinterpret_cast<float4*>(op + d * 32 + r4 * 8 + half * 4) =
               make_float4(o[d][r4 * 4], o[d][r4 * 4 + 1], o[d][r4 * 4 + 2], o[d][r4 * 4 + 3]);
-      if (wave == 0 && half == 0) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(m, lsum);
+      if (wave == 0 && half == 0) *reinterpret_cast<float2*>(a.part.ml + at * 2) = make_float2(m, lsum);
     } else {
       const float inv = 1.0f / lsum;
       uint16_t* op = static_cast<uint16_t*>(a.out) + at * D + wave * NDW * 32;
@@ -213,45 +213,47 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
     __syncthreads();
     put_bad_values(a, vpool, bt, g, k_begin + wave, k_end, kWaves, W, sq.ctx, lg, 0, n_pairs, [&](int p, int x, float v) {
       const int64_t at = slot_of(p) * D + x;
-      if (a.n_seg > 1)
-        a.part_acc[at] = v;
+      if (a.part.n_seg > 1)
+        a.part.acc[at] = v;
       else
         static_cast<uint16_t*>(a.out)[at] = (uint16_t)(__float_as_uint(v) >> 16);
     });
   }
 }
 
-// out = the segments of a row and query head of the few kernel's, folded in ascending order: a workgroup of D lanes (a
-// dimension each).
+// The folds.  out = a row's segments folded in ascending order, in the operations of a tile kernel that walks all keys.
+//
+// Rows of the few kernel's: a lane a dimension of a (layer, row of the launch, query head).
 template <int D>
-__global__ __launch_bounds__(D) void packed_few_fold_kernel(const PackedAttnArgs a) {
-  const int64_t id = blockIdx.x;                     // (layer, row of the launch, query head)
+__device__ __forceinline__ void fold_few(const PackedAttnArgs& a, const PackedPartials& part, uint32_t workgroup) {
+  const int64_t id = (int64_t)workgroup * (256 / D) + __builtin_amdgcn_readfirstlane(threadIdx.x / D);
+  const int x = threadIdx.x % D;
   const int h = (int)(id % a.Hq);
   const int t = (int)(id / a.Hq % a.few_rows), l = (int)(id / a.Hq / a.few_rows);
+  if (l >= a.n_layers) return;
   const SeqUnit u = find_unit(a.seqs, t, [&](const SeqRange& s) { return is_few(a, s) ? s.len : 0; });
   if (u.b < 0) return;
   const int n = u.range.ctx + u.at;
   const int s_lo = window_start(layer_window(a, l), n + 1) / kPackedSeg, s_hi = n / kPackedSeg;
-  const float* ml = a.part_ml + id * a.n_seg * 2;
-  const float* acc = a.part_acc + id * a.n_seg * D + threadIdx.x;
+  const float* ml = part.ml + id * part.n_seg * 2;
+  const float* acc = part.acc + id * part.n_seg * D + x;
   float m_run = -INFINITY, l_run = 0.0f, o_run = 0.0f;
 #pragma unroll 8
   for (int s = s_lo; s <= s_hi; ++s) {
-    const float2 x = *reinterpret_cast<const float2*>(ml + 2 * s);
-    const FoldFactors f = fold_factors(m_run, l_run, x.x, x.y);
+    const float2 y = *reinterpret_cast<const float2*>(ml + 2 * s);
+    const FoldFactors f = fold_factors(m_run, l_run, y.x, y.y);
     o_run = fmaf(acc[(int64_t)s * D], f.part, o_run * f.run);
   }
   const int64_t row = (int64_t)l * a.seqs.n_tokens + u.range.row0 + u.at;
-  static_cast<__bf16*>(a.out)[(row * a.Hq + h) * D + threadIdx.x] = (__bf16)(o_run * (1.0f / l_run));
+  static_cast<__bf16*>(a.out)[(row * a.Hq + h) * D + x] = (__bf16)(o_run * (1.0f / l_run));
 }
 
-// out = the segments of a split tile launch folded in ascending order.  A workgroup takes 32 dims of a block of 32 pairs, a wave
-// 8 of them: a lane a pair and 4 dims.  Segments that the block's other rows see but the lane's row does not have weight 0 there.
-// T: type of the result.  kPairs: pairs of a tile.
+// Tiles: a workgroup takes 32 dims of a block of 32 pairs, a wave 8 of them, a lane a pair and 4 dims.  Segments that the
+// block's other rows see but the lane's row does not have weight 0 there.  T: type of the result.  kPairs: pairs of a tile.
 template <typename T, int D, int kPairs>
-__global__ __launch_bounds__(256) void packed_fold_kernel(const PackedAttnArgs a) {
+__device__ __forceinline__ void fold_tiles(const PackedAttnArgs& a, const PackedPartials& part, uint32_t id) {
   constexpr int kBlocks = kPairs / 32, kAhead = 8;   // kAhead: segments requested at a time
-  uint32_t id = blockIdx.x;                          // (layer, tile, KV head, block, 32 dims)
+  // (layer, tile, KV head, block, 32 dims)
   const int chunk = (int)(id % (D / 32)) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   id /= D / 32;
   const int i = (int)(id % kBlocks);
@@ -269,9 +271,9 @@ __global__ __launch_bounds__(256) void packed_fold_kernel(const PackedAttnArgs a
   if (first >= u.range.len) return;
   const int s_lo = window_start(layer_window(a, l), u.range.ctx + first + 1) / kPackedSeg, s_hi = (u.range.ctx + last) / kPackedSeg;
   const int lane = threadIdx.x & 63;
-  const int64_t block = part_block(a, l, slot, g, kBlocks, i, 0);
-  const float* ml = a.part_ml + (block * 32 + (lane & 31)) * 2;
-  const float* acc = a.part_acc + block * (32 * D) + (chunk * 64 + lane) * 4;
+  const int64_t block = part_block(a, part.n_seg, l, slot, g, kBlocks, i, 0);
+  const float* ml = part.ml + (block * 32 + (lane & 31)) * 2;
+  const float* acc = part.acc + block * (32 * D) + (chunk * 64 + lane) * 4;
   float m_run = -INFINITY, l_run = 0.0f, o_run[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int s0 = s_lo; s0 <= s_hi; s0 += kAhead) {
     float2 x[kAhead];
@@ -303,6 +305,15 @@ __global__ __launch_bounds__(256) void packed_fold_kernel(const PackedAttnArgs a
       {(T)(o_run[0] * inv), (T)(o_run[1] * inv), (T)(o_run[2] * inv), (T)(o_run[3] * inv)}};
 }
 
+// Both in one launch: the few kernel's rows first, in few_workgroups workgroups.
+template <typename T, int D, int kPairs>
+__global__ __launch_bounds__(256) void packed_fold_kernel(const PackedAttnArgs a, const PackedPartials few, const uint32_t few_workgroups) {
+  if (blockIdx.x < few_workgroups)
+    fold_few<D>(a, few, blockIdx.x);
+  else
+    fold_tiles<T, D, kPairs>(a, a.part, blockIdx.x - few_workgroups);
+}
+
 // Waves of a workgroup: four take a segment of a launch that leaves CUs idle soonest (one token over 4.6k keys at head_dim 256,
 // 80 workgroups: 19 us; two waves 27), two leave room for more workgroups on a CU, whose starts and ends then
 // overlap (16 tokens over 33k keys: 650 us with four waves, 521 with two).
@@ -329,8 +340,11 @@ hipError_t launch_few_t(const PackedAttnArgs& a, hipStream_t stream) {
 }
 
 template <typename T, int D, int kPairs>
-hipError_t launch_fold_d(const PackedAttnArgs& a, hipStream_t stream) {
-  packed_fold_kernel<T, D, kPairs><<<(unsigned)packed_fold_workgroups(a, kPairs), 256, 0, stream>>>(a);
+hipError_t launch_fold_d(const PackedAttnArgs& a, const PackedPartials& few, hipStream_t stream) {
+  const int64_t few_rows = few.n_seg > 1 ? (int64_t)a.n_layers * a.few_rows * a.Hq : 0;
+  const unsigned few_workgroups = (unsigned)((few_rows + 256 / D - 1) / (256 / D));
+  const unsigned tiles = a.part.n_seg > 1 ? (unsigned)packed_fold_workgroups(a, kPairs) : 0;
+  packed_fold_kernel<T, D, kPairs><<<few_workgroups + tiles, 256, 0, stream>>>(a, few, few_workgroups);
   return hipGetLastError();
 }
 
@@ -342,23 +356,12 @@ hipError_t launch_packed_few(const PackedAttnArgs& a, int dtype, hipStream_t str
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_packed_few_fold(const PackedAttnArgs& a, hipStream_t stream) {
-  const unsigned grid = (unsigned)packed_few_fold_workgroups(a);
-  switch (a.D) {
-    case 64: packed_few_fold_kernel<64><<<grid, 64, 0, stream>>>(a); break;
-    case 128: packed_few_fold_kernel<128><<<grid, 128, 0, stream>>>(a); break;
-    case 256: packed_few_fold_kernel<256><<<grid, 256, 0, stream>>>(a); break;
-    default: return hipErrorInvalidValue;
-  }
-  return hipGetLastError();
-}
-
-hipError_t launch_packed_fold(const PackedAttnArgs& a, int dtype, hipStream_t stream) {
+hipError_t launch_packed_fold(const PackedAttnArgs& a, const PackedPartials& few, int dtype, hipStream_t stream) {
   const bool f32 = dtype == kDtypeF32;
   switch (a.D) {
-    case 64: return f32 ? launch_fold_d<float, 64, kF32Pairs>(a, stream) : launch_fold_d<__bf16, 64, packed_tile_pairs(64)>(a, stream);
-    case 128: return f32 ? launch_fold_d<float, 128, kF32Pairs>(a, stream) : launch_fold_d<__bf16, 128, packed_tile_pairs(128)>(a, stream);
-    case 256: return f32 ? launch_fold_d<float, 256, kF32Pairs>(a, stream) : launch_fold_d<__bf16, 256, packed_tile_pairs(256)>(a, stream);
+    case 64: return f32 ? launch_fold_d<float, 64, kF32Pairs>(a, few, stream) : launch_fold_d<__bf16, 64, packed_tile_pairs(64)>(a, few, stream);
+    case 128: return f32 ? launch_fold_d<float, 128, kF32Pairs>(a, few, stream) : launch_fold_d<__bf16, 128, packed_tile_pairs(128)>(a, few, stream);
+    case 256: return f32 ? launch_fold_d<float, 256, kF32Pairs>(a, few, stream) : launch_fold_d<__bf16, 256, packed_tile_pairs(256)>(a, few, stream);
     default: return hipErrorInvalidValue;
   }
 }

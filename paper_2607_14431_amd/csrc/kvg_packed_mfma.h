@@ -190,8 +190,8 @@ __device__ __forceinline__ int few_rows_before(const PackedAttnArgs& a, int b) {
 // Where a split tile launch leaves its partials: blocks of 32 pairs x D sums for every (layer, tile, KV head, block of the
 // tile, segment).  A block's sums are in the order of the matrix steps' results (lane of 64, 4 dims), so that they are
 // written and read 1 KiB at a time.
-__device__ __forceinline__ int64_t part_block(const PackedAttnArgs& a, int l, int slot, int g, int blocks, int i, int seg) {
-  return ((((int64_t)l * a.n_tiles + slot) * a.Hkv + g) * blocks + i) * a.n_seg + seg;
+__device__ __forceinline__ int64_t part_block(const PackedAttnArgs& a, int n_seg, int l, int slot, int g, int blocks, int i, int seg) {
+  return ((((int64_t)l * a.n_tiles + slot) * a.Hkv + g) * blocks + i) * n_seg + seg;
 }
 __device__ __forceinline__ int part_at(int pair, int x) { return ((x >> 3) * 64 + ((x >> 2) & 1) * 32 + pair) * 4 + (x & 3); }
 

@@ -66,12 +66,12 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
   id /= (uint32_t)a.Hkv;
   int seg = 0;
   if constexpr (kSplitKeys) {
-    seg = (int)(id % (uint32_t)a.n_seg);
-    id /= (uint32_t)a.n_seg;
+    seg = (int)(id % (uint32_t)a.part.n_seg);
+    id /= (uint32_t)a.part.n_seg;
   }
   const int l = (int)(id % (uint32_t)a.n_layers);
   const int slot = (int)(id / (uint32_t)a.n_layers);
-  if constexpr (kSplitKeys) seg = (int)((uint32_t)(seg + slot) % (uint32_t)a.n_seg);      // a segment not always on the same XCD
+  if constexpr (kSplitKeys) seg = (int)((uint32_t)(seg + slot) % (uint32_t)a.part.n_seg);      // a segment not always on the same XCD
   const SeqUnit u = find_unit(a.seqs, slot, [&](const SeqRange& s) {
     return is_few(a, s) ? 0 : (int)((((int64_t)s.len << lg) + BM - 1) / BM);
   });
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
   __builtin_amdgcn_s_waitcnt(0x0F70);     // the empty loads past the last tile write LDS: none may outlive the workgroup
 
   // where a pair's results go: its block's partial, or its row of the output
-  auto block_of = [&](int rb) { return part_block(a, l, slot, g, kWaves * kBlocks, wave * kBlocks + rb, seg); };
+  auto block_of = [&](int rb) { return part_block(a, a.part.n_seg, l, slot, g, kWaves * kBlocks, wave * kBlocks + rb, seg); };
   auto row_of = [&](int p) -> int64_t {
     const int64_t tok = (int64_t)l * a.seqs.n_tokens + sq.row0 + (p >> lg);
     return tok * a.Hq + g * a.group + (p & (a.group - 1));
@@ -400,14 +400,14 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
     if constexpr (kSplitKeys) {
       if (idle) break;
       const int64_t block = block_of(rb);
-      float* op = a.part_acc + block * (32 * D) + lane * 4;
+      float* op = a.part.acc + block * (32 * D) + lane * 4;
 #pragma unroll
       for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4)
           *reinterpret_cast<float4*>(op + (d * 4 + r4) * 256) =
               make_float4(o[rb][d][r4 * 4], o[rb][d][r4 * 4 + 1], o[rb][d][r4 * 4 + 2], o[rb][d][r4 * 4 + 3]);
-      if (half == 0) *reinterpret_cast<float2*>(a.part_ml + (block * 32 + lrow) * 2) = make_float2(m[rb], lsum[rb]);
+      if (half == 0) *reinterpret_cast<float2*>(a.part.ml + (block * 32 + lrow) * 2) = make_float2(m[rb], lsum[rb]);
     } else {
       if (!row_ok[rb]) continue;
       const float inv = 1.0f / l_run[rb];
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
       put_bad_values(a, vpool, bt, g, max(key0, wave_lo), min(key0 + kTileKeys, wave_last + 1), 1, W, ctx, lg, pair0, pairs,
                      [&](int p, int x, float v) {
                        if constexpr (kSplitKeys)
-                         a.part_acc[block_of(p >> 5) * (32 * D) + part_at(p & 31, x)] = v;
+                         a.part.acc[block_of(p >> 5) * (32 * D) + part_at(p & 31, x)] = v;
                        else
                          static_cast<uint16_t*>(a.out)[row_of(pair0 + p) * D + x] = (uint16_t)(__float_as_uint(v) >> 16);
                      });
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
 template <typename T, int D, int kBlocks>
 hipError_t launch_d(const PackedAttnArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)packed_tile_workgroups(a));
-  if (a.n_seg > 1)
+  if (a.part.n_seg > 1)
     packed_tiles_kernel<T, D, kBlocks, true><<<grid, 64 * kWaves, 0, stream>>>(a);
   else
     packed_tiles_kernel<T, D, kBlocks, false><<<grid, 64 * kWaves, 0, stream>>>(a);

@@ -400,6 +400,14 @@ def _token_stride(t: torch.Tensor, n_layers: int, n_tokens: int, heads: int, hea
     return st
 
 
+def _on_current_device(*tensors):
+    """The packed calls run on the current device's current stream: tensors of another device are refused."""
+    here = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"a tensor on {t.device}, the current device is {here}")
+
+
 def kvg_rotary_frequencies(rt: kvg_rotary, head_dim: int) -> list[float]:
     theta = (ctypes.c_double * 128)()
     _check(_lib.kvg_rotary_frequencies(ctypes.byref(rt), head_dim, theta), "kvg_rotary_frequencies")
@@ -420,6 +428,7 @@ def kvg_rotate(rt: kvg_rotary, positions: torch.Tensor, x: torch.Tensor, y: torc
     if T <= 1:
         sx = sy = 0
     assert positions.dtype is torch.int64 and positions.is_contiguous() and positions.numel() == T
+    _on_current_device(positions, x, y)
     _check(_lib.kvg_rotate(ctypes.byref(rt), 1 if dtype is torch.bfloat16 else 0, D, T, H, positions.data_ptr(), x.data_ptr(), sx,
                            y.data_ptr(), sy, _stream(stream)), "kvg_rotate")
 
@@ -437,6 +446,7 @@ def kvg_norm_append(cache: Cache, seqs: Seqs, packed: Packed, rt: kvg_rotary, no
         assert q_out.shape == (n_layers, T, cache.n_q_heads, D) and q_out.dtype is raw and q_out.is_contiguous()
     sk, sv = (_token_stride(t, n_layers, T, Hkv, D, raw) for t in (k_raw, v_raw))
     ns = None if norm is None else norm.struct(cache, n_layers)
+    _on_current_device(cache.k_pool, cache.v_pool, packed.cu_tokens, seqs.block_tables, k_raw, v_raw, q_raw, q_out)
     _check(_lib.kvg_norm_append(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()),
                                 ctypes.byref(packed.struct(seqs, sq, sk, sv)), ctypes.byref(rt),
                                 None if ns is None else ctypes.byref(ns), layer0, n_layers, _ptr(q_raw), _ptr(k_raw),
@@ -461,6 +471,7 @@ def kvg_packed_attn(cache: Cache, seqs: Seqs, packed: Packed, layer0: int, n_lay
     raw, T, D, Hq = cache.raw_dtype, packed.n_tokens, cache.head_dim, cache.n_q_heads
     sq = _token_stride(q, n_layers, T, Hq, D, raw)
     assert out.shape == (n_layers, T, Hq, D) and out.dtype is raw and out.is_contiguous()
+    _on_current_device(cache.k_pool, cache.v_pool, packed.cu_tokens, seqs.block_tables, q, out, ws)
     _check(_lib.kvg_packed_attn(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()),
                                 ctypes.byref(packed.struct(seqs, sq)), layer0, n_layers, _ptr(q), scale, _ptr(out),
                                 _ptr(ws), ws.nbytes, _stream(stream)), "kvg_packed_attn")
