@@ -384,7 +384,7 @@ typedef struct {
 /* The new tokens of a batch, one sequence after the other: rows [cu_tokens[b], cu_tokens[b + 1]) of the
  * packed tensors are sequence b's tokens at logical indices ctx_lens[b] + 0, 1, ... (ctx_lens: the
  * tokens cached before them).  A sequence may have none.  Rows below cu_tokens[0] and from
- * cu_tokens[batch] on (a batch padded to a fixed size) are neither read nor written.  cu_tokens ascends; a
+ * cu_tokens[batch] on (a batch padded to a fixed size) are neither used nor written.  cu_tokens ascends; a
  * sequence whose range descends, passes n_tokens or holds more than max_len tokens, whose ctx_lens is
  * outside [0, max_ctx_len], or whose tokens pass its block table is skipped.
  * Strides: elements from one token's row of the raw queries (keys, values) to the next one's,
@@ -444,7 +444,8 @@ size_t kvg_packed_attn_workspace_bytes(const kvg_cache* cache, const kvg_seqs* s
  * into calls, nor on the other sequences or the pages.  A whole prompt and a suffix over its grafted
  * prefix give the same bytes for the same token.  Inf and NaN among the keys and values reach
  * the rows that see their token and no others.  seqs->start_pos is not read; seqs->shared_tokens is
- * ignored.  ws_dev: kvg_packed_attn_workspace_bytes() bytes of scratch.
+ * ignored.  ws_dev: kvg_packed_attn_workspace_bytes() bytes of scratch; nothing is kept in it from call to
+ * call, and calls that may run at once need one each.
  * Errors: as kvg_norm_append, and KVG_E_WORKSPACE. */
 int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, int32_t layer0,
                     int32_t n_layers, const void* q_dev, float scale, void* out_dev, void* ws_dev, size_t ws_bytes,

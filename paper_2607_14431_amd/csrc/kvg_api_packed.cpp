@@ -92,7 +92,7 @@ int check_packed(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p) {
   if (p == nullptr || p->cu_tokens == nullptr || p->n_tokens < 0 || p->max_len < 0) return KVG_E_INVAL;
   if (s->batch <= 0 || s->max_pages <= 0 || s->max_ctx_len < 0) return KVG_E_INVAL;
   const int64_t room = (int64_t)s->max_pages * c->page_size;
-  if (room > INT32_MAX) return KVG_E_SHAPE;
+  if (room > INT32_MAX - 2 * kvg::kPackedSeg) return KVG_E_SHAPE;      // a segment's end is an int
   if (s->max_ctx_len > room || p->max_len > room) return KVG_E_CAPACITY;
   return KVG_OK;
 }

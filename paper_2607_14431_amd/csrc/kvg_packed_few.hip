@@ -314,9 +314,10 @@ __global__ __launch_bounds__(256) void packed_fold_kernel(const PackedAttnArgs a
     fold_tiles<T, D, kPairs>(a, a.part, blockIdx.x - few_workgroups);
 }
 
-// Waves of a workgroup: four take a segment of a launch that leaves CUs idle soonest (one token over 4.6k keys at head_dim 256,
-// 80 workgroups: 19 us; two waves 27), two leave room for more workgroups on a CU, whose starts and ends then
-// overlap (16 tokens over 33k keys: 650 us with four waves, 521 with two).
+// Waves of a workgroup: four take a segment of a launch that leaves CUs idle soonest, two leave room for more
+// workgroups on a CU, whose starts and ends then overlap.  Two against four, us, at workgroups (bf16 unless noted):
+// head_dim 256: 80 27 / 20, 256 31 / 28, fp8 256 26 / 21, 512 45 / 53, 768 74 / 78, fp8 768 35 / 46, 4,224 (16 tokens over
+// 33k keys) 521 / 650; 128: 128 23 / 18, 256 24 / 19, 512 27 / 25, 768 34 / 45, 8,448 528 / 577.
 constexpr unsigned kFewGrid = 256;
 template <typename T, int D>
 void launch_few_d(const PackedAttnArgs& a, hipStream_t stream) {

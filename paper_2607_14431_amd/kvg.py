@@ -446,7 +446,8 @@ def kvg_norm_append(cache: Cache, seqs: Seqs, packed: Packed, rt: kvg_rotary, no
         assert q_out.shape == (n_layers, T, cache.n_q_heads, D) and q_out.dtype is raw and q_out.is_contiguous()
     sk, sv = (_token_stride(t, n_layers, T, Hkv, D, raw) for t in (k_raw, v_raw))
     ns = None if norm is None else norm.struct(cache, n_layers)
-    _on_current_device(cache.k_pool, cache.v_pool, packed.cu_tokens, seqs.block_tables, k_raw, v_raw, q_raw, q_out)
+    _on_current_device(cache.k_pool, cache.v_pool, packed.cu_tokens, seqs.block_tables, seqs.ctx_lens, seqs.start_pos, k_raw,
+                       v_raw, q_raw, q_out, *(() if norm is None else (norm.q_weight, norm.k_weight)))
     _check(_lib.kvg_norm_append(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()),
                                 ctypes.byref(packed.struct(seqs, sq, sk, sv)), ctypes.byref(rt),
                                 None if ns is None else ctypes.byref(ns), layer0, n_layers, _ptr(q_raw), _ptr(k_raw),
@@ -471,7 +472,7 @@ def kvg_packed_attn(cache: Cache, seqs: Seqs, packed: Packed, layer0: int, n_lay
     raw, T, D, Hq = cache.raw_dtype, packed.n_tokens, cache.head_dim, cache.n_q_heads
     sq = _token_stride(q, n_layers, T, Hq, D, raw)
     assert out.shape == (n_layers, T, Hq, D) and out.dtype is raw and out.is_contiguous()
-    _on_current_device(cache.k_pool, cache.v_pool, packed.cu_tokens, seqs.block_tables, q, out, ws)
+    _on_current_device(cache.k_pool, cache.v_pool, packed.cu_tokens, seqs.block_tables, seqs.ctx_lens, q, out, ws)
     _check(_lib.kvg_packed_attn(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()),
                                 ctypes.byref(packed.struct(seqs, sq)), layer0, n_layers, _ptr(q), scale, _ptr(out),
                                 _ptr(ws), ws.nbytes, _stream(stream)), "kvg_packed_attn")

@@ -139,7 +139,7 @@ def test_single_tokens_beside_the_decode_call(kvg):
 @pytest.mark.parametrize("dtype,heads", [("bf16", (16, 8, 256)), ("fp8", (16, 2, 128)), ("bf16", (4, 2, 64)), ("f32", (4, 2, 64))])
 def test_captured_steps(kvg, dtype, heads):
     """A mixed batch's append and attention of two layers, captured; the replays read what the tensors hold then, and a second
-    graph with its own workspace runs between them.  Every replay against the eager call."""
+    graph that shares the workspace runs between them.  Every replay against the eager call."""
     Hq, Hkv, D = heads
     lens, ctxs, pages = [1, 90, 0, 1, 33], [700, 30, 5, 1300, 0], 90
     m = Model(kvg, heads, dtype, 2, (0, 200), 5 * pages)
@@ -152,9 +152,10 @@ def test_captured_steps(kvg, dtype, heads):
              for x in inputs]
     assert not torch.equal(eager[0], eager[1])
     graphs = []
+    ws = kvg.packed_attn_workspace(m.cache, seqs, packed, 1)          # one for both: they never run at once
     for _ in range(2):
         rows, out = inputs[0].clone(), torch.full_like(eager[0], 7.0)
-        q, ws = torch.empty_like(out), kvg.packed_attn_workspace(m.cache, seqs, packed, 1)
+        q = torch.empty_like(out)
         m.run(seqs, packed, rows, out, q, ws)
         torch.cuda.synchronize()
         g = torch.cuda.CUDAGraph()
@@ -221,6 +222,26 @@ def test_rows_do_not_depend_on_the_launch(kvg, dtype, heads, lens, ctxs, window)
     if len(lens) == 1 and window == 0:
         assert small > ws.nbytes, "the one is meant to be split, the other not"
     kvg.kvg_packed_attn(cache, one.seqs, one.packed, 0, L, q.repeat(L, 1, 1, 1), 0.1, out, ws)
+    for l in range(L):
+        assert torch.equal(bits(out[l]), bits(want[0])), l
+
+
+@pytest.mark.parametrize("dtype,heads,lens,ctxs", [
+    ("bf16", (16, 2, 128), [1, 4, 1], [1500, 700, 3]), ("bf16", (4, 2, 256), [1], [1100]), ("fp8", (16, 8, 256), [16, 1], [600, 513]),
+    ("bf16", (4, 2, 64), [2, 1], [1400, 511]), ("fp8", (4, 4, 128), [32, 1], [1000, 1023])])
+@pytest.mark.parametrize("window", [0, 100, 700])
+def test_few_rows_do_not_depend_on_the_launch(kvg, dtype, heads, lens, ctxs, window):
+    """Workgroups of four waves in a small launch, of two in one of many layers: the same bytes for every layer."""
+    L = 80
+    one = Batch(lens, ctxs, heads, dtype, layers=1, windows=(window,), seed=61)
+    q = one.rows(heads[0], 2.0)
+    want = one.attend(q, 0.1)
+    check_attention(one, q, want, 0.1)
+    pools = [p.view(torch.uint8).repeat(L, 1, 1, 1, 1).view(p.dtype) for p in (one.cache.k_pool, one.cache.v_pool)]
+    cache = kvg.Cache(pools[0], pools[1], heads[0], (window,) * L)
+    out = torch.full((L, *want.shape[1:]), 7.0, dtype=want.dtype, device="cuda")
+    kvg.kvg_packed_attn(cache, one.seqs, one.packed, 0, L, q.repeat(L, 1, 1, 1), 0.1, out,
+                        kvg.packed_attn_workspace(cache, one.seqs, one.packed, L))
     for l in range(L):
         assert torch.equal(bits(out[l]), bits(want[0])), l
 
