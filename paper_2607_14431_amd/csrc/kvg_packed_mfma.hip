@@ -17,6 +17,12 @@
 //                  fold by one addition; weights are rounded to bf16 and summed as rounded, so a row of one key
 //                  gives its value exactly and rounding errors of the heavy weights cancel
 //   O^T += V^T P^T A = V^T fragments (ds_read_b64_tr), B = P straight from the S^T registers
+//
+// What bounds it: the matrix cores and the LDS together.  A fragment of 1 KiB takes the LDS 8 cycles and feeds one matrix
+// step of 32, and four waves read at a time: both are busy alike, with the softmax's vector work (at head_dim 128 as many
+// cycles again) and the waits between them.  A prompt of 12,288 tokens (16 / 8 heads x 256, bf16) takes 1,190 us: 1.04 PFLOP/s,
+// matrix cores 48% busy at 2.1 GHz; eight of up to 4,096 (32 / 16 x 128) 475 us: 0.81 PFLOP/s, 37%.  Two blocks of 32 pairs a
+// wave, which halve the fragments, leave one wave a SIMD at head_dim 128 and are slower (12,288 tokens 1,844 us, 1,480).
 #include "kvg_launch.h"
 #include "kvg_packed_mfma.h"
 
@@ -41,8 +47,12 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
   constexpr int ND = D / 32;               // 32-wide blocks of head_dim
   constexpr int BM = 32 * kBlocks * kWaves;
   static_assert(BM == packed_tile_pairs(D), "the host's tiles");
+  // Fragments ahead of their use at D <= 128: a row block's worth where the registers hold it (the others: prompts of up
+  // to 4,096 tokens, 32 / 16 heads x 128: four 598 us, six 579, eight, with spills, 841).
   constexpr int kRing = kSplitKeys || D == 64 ? NS : 6;
-  constexpr bool kSpread = D == 256;       // a tile's loads among the matrix steps, or all at its start
+  // A tile's loads among the matrix steps, or all at its start: 12,288 tokens at head_dim 256 1,306 us / 1,476; 64 236 / 247;
+  // 128 584 / 579.
+  constexpr bool kSpread = D != 128;
   using KR = KRows<RB>;
   using VR = VRows<RB>;
   // a wave brings one page of a tile; the V stages first, where an LDS instruction's immediate offset reaches
@@ -255,7 +265,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
       fresh = false;
     };
     // K fragments of both blocks form one stream read LK ahead of their MFMAs, V^T fragments one read LV ahead, whose first
-    // LV are issued with block 1's scores
+    // LV are issued with block 1's scores (four or six ahead: the same time)
     if constexpr (D <= 128) {
       // Two waves a SIMD: one's softmax runs beside the other's matrix steps.  The tile's K and V^T fragments, in the order of
       // their use, pass through one ring: a fragment's place is refilled with the one LR steps on.
