@@ -19,6 +19,8 @@ otherwise), from the paper's statement of the method:
 * ``attention``  causal grouped-query softmax attention for query rows at given
                  logical indices (fresh-context inference on top of the restored
                  prefix, Sec. 3.2; decode over the restored context, Sec. 4.3).
+* ``packed``     packed sequences: scaled rotary frequencies, norms of query and key heads, rotation, and
+                 attention with the sizes its error bounds need.
 * ``path``       the fresh computation of a workload end to end, whose outputs
                  the graft path must reproduce byte for byte (Eq. 1).
 * ``digest``     SHA-256 content digests of an artifact's leaves, a Merkle root over
