@@ -107,13 +107,20 @@ kvg::PackedSeqs packed_seqs(const kvg_seqs* s, const kvg_packed* p) {
 // fold, us, at workgroups x segments.  bf16 and fp8, head_dim 256: 16 x 3 52 / 31, 40 x 9 116 / 53, 64 x 33 445 / 302,
 // 96 x 34 447 / 453, 104 x 3 46 / 53, 128 x 10 144 / 136, 128 x 34 456 / 571; 128: 64 x 33 334 / 134, 128 x 9 99 / 78,
 // 128 x 33 357 / 294, 160 x 2 33 / 41, 184 x 12 128-134 / 96-122 (with and without windows), 192 x 4 35 / 51, 192 x 9
-// 109 / 110, 192 x 34 363 / 442, 242 x 12 166 / 143, 250 x 4 51 / 60, 314 x 5 65 / 67, 388 x 12 167 / 189; 64: 46 x 13 229 / 55,
-// 126 x 40 756 / 292, 242 x 8 165 / 91.  fp32, more work on fewer rows to a workgroup: 32 x 2 26 / 21, 104 x 3 35 / 32,
+// 109 / 110, 192 x 34 363 / 442, 242 x 12 166 / 143, 250 x 4 51 / 60, 314 x 5 65 / 67, 388 x 12 167 / 189; 64: 54 x 35 271 / 63,
+// 56 x 3 27 / 17, 88 x 13 98 / 49, 176 x 13 103 / 67, 250 x 40 330 / 280, 468 x 8 78 / 70.  fp32, more work on fewer rows to a workgroup: 32 x 2 26 / 21, 104 x 3 35 / 32,
 // 184 x 3 45 / 34, 216 x 2 31 / 34, 256 x 5 73 / 81, 528 x 3 191 / 195.
 bool split_tiles(bool f32, int64_t head_dim, int64_t workgroups, int64_t segs) {
   if (f32) return workgroups < std::min<int64_t>(256, 96 * (segs - 1));
   return workgroups < std::min<int64_t>(256, 48 * (segs - 1)) && workgroups * segs < 576000 / head_dim;
 }
+
+// Whether a split tile launch takes the short sequences too, whose own launch would have `workgroups`: one launch less, and its
+// two stages of keys and values hide more of a small launch's waiting; large ones want the few kernel's smaller
+// workgroups and no empty waves.  Few kernel against tiles, each with its fold, us, at workgroups.  bf16, head_dim 256: 80
+// 26 / 24, 256 33 / 30, 512 52 / 56, 1,024 92 / 132, 8,448 536 / 1,090; 128: 128 23 / 21, 256 24 / 22, 512 31 / 32, 1,024 49 / 59; 64:
+// 64 20 / 17, 256 24 / 17, 512 27 / 23.  fp8, 256: 256 26 / 31, 512 35 / 56; 128: 64 19 / 21, 256 20 / 23.
+bool few_in_tiles(const kvg_cache* c, int64_t workgroups) { return c->dtype == KVG_BF16 && workgroups <= 256; }
 
 // How an attention call runs: rows of the few kernel and tiles at most, each launch's segments (1: not
 // split), and where their partials lie in the workspace.
@@ -130,26 +137,30 @@ AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, i
   AttnPlan r = {0, 0, 1, 1, 0, 0, 0, 0, true};
   if (p->n_tokens == 0 || p->max_len == 0) return r;
   const bool f32 = c->dtype == KVG_F32;
-  const int64_t group = c->n_q_heads / c->n_kv_heads, bm = f32 ? kvg::kF32Pairs : kvg::packed_tile_pairs(c->head_dim);
+  const int64_t group = c->n_q_heads / c->n_kv_heads, bm = f32 ? kvg::kF32Pairs : kvg::kTilePairs;
   const int64_t len = std::min(p->max_len, p->n_tokens);
   const int64_t keys = std::min((int64_t)s->max_ctx_len + p->max_len, (int64_t)s->max_pages * c->page_size);
   const int32_t segs = (int32_t)((keys + kvg::kPackedSeg - 1) / kvg::kPackedSeg);
+  // all sequences in tiles; each sequence's round up
+  const int64_t per_seq = (len * group + bm - 1) / bm;
+  r.n_tiles = std::min(s->batch * per_seq, (p->n_tokens * group + (int64_t)std::min(s->batch, p->n_tokens) * (bm - 1)) / bm);
+  int64_t longest = 0, sum = 0;                                        // segments of a layer's tile, about
+  for (int l = 0; l < n_layers; ++l) {
+    const int64_t W = window != nullptr ? window[l] : 0;
+    const int64_t walk = W > 0 ? std::min<int64_t>(segs, (W + bm / group) / kvg::kPackedSeg + 1) : segs;
+    longest = std::max(longest, walk);
+    sum += walk;
+  }
+  if (split_tiles(f32, c->head_dim, r.n_tiles * c->n_kv_heads * sum / longest, longest)) r.tile_seg = segs;
   // The lengths are the device's.  A single sequence that may be long goes in tiles whatever its length.
-  if (!f32 && (len * group <= kvg::kFewPairs || s->batch > 1)) {
+  if (!f32 && (len * group <= kvg::kFewPairs || s->batch > 1) &&
+      !(r.tile_seg > 1 && few_in_tiles(c, (int64_t)n_layers * segs * s->batch * c->n_kv_heads))) {
     r.few_rows = std::min<int64_t>(p->n_tokens, s->batch * std::min<int64_t>(len, kvg::kFewPairs / group));
     r.few_seg = segs;
-  }
-  if (f32 || len * group > kvg::kFewPairs) {
-    const int64_t per_seq = (len * group + bm - 1) / bm;               // each sequence's tiles round up
-    r.n_tiles = std::min(s->batch * per_seq, (p->n_tokens * group + (int64_t)std::min(s->batch, p->n_tokens) * (bm - 1)) / bm);
-    int64_t longest = 0, sum = 0;                                      // segments of a layer's tile, about
-    for (int l = 0; l < n_layers; ++l) {
-      const int64_t W = window != nullptr ? window[l] : 0;
-      const int64_t walk = W > 0 ? std::min<int64_t>(segs, (W + bm / group) / kvg::kPackedSeg + 1) : segs;
-      longest = std::max(longest, walk);
-      sum += walk;
+    if (len * group <= kvg::kFewPairs) {
+      r.n_tiles = 0;
+      r.tile_seg = 1;
     }
-    if (split_tiles(f32, c->head_dim, r.n_tiles * c->n_kv_heads * sum / longest, longest)) r.tile_seg = segs;
   }
   const int64_t tile_grid = n_layers * r.n_tiles * c->n_kv_heads, fold_grid = (bm / 32) * (c->head_dim / 32);
   r.fits = fits_grid((int64_t)n_layers * r.few_seg * (r.few_rows > 0 ? s->batch : 0) * c->n_kv_heads, 256) &&

@@ -151,7 +151,7 @@ constexpr int kFewPairs = 32;
 __device__ __forceinline__ bool is_few(const PackedAttnArgs& a, const SeqRange& s) {
   return a.few_rows > 0 && (int64_t)s.len * a.group <= kFewPairs;
 }
-constexpr int packed_tile_pairs(int D) { return D == 64 ? 256 : 128; }
+constexpr int kTilePairs = 128;
 inline int64_t packed_tile_workgroups(const PackedAttnArgs& a) { return (int64_t)a.n_layers * a.part.n_seg * a.n_tiles * a.Hkv; }
 inline int64_t packed_few_workgroups(const PackedAttnArgs& a) { return (int64_t)a.n_layers * a.part.n_seg * a.seqs.batch * a.Hkv; }
 hipError_t launch_packed_tiles(const PackedAttnArgs& a, int dtype, hipStream_t stream);

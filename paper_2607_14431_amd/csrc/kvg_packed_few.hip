@@ -362,9 +362,9 @@ hipError_t launch_packed_few(const PackedAttnArgs& a, int dtype, hipStream_t str
 hipError_t launch_packed_fold(const PackedAttnArgs& a, const PackedPartials& few, int dtype, hipStream_t stream) {
   const bool f32 = dtype == kDtypeF32;
   switch (a.D) {
-    case 64: return f32 ? launch_fold_d<float, 64, kF32Pairs>(a, few, stream) : launch_fold_d<__bf16, 64, packed_tile_pairs(64)>(a, few, stream);
-    case 128: return f32 ? launch_fold_d<float, 128, kF32Pairs>(a, few, stream) : launch_fold_d<__bf16, 128, packed_tile_pairs(128)>(a, few, stream);
-    case 256: return f32 ? launch_fold_d<float, 256, kF32Pairs>(a, few, stream) : launch_fold_d<__bf16, 256, packed_tile_pairs(256)>(a, few, stream);
+    case 64: return f32 ? launch_fold_d<float, 64, kF32Pairs>(a, few, stream) : launch_fold_d<__bf16, 64, kTilePairs>(a, few, stream);
+    case 128: return f32 ? launch_fold_d<float, 128, kF32Pairs>(a, few, stream) : launch_fold_d<__bf16, 128, kTilePairs>(a, few, stream);
+    case 256: return f32 ? launch_fold_d<float, 256, kF32Pairs>(a, few, stream) : launch_fold_d<__bf16, 256, kTilePairs>(a, few, stream);
     default: return hipErrorInvalidValue;
   }
 }

@@ -1,7 +1,7 @@
 // Causal attention of packed sequences over a paged bf16 or fp8 cache, on bf16 MFMA (v_mfma_f32_32x32x16_bf16).
 //
 // Workgroup = (layer, KV head g, tile of a sequence): BM (row, query head) pairs of the sequence, heads
-// fastest, kBlocks blocks of 32 pairs per wave.  Keys come in tiles of 64 (absolute multiples of 64 of the
+// fastest, 32 per wave.  Keys come in tiles of 64 (absolute multiples of 64 of the
 // logical index) in two LDS stages, loaded with buffer_load ... lds while the tile before is computed.
 //
 // A row's sums have one order, whatever the launch: keys in blocks of 32, an online softmax over the blocks of a
@@ -22,7 +22,7 @@
 // step of 32, and four waves read at a time: both are busy alike, with the softmax's vector work (at head_dim 128 as many
 // cycles again) and the waits between them.  A prompt of 12,288 tokens (16 / 8 heads x 256, bf16) takes 1,190 us: 1.04 PFLOP/s,
 // matrix cores 48% busy at 2.1 GHz; eight of up to 4,096 (32 / 16 x 128) 475 us: 0.81 PFLOP/s, 37%.  Two blocks of 32 pairs a
-// wave, which halve the fragments, leave one wave a SIMD at head_dim 128 and are slower (12,288 tokens 1,844 us, 1,480).
+// wave, which halve the fragments, are slower (12,288 tokens at head_dim 128, one wave a SIMD then: 1,844 us, 1,480; 64: 236, 170).
 #include "kvg_launch.h"
 #include "kvg_packed_mfma.h"
 
@@ -37,16 +37,15 @@ namespace {
 constexpr int kTileKeys = 64;
 constexpr int kSegTiles = kPackedSeg / kTileKeys;
 constexpr int kWaves = 4;
-// T: cache storage (uint16_t bf16, uint8_t fp8 E4M3).  kBlocks: blocks of 32 pairs per wave.
-// kSplit: a workgroup takes one segment and leaves its partial.
-template <typename T, int D, int kBlocks, bool kSplitKeys>
+// T: cache storage (uint16_t bf16, uint8_t fp8 E4M3).  kSplitKeys: a workgroup takes one segment and leaves its partial.
+template <typename T, int D, bool kSplitKeys>
 __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_kernel(const PackedAttnArgs a) {
   constexpr bool kFp8 = sizeof(T) == 1;
   constexpr int RB = D * (int)sizeof(T);   // bytes per cache row
   constexpr int NS = D / 16;               // MFMA steps over head_dim
   constexpr int ND = D / 32;               // 32-wide blocks of head_dim
-  constexpr int BM = 32 * kBlocks * kWaves;
-  static_assert(BM == packed_tile_pairs(D), "the host's tiles");
+  constexpr int BM = kTilePairs;
+  static_assert(BM == 32 * kWaves, "a block of 32 pairs per wave");
   // Fragments ahead of their use at D <= 128: a row block's worth where the registers hold it (the others: prompts of up
   // to 4,096 tokens, 32 / 16 heads x 128: four 598 us, six 579, eight, with spills, 841).
   constexpr int kRing = kSplitKeys || D == 64 ? NS : 6;
@@ -90,19 +89,13 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
   const int tile_id = u.count - 1 - u.at;
   const int ctx = sq.ctx, len = sq.len;
 
-  const int pair0 = tile_id * BM + wave * (32 * kBlocks);   // this wave's first pair
-  int row_n[kBlocks], row_lo[kBlocks];                      // this lane's rows' visible keys [row_lo, row_n]
-  bool row_ok[kBlocks];
+  const int pair0 = tile_id * BM + wave * 32;   // this wave's first pair
   const int W = layer_window(a, l);
-#pragma unroll
-  for (int rb = 0; rb < kBlocks; ++rb) {
-    const int row = (pair0 + 32 * rb + lrow) >> lg;
-    row_ok[rb] = row < len;
-    row_n[rb] = ctx + row;
-    row_lo[rb] = window_start(W, ctx + row + 1);
-  }
+  const int row = (pair0 + lrow) >> lg;
+  const bool row_ok = row < len;
+  const int row_n = ctx + row, row_lo = window_start(W, row_n + 1);      // this lane's row's visible keys [row_lo, row_n]
   const int first_row = pair0 >> lg;
-  const int last_row = min((pair0 + 32 * kBlocks - 1) >> lg, len - 1);
+  const int last_row = min((pair0 + 31) >> lg, len - 1);
   const bool idle = first_row >= len;                       // a wave without rows
   const int wave_first = ctx + first_row, wave_last = idle ? -1 : ctx + last_row;
   const int tile_first = ctx + ((tile_id * BM) >> lg);       // the workgroup's first row, and the first key all of its rows see
@@ -145,27 +138,20 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
   };
 
   // ---- queries (B operand of S^T), zeros past the rows
-  uint4 qf[kBlocks][NS];
+  uint4 qf[NS];
+  {
+    const int64_t tok = (int64_t)l * a.seqs.n_tokens + sq.row0 + (row_ok ? row : 0);
+    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + tok * a.q_stride + (int64_t)(g * a.group + ((pair0 + lrow) & (a.group - 1))) * D;
 #pragma unroll
-  for (int rb = 0; rb < kBlocks; ++rb) {
-    const int p = pair0 + 32 * rb + lrow;
-    const int64_t tok = (int64_t)l * a.seqs.n_tokens + sq.row0 + (row_ok[rb] ? p >> lg : 0);
-    const uint16_t* qp = static_cast<const uint16_t*>(a.q) + tok * a.q_stride + (int64_t)(g * a.group + (p & (a.group - 1))) * D;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) qf[rb][s] = row_ok[rb] ? ld16(qp + (2 * s + half) * 8) : make_uint4(0, 0, 0, 0);
+    for (int s = 0; s < NS; ++s) qf[s] = row_ok ? ld16(qp + (2 * s + half) * 8) : make_uint4(0, 0, 0, 0);
   }
 
-  f32x16 o[kBlocks][ND], o_run[kSplitKeys ? 1 : kBlocks][ND];
-  float m[kBlocks], lsum[kBlocks], m_run[kBlocks], l_run[kBlocks];
+  f32x16 o[ND], o_run[kSplitKeys ? 1 : ND];
+  float m = -INFINITY, lsum = 0.0f, m_run = -INFINITY, l_run = 0.0f;
 #pragma unroll
-  for (int rb = 0; rb < kBlocks; ++rb) {
-    m[rb] = m_run[rb] = -INFINITY;
-    lsum[rb] = l_run[rb] = 0.0f;
-#pragma unroll
-    for (int d = 0; d < ND; ++d) {
-      o[rb][d] = splat(0.0f);
-      if constexpr (!kSplitKeys) o_run[rb][d] = splat(0.0f);
-    }
+  for (int d = 0; d < ND; ++d) {
+    o[d] = splat(0.0f);
+    if constexpr (!kSplitKeys) o_run[d] = splat(0.0f);
   }
 
   const int k_lane = k_lane_base<RB, kFp8>(lane), v_lane = v_lane_base<RB, kFp8>(lane);
@@ -206,62 +192,54 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
     auto kread = [&](int f) { return k_fragment<RB, kFp8>(kbase + KR::at(32 * (f / NS), 0), f % NS); };        // f = block * NS + step
     auto vread = [&](int t) { return v_fragment<RB, kFp8>(vbase + VR::at(16 * (t / ND), 0), t % ND); };        // t = 16-key step * ND + d
 
-    f32x16 s[2][kBlocks];
-    if constexpr (D > 128) {
-#pragma unroll
-      for (int rb = 0; rb < kBlocks; ++rb) s[0][rb] = s[1][rb] = splat(0.0f);
-    }
+    f32x16 s[2];
+    if constexpr (D > 128) s[0] = s[1] = splat(0.0f);
     const bool need_mask = key0 + kTileKeys - 1 > wave_first || key0 < mask_lo;
     auto mask_block = [&](int kb) {
       if (need_mask) {
+        const int at = D <= 128 ? 0 : kb;
 #pragma unroll
-        for (int rb = 0; rb < kBlocks; ++rb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            // key - row_lo as unsigned: keys below the window wrap round
-            const uint32_t key = key0 + kb * 32 + half * 4 - row_lo[rb] + (r >> 2) * 8 + (r & 3);
-            const int at = D <= 128 ? 0 : kb;
-            s[at][rb][r] = key <= (uint32_t)(row_n[rb] - row_lo[rb]) ? s[at][rb][r] : -INFINITY;
-          }
+        for (int r = 0; r < 16; ++r) {
+          // key - row_lo as unsigned: keys below the window wrap round
+          const uint32_t key = key0 + kb * 32 + half * 4 - row_lo + (r >> 2) * 8 + (r & 3);
+          s[at][r] = key <= (uint32_t)(row_n - row_lo) ? s[at][r] : -INFINITY;
+        }
       }
     };
-    // softmax of one block of one row block in 16 pieces, to sit beside the matrix steps of another phase: 0-3 the largest
+    // softmax of one block in 16 pieces, to sit beside the matrix steps of another phase: 0-3 the largest
     // score, 4 the reference, 5-12 two exponentials each, 13-14 rounding of eight weights and their sum, 15 the sum
-    uint4 pf[2][kBlocks][2];
-    struct SoftState {
+    uint4 pf[2][2];
+    struct {
       float mx, alpha, m_ref, psum;
       bool raised;
-    } st[kBlocks];
-    auto soft_piece = [&](int kb, int rb, int j) {
-      SoftState& x = st[rb];
+    } x;
+    auto soft_piece = [&](int kb, int j) {
       if (j < 4) {
         if (j == 0) x.mx = -INFINITY;
 #pragma unroll
-        for (int r = 4 * j; r < 4 * j + 4; ++r) x.mx = fmaxf(x.mx, s[kb][rb][r]);
+        for (int r = 4 * j; r < 4 * j + 4; ++r) x.mx = fmaxf(x.mx, s[kb][r]);
       } else if (j == 4) {
         const float2 mh = halves32(x.mx);
-        x.alpha = raise_reference(m[rb], fmaxf(mh.x, mh.y) * a.scale_log2, x.raised);
-        x.m_ref = m[rb] == -INFINITY ? 0.0f : m[rb];      // no key seen yet: every weight is 0
+        x.alpha = raise_reference(m, fmaxf(mh.x, mh.y) * a.scale_log2, x.raised);
+        x.m_ref = m == -INFINITY ? 0.0f : m;      // no key seen yet: every weight is 0
         x.psum = 0.0f;
       } else if (j < 13) {
 #pragma unroll
         for (int r = 2 * (j - 5); r < 2 * (j - 5) + 2; ++r)
-          s[kb][rb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][rb][r], a.scale_log2, -x.m_ref));
+          s[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, -x.m_ref));
       } else if (j < 15) {
-        pf[kb][rb][j - 13] = round_weights(s[kb][rb], j - 13, x.psum);
+        pf[kb][j - 13] = round_weights(s[kb], j - 13, x.psum);
       } else {
         const float2 ph = halves32(x.psum);
-        lsum[rb] = fmaf(lsum[rb], x.alpha, ph.x + ph.y);
+        lsum = fmaf(lsum, x.alpha, ph.x + ph.y);
       }
     };
     // O of a segment's first block is still 0
     auto rescale_o = [&]() {
+      if (!fresh && __builtin_amdgcn_ballot_w64(x.raised) != 0) {
 #pragma unroll
-      for (int rb = 0; rb < kBlocks; ++rb)
-        if (!fresh && __builtin_amdgcn_ballot_w64(st[rb].raised) != 0) {
-#pragma unroll
-          for (int d = 0; d < ND; ++d) o[rb][d] *= st[rb].alpha;
-        }
+        for (int d = 0; d < ND; ++d) o[d] *= x.alpha;
+      }
       fresh = false;
     };
     // K fragments of both blocks form one stream read LK ahead of their MFMAs, V^T fragments one read LV ahead, whose first
@@ -282,23 +260,19 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
 #pragma unroll
         for (int ss = 0; ss < NS; ++ss) {
           const int t = 2 * kb * NS + ss;
-#pragma unroll
-          for (int rb = 0; rb < kBlocks; ++rb) s[0][rb] = mfma32(ring[t % LR], qf[rb][ss], ss ? s[0][rb] : splat(0.0f));
+          s[0] = mfma32(ring[t % LR], qf[ss], ss ? s[0] : splat(0.0f));
           fetch(t + LR);
           issue_step(kb * NS + ss);
           __builtin_amdgcn_sched_barrier(0);
         }
         mask_block(kb);
 #pragma unroll
-        for (int rb = 0; rb < kBlocks; ++rb)
-#pragma unroll
-          for (int j = 0; j < 16; ++j) soft_piece(0, rb, j);
+        for (int j = 0; j < 16; ++j) soft_piece(0, j);
         rescale_o();
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
           const int t = (2 * kb + 1) * NS + i;
-#pragma unroll
-          for (int rb = 0; rb < kBlocks; ++rb) o[rb][i % ND] = mfma32(ring[t % LR], pf[0][rb][i / ND], o[rb][i % ND]);
+          o[i % ND] = mfma32(ring[t % LR], pf[0][i / ND], o[i % ND]);
           fetch(t + LR);
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -325,13 +299,12 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
       kfetch(ss + LK);
       issue_step(ss);
       __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int rb = 0; rb < kBlocks; ++rb) s[0][rb] = mfma32(kf[ss % RK], qf[rb][ss], s[0][rb]);
+      s[0] = mfma32(kf[ss % RK], qf[ss], s[0]);
       __builtin_amdgcn_sched_barrier(0);
     }
     mask_block(0);
     // phase B: scores of block 1 beside the softmax of block 0
-    constexpr int kPieces = 16 * kBlocks;
+    constexpr int kPieces = 16;
     static_assert(D <= 128 || LV <= NS, "first V^T fragments");
 #pragma unroll
     for (int ss = 0; ss < NS; ++ss) {
@@ -339,10 +312,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
       kfetch(f + LK);
       issue_step(NS + ss);
       if (ss >= NS - LV) vfetch(ss - (NS - LV));
+      s[1] = mfma32(kf[f % RK], qf[ss], s[1]);
 #pragma unroll
-      for (int rb = 0; rb < kBlocks; ++rb) s[1][rb] = mfma32(kf[f % RK], qf[rb][ss], s[1][rb]);
-#pragma unroll
-      for (int j = ss * kPieces / NS; j < (ss + 1) * kPieces / NS; ++j) soft_piece(0, j % kBlocks, j / kBlocks);
+      for (int j = ss * kPieces / NS; j < (ss + 1) * kPieces / NS; ++j) soft_piece(0, j);
       __builtin_amdgcn_sched_barrier(0);
     }
     rescale_o();
@@ -351,10 +323,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
 #pragma unroll
     for (int t = 0; t < 2 * ND; ++t) {
       vfetch(t + LV);
+      o[t % ND] = mfma32(vf[t % RV], pf[0][t / ND], o[t % ND]);
 #pragma unroll
-      for (int rb = 0; rb < kBlocks; ++rb) o[rb][t % ND] = mfma32(vf[t % RV], pf[0][rb][t / ND], o[rb][t % ND]);
-#pragma unroll
-      for (int j = t * kPieces / (2 * ND); j < (t + 1) * kPieces / (2 * ND); ++j) soft_piece(1, j % kBlocks, j / kBlocks);
+      for (int j = t * kPieces / (2 * ND); j < (t + 1) * kPieces / (2 * ND); ++j) soft_piece(1, j);
       __builtin_amdgcn_sched_barrier(0);
     }
     rescale_o();
@@ -362,29 +333,25 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
     for (int t = 2 * ND; t < NT; ++t) {
       vfetch(t + LV);
       __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int rb = 0; rb < kBlocks; ++rb) o[rb][t % ND] = mfma32(vf[t % RV], pf[1][rb][t / ND - 2], o[rb][t % ND]);
+      o[t % ND] = mfma32(vf[t % RV], pf[1][t / ND - 2], o[t % ND]);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   // end of a segment: its state folded into the running one, which packed_fold_kernel does with the same operations
   auto fold = [&]() {
     if constexpr (!kSplitKeys) {
+      const FoldFactors f = fold_factors(m_run, l_run, m, lsum);
+      if (__builtin_amdgcn_ballot_w64(f.run != 1.0f || f.part != 1.0f) == 0) {
 #pragma unroll
-      for (int rb = 0; rb < kBlocks; ++rb) {
-        const FoldFactors f = fold_factors(m_run[rb], l_run[rb], m[rb], lsum[rb]);
-        if (__builtin_amdgcn_ballot_w64(f.run != 1.0f || f.part != 1.0f) == 0) {
+        for (int d = 0; d < ND; ++d) o_run[d] += o[d];
+      } else {
 #pragma unroll
-          for (int d = 0; d < ND; ++d) o_run[rb][d] += o[rb][d];
-        } else {
-#pragma unroll
-          for (int d = 0; d < ND; ++d) o_run[rb][d] = __builtin_elementwise_fma(o[rb][d], splat(f.part), o_run[rb][d] * f.run);
-        }
-        m[rb] = -INFINITY;
-        lsum[rb] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < ND; ++d) o[rb][d] = splat(0.0f);
+        for (int d = 0; d < ND; ++d) o_run[d] = __builtin_elementwise_fma(o[d], splat(f.part), o_run[d] * f.run);
       }
+      m = -INFINITY;
+      lsum = 0.0f;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] = splat(0.0f);
       fresh = true;
     }
   };
@@ -398,51 +365,49 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);     // the empty loads past the last tile write LDS: none may outlive the workgroup
 
-  // where a pair's results go: its block's partial, or its row of the output
-  auto block_of = [&](int rb) { return part_block(a, a.part.n_seg, l, slot, g, kWaves * kBlocks, wave * kBlocks + rb, seg); };
+  // where a pair's results go: the wave's block of the partials, or its row of the output
+  const int64_t block = part_block(a, a.part.n_seg, l, slot, g, kWaves, wave, seg);
   auto row_of = [&](int p) -> int64_t {
     const int64_t tok = (int64_t)l * a.seqs.n_tokens + sq.row0 + (p >> lg);
     return tok * a.Hq + g * a.group + (p & (a.group - 1));
   };
-  if constexpr (!kSplitKeys) fold();
-#pragma unroll
-  for (int rb = 0; rb < kBlocks; ++rb) {
-    if constexpr (kSplitKeys) {
-      if (idle) break;
-      const int64_t block = block_of(rb);
+  if constexpr (kSplitKeys) {
+    if (!idle) {
       float* op = a.part.acc + block * (32 * D) + lane * 4;
 #pragma unroll
       for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4)
           *reinterpret_cast<float4*>(op + (d * 4 + r4) * 256) =
-              make_float4(o[rb][d][r4 * 4], o[rb][d][r4 * 4 + 1], o[rb][d][r4 * 4 + 2], o[rb][d][r4 * 4 + 3]);
-      if (half == 0) *reinterpret_cast<float2*>(a.part.ml + (block * 32 + lrow) * 2) = make_float2(m[rb], lsum[rb]);
-    } else {
-      if (!row_ok[rb]) continue;
-      const float inv = 1.0f / l_run[rb];
-      uint16_t* op = static_cast<uint16_t*>(a.out) + row_of(pair0 + 32 * rb + lrow) * D;
+              make_float4(o[d][r4 * 4], o[d][r4 * 4 + 1], o[d][r4 * 4 + 2], o[d][r4 * 4 + 3]);
+      if (half == 0) *reinterpret_cast<float2*>(a.part.ml + (block * 32 + lrow) * 2) = make_float2(m, lsum);
+    }
+  } else {
+    fold();
+    if (row_ok) {
+      const float inv = 1.0f / l_run;
+      uint16_t* op = static_cast<uint16_t*>(a.out) + row_of(pair0 + lrow) * D;
 #pragma unroll
       for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4)
           *reinterpret_cast<uint2*>(op + d * 32 + r4 * 8 + half * 4) =
-              make_uint2(pack_bf16_rne(o_run[rb][d][r4 * 4] * inv, o_run[rb][d][r4 * 4 + 1] * inv),
-                         pack_bf16_rne(o_run[rb][d][r4 * 4 + 2] * inv, o_run[rb][d][r4 * 4 + 3] * inv));
+              make_uint2(pack_bf16_rne(o_run[d][r4 * 4] * inv, o_run[d][r4 * 4 + 1] * inv),
+                         pack_bf16_rne(o_run[d][r4 * 4 + 2] * inv, o_run[d][r4 * 4 + 3] * inv));
     }
   }
   // ---- the values that are not finite, to the rows that see them
   __syncthreads();
   if (s_bad != 0 && !idle) {
     __builtin_amdgcn_s_waitcnt(0x0F70);
-    const int pairs = min(32 * kBlocks, (len << lg) - pair0);
+    const int pairs = min(32, (len << lg) - pair0);
     for (int kt = kt_begin; kt < n_tiles; ++kt) {
       const int key0 = kt * kTileKeys;
       if (!(min(key0 + kTileKeys, n_hi) - 1 > tile_first || key0 < tile_mask_lo)) continue;
       put_bad_values(a, vpool, bt, g, max(key0, wave_lo), min(key0 + kTileKeys, wave_last + 1), 1, W, ctx, lg, pair0, pairs,
                      [&](int p, int x, float v) {
                        if constexpr (kSplitKeys)
-                         a.part.acc[block_of(p >> 5) * (32 * D) + part_at(p & 31, x)] = v;
+                         a.part.acc[block * (32 * D) + part_at(p, x)] = v;
                        else
                          static_cast<uint16_t*>(a.out)[row_of(pair0 + p) * D + x] = (uint16_t)(__float_as_uint(v) >> 16);
                      });
@@ -450,22 +415,22 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
   }
 }
 
-template <typename T, int D, int kBlocks>
+template <typename T, int D>
 hipError_t launch_d(const PackedAttnArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)packed_tile_workgroups(a));
   if (a.part.n_seg > 1)
-    packed_tiles_kernel<T, D, kBlocks, true><<<grid, 64 * kWaves, 0, stream>>>(a);
+    packed_tiles_kernel<T, D, true><<<grid, 64 * kWaves, 0, stream>>>(a);
   else
-    packed_tiles_kernel<T, D, kBlocks, false><<<grid, 64 * kWaves, 0, stream>>>(a);
+    packed_tiles_kernel<T, D, false><<<grid, 64 * kWaves, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_t(const PackedAttnArgs& a, hipStream_t stream) {
   switch (a.D) {
-    case 64: return launch_d<T, 64, 2>(a, stream);
-    case 128: return launch_d<T, 128, 1>(a, stream);
-    case 256: return launch_d<T, 256, 1>(a, stream);
+    case 64: return launch_d<T, 64>(a, stream);
+    case 128: return launch_d<T, 128>(a, stream);
+    case 256: return launch_d<T, 256>(a, stream);
     default: return hipErrorInvalidValue;
   }
 }
