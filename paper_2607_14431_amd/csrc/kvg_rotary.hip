@@ -7,10 +7,10 @@
 // and half swaps, no LDS).  A vector whose pairs lie in another one (half pairing) reads that one too, from L1; a lane
 // keeps its place in the head, and with it its weights, from head to head.
 //
-// What bounds them: HBM in large calls, where each raw value is read and each result written once (those prompts 5.3 TB/s, a
-// 4,096-token block of 48 heads x 128 rotated at 5.9); the round trips in small ones (metadata, then angles; the first
+// What bounds them: HBM in large calls, where each raw value is read and each result written once (eight prompts up to 4,096 tokens 4.8 to 5.3 TB/s, a
+// 4,096-token block of 48 heads x 128 rotated at 6.0); the round trips in small ones (metadata, then angles; the first
 // rows are requested before either: 16 single tokens of 16 + 2 x 8 heads x 256 5.1 us, one token's 24 heads rotated in 3.0).
-// Four tokens a workgroup, whose tables fill all lanes, are no faster (fp8 suffixes, 6 layers x 1,063 tokens: 45 us, 41), nor
+// Four tokens a workgroup, whose tables fill all lanes, are no faster (fp8, 1,063 tokens x 6 layers: 45 us, then 41), nor
 // more wavefronts with spills (157 us for the prompts with six a SIMD).
 #include "kvg_launch.h"
 #include "kvg_mfma.h"
@@ -23,7 +23,9 @@ namespace kvg {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int64_t kSmallGrid = 1024;       // workgroups below which a token's heads are spread over several (16 tokens: 8.8 -> 5.1 us)
+// Workgroups below which a token's heads are spread over several: not at all, up to 256, up to 1,024 workgroups: 16 tokens 8.8, 5.1,
+// 5.2 us, 8 layers of them -, 6.8, 6.0; 300 tokens of 48 heads rotated -, 4.6, 4.0.
+constexpr int64_t kSmallGrid = 1024;
 
 // Results are written past the caches (8 prompts up to 4,096 tokens, 32 + 2 x 16 heads x 128: 134 us with plain stores, 90);
 // raw rows are read with plain loads, because a vector is read twice (nontemporal: 121).
@@ -286,8 +288,9 @@ template <typename T, int D>
 hipError_t launch_norm_append_d(NormAppendArgs a, hipStream_t stream) {
   constexpr int RS = kThreads / (D / Elem<typename RawOf<T>::type>::kPerVec);
   const int rows = (a.q_raw != nullptr ? a.Hq : 0) + 2 * a.Hkv;
-  // layers per workgroup: enough workgroups to fill the chip, fewer sincos recomputations
-  const int64_t per = ((int64_t)a.n_layers * a.seqs.n_tokens + 8191) / 8192;
+  // Layers per workgroup, which share its angles, as long as there are 4,096 workgroups.  One layer each / 4,096 / 2,048
+  // workgroups, us: fp8, 1,063 tokens x 6 layers 41.7 / 39.6 / 37.8, x 24 188 / 163 / 179; 14,472 tokens x 4 491 / 414 / 407.
+  const int64_t per = ((int64_t)a.n_layers * a.seqs.n_tokens + 4095) / 4096;
   a.layers_per_block = (int)(per < 1 ? 1 : per > a.n_layers ? a.n_layers : per);
   if (a.layers_per_block < (a.n_layers + 65534) / 65535) a.layers_per_block = (a.n_layers + 65534) / 65535;
   const unsigned layer_groups = (a.n_layers + a.layers_per_block - 1) / a.layers_per_block;
