@@ -1,17 +1,18 @@
 // Rotary positions of packed rows, alone (kvg_rotate) and with the heads' norms and the append to the
 // paged cache (kvg_norm_append).
 //
-// A workgroup takes a token (in a small call a part of its heads, in a large one several layers).  Angles pos * theta_i, their cosines and sines
-// are taken in fp64 once per token and kept in LDS as fp32; then every 16-byte vector of the tokens' heads is a lane's
-// work: a head is D / E consecutive lanes (E values a vector), which sum its squares among themselves for the norm (DPP
-// and half swaps, no LDS).  A vector whose pairs lie in another one (half pairing) reads that one too, from L1; a lane
+// A workgroup takes a token (in a small call a part of its heads, in a large one several layers).  Angles pos * theta_i,
+// their cosines and sines are taken in fp64 once per token and kept in LDS as fp32; then every 16-byte vector of the
+// token's heads is a lane's work: a head is D / E consecutive lanes (E values a vector), which sum its squares among
+// themselves for the norm (DPP and half swaps) and give each other the partners of half pairing (ds_bpermute).  A lane
 // keeps its place in the head, and with it its weights, from head to head.
 //
-// What bounds them: HBM in large calls, where each raw value is read and each result written once (eight prompts up to 4,096 tokens 4.8 to 5.3 TB/s, a
-// 4,096-token block of 48 heads x 128 rotated at 6.0); the round trips in small ones (metadata, then angles; the first
-// rows are requested before either: 16 single tokens of 16 + 2 x 8 heads x 256 5.1 us, one token's 24 heads rotated in 3.0).
-// Four tokens a workgroup, whose tables fill all lanes, are no faster (fp8, 1,063 tokens x 6 layers: 45 us, then 41), nor
-// more wavefronts with spills (157 us for the prompts with six a SIMD).
+// What bounds them: HBM in large calls, where each raw value is read and each result written once (eight prompts up to 4,096
+// tokens, 32 + 2 x 16 heads x 128: 78 us, 6.1 TB/s; a 4,096-token block of 48 heads x 128 rotated: 17 us, 6.0); the round
+// trips in small ones (metadata, then angles; the first rows are requested before either: 16 single tokens of 16 + 2 x 8
+// heads x 256 5 to 6 us, one token's 24 heads rotated in 3.0).  Partners read from memory cost their second load and the registers
+// of two waves a SIMD (those prompts 89 us; fp8, 1,063 tokens x 6 layers 40, then 34).  Four tokens a workgroup, whose tables fill all
+// lanes, were no faster (45 us, then 41), nor more wavefronts with spills (seven a SIMD: 81 us for the prompts, 37; eight: 140, 52).
 #include "kvg_launch.h"
 #include "kvg_mfma.h"
 #include "kvg_packed.h"
@@ -27,8 +28,8 @@ constexpr int kThreads = 256;
 // 5.2 us, 8 layers of them -, 6.8, 6.0; 300 tokens of 48 heads rotated -, 4.6, 4.0.
 constexpr int64_t kSmallGrid = 1024;
 
-// Results are written past the caches (8 prompts up to 4,096 tokens, 32 + 2 x 16 heads x 128: 134 us with plain stores, 90);
-// raw rows are read with plain loads, because a vector is read twice (nontemporal: 121).
+// Results are written past the caches (those prompts 134 us with plain stores, 90, with partners from memory), raw rows are read
+// through them: a projection has just written them (nontemporal 95 us, 78 when the last-level cache holds some of them).
 __device__ __forceinline__ void st16s(void* p, const uint4& v) {
   __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(p));
 }
@@ -55,6 +56,14 @@ __device__ __forceinline__ Place place(const RotaryArgs& r, int e0) {
   p.partner = !p.rotated || r.pairing != 0 ? e0 : p.first ? e0 + half : e0 - half;
   p.pair = r.pairing != 0 ? e0 >> 1 : p.first ? e0 : p.partner;
   return p;
+}
+
+// y: the values of this lane's partners (half pairing), from the lane of the head that holds them in x
+template <int E>
+__device__ __forceinline__ void from_partner(const Place& p, int e0, const float (&x)[E], float (&y)[E]) {
+  const int from = 4 * ((int)(threadIdx.x & 63) + (p.partner - e0) / E);
+#pragma unroll
+  for (int e = 0; e < E; ++e) y[e] = __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)__float_as_uint(x[e])));
 }
 
 // x: the vector's values, y: its partners' (half pairing); the operations of rotate_pair()
@@ -133,12 +142,9 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   R* y = reinterpret_cast<R*>(a.y) + tok * a.y_stride;
   int h = blockIdx.y * RS * a.steps + threadIdx.x / VECS;
   const int h_end = min(a.n_heads, (int)(blockIdx.y + 1) * RS * a.steps);
-  uint4 own = make_uint4(0, 0, 0, 0), other = own;
+  uint4 own = make_uint4(0, 0, 0, 0);
   auto load = [&](int head) {
-    if (head < h_end) {
-      own = ld16(x + (int64_t)head * D + e0);
-      other = ld16(x + (int64_t)head * D + p.partner);
-    }
+    if (head < h_end) own = ld16(x + (int64_t)head * D + e0);
   };
   load(h);                                           // before the angles, which wait for the position
   const int64_t pos = a.positions[tok];
@@ -147,10 +153,10 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateArgs a) {
   // a head's lanes are in one wave, so a row rotated in place is read whole before it is written
   for (; h < h_end; h += RS) {
     float v[E], w[E];
-    unpack<R>(own, v);
-    unpack<R>(other, w);
     const uint4 raw = own;
     load(h + RS);
+    unpack<R>(raw, v);
+    if (a.rot.pairing == 0) from_partner<E>(p, e0, v, w);
     rotate_values(p, a.rot.pairing, cs, v, w);
     if (p.rotated)
       store_values<R>(y + (int64_t)h * D + e0, v);
@@ -174,7 +180,7 @@ __global__ __launch_bounds__(kThreads) void norm_append_kernel(const NormAppendA
   const int r_begin = blockIdx.z * RS * a.steps + threadIdx.x / VECS, r_end = min(rows, (int)(blockIdx.z + 1) * RS * a.steps);
 
   // row r of the token: its queries, then its keys, then its values
-  uint4 own = make_uint4(0, 0, 0, 0), other = own;
+  uint4 own = make_uint4(0, 0, 0, 0);
   auto load = [&](int l, int r) {
     if (r >= r_end) return;
     const int64_t at = (int64_t)l * a.seqs.n_tokens + tok;
@@ -182,7 +188,6 @@ __global__ __launch_bounds__(kThreads) void norm_append_kernel(const NormAppendA
                  : r < n_q + a.Hkv ? reinterpret_cast<const R*>(a.k_raw) + at * a.k_stride + (int64_t)(r - n_q) * D
                                    : reinterpret_cast<const R*>(a.v_raw) + at * a.v_stride + (int64_t)(r - n_q - a.Hkv) * D;
     own = ld16(s + e0);
-    other = ld16(s + (r < n_q + a.Hkv ? p.partner : e0));
   };
   load(l_begin, r_begin);                            // before the sequence and the angles are known
 
@@ -197,23 +202,17 @@ __global__ __launch_bounds__(kThreads) void norm_append_kernel(const NormAppendA
   __syncthreads();
 
   for (int l = l_begin; l < l_end; ++l) {
-    // this lane's weights and its partners', 1 / 0 where there is no norm
+    // this lane's weights
     const R* wq = reinterpret_cast<const R*>(a.q_weight) + (int64_t)l * D;
     const R* wk = reinterpret_cast<const R*>(a.k_weight) + (int64_t)l * D;
-    uint4 wq_own, wq_other, wk_own, wk_other;
-    if (a.q_weight != nullptr) {
-      wq_own = ld16(wq + e0);
-      wq_other = ld16(wq + p.partner);
-    }
-    if (a.k_weight != nullptr) {
-      wk_own = ld16(wk + e0);
-      wk_other = ld16(wk + p.partner);
-    }
+    uint4 wq_own, wk_own;
+    if (a.q_weight != nullptr) wq_own = ld16(wq + e0);
+    if (a.k_weight != nullptr) wk_own = ld16(wk + e0);
     T* kpool = reinterpret_cast<T*>(a.k_pool) + (int64_t)(a.layer0 + l) * a.layer_elems;
     T* vpool = reinterpret_cast<T*>(a.v_pool) + (int64_t)(a.layer0 + l) * a.layer_elems;
 #pragma unroll 1
     for (int r = r_begin; r < r_end; r += RS) {
-      const uint4 raw = own, raw_other = other;
+      const uint4 raw = own;
       if (r + RS < r_end)
         load(l, r + RS);
       else if (l + 1 < l_end)
@@ -233,21 +232,17 @@ __global__ __launch_bounds__(kThreads) void norm_append_kernel(const NormAppendA
       const bool is_q = r < n_q;
       float x[E], y[E];
       unpack<R>(raw, x);
-      unpack<R>(raw_other, y);
       if ((is_q ? a.q_weight : a.k_weight) != nullptr) {
         float sum = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) sum = fmaf(x[e], x[e], sum);
         const float inv = 1.0f / sqrtf(sum_lanes<VECS>(sum) * (1.0f / D) + a.eps);
-        float wx[E], wy[E];
+        float wx[E];
         unpack<R>(is_q ? wq_own : wk_own, wx);
-        unpack<R>(is_q ? wq_other : wk_other, wy);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          x[e] = x[e] * inv * (wx[e] + a.weight_offset);
-          y[e] = y[e] * inv * (wy[e] + a.weight_offset);
-        }
+        for (int e = 0; e < E; ++e) x[e] = x[e] * inv * (wx[e] + a.weight_offset);
       }
+      if (a.rot.pairing == 0) from_partner<E>(p, e0, x, y);
       rotate_values(p, a.rot.pairing, cs, x, y);
       if (is_q) {
         store_values<R>(reinterpret_cast<R*>(a.q_out) + (((int64_t)l * a.seqs.n_tokens + tok) * a.Hq + r) * D + e0, x);
