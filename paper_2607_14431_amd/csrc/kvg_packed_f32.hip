@@ -292,12 +292,11 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_f32_kernel(const Packed
   if (s_bad != 0) {
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __syncthreads();
-    put_bad_values(a, vpool, bt, g, max(seg_begin * kPackedSeg, tile_lo) + wave, min(seg_end * kPackedSeg, tile_hi), kWaves, W, sq.ctx, lg,
-                   pair0, pairs, [&](int p, int x, float v) {
-                     if constexpr (kSplitKeys)
-                       a.part.acc[block * (32 * D) + part_at(p, x)] = v;
-                     else
-                       static_cast<float*>(a.out)[row_of(p) * D + x] = v;
+    if (wave != 0) return;
+    put_bad_values(a, vpool, bt, g, max(seg_begin * kPackedSeg, tile_lo), min(seg_end * kPackedSeg, tile_hi), W, sq.ctx, lg, pair0, pairs,
+                   [&](int p, int x, float v) {
+                     float* to = kSplitKeys ? a.part.acc + block * (32 * D) + part_at(p, x) : static_cast<float*>(a.out) + row_of(p) * D + x;
+                     *to = take_in(*to, v);
                    });
   }
 }

@@ -213,12 +213,15 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
   if (s_bad != 0) {                                  // the values that are not finite, to the rows that see them
     __builtin_amdgcn_s_waitcnt(vm_wait(0));
     __syncthreads();
-    put_bad_values(a, vpool, bt, g, k_begin + wave, k_end, kWaves, W, sq.ctx, lg, 0, n_pairs, [&](int p, int x, float v) {
+    if (wave != 0) return;
+    put_bad_values(a, vpool, bt, g, k_begin, k_end, W, sq.ctx, lg, 0, n_pairs, [&](int p, int x, float v) {
       const int64_t at = slot_of(p) * D + x;
-      if (a.part.n_seg > 1)
-        a.part.acc[at] = v;
-      else
-        static_cast<uint16_t*>(a.out)[at] = (uint16_t)(__float_as_uint(v) >> 16);
+      if (a.part.n_seg > 1) {
+        a.part.acc[at] = take_in(a.part.acc[at], v);
+      } else {
+        uint16_t* to = static_cast<uint16_t*>(a.out) + at;
+        *to = (uint16_t)(__float_as_uint(take_in(bf16_bits_to_f32(*to), v)) >> 16);
+      }
     });
   }
 }

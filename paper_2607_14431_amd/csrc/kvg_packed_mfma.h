@@ -161,12 +161,16 @@ __device__ __forceinline__ uint4 round_weights(const f32x16& p, int h, float& ps
   }
   return f;
 }
-// The values of keys key0, key0 + step, .. (below key1) that are not finite, to those of the pairs [pair0, pair0 + pairs) of a
-// sequence that see them: put(pair - pair0, dimension, value), a dimension per lane.  For the keys a kernel has left out.
+// A result that takes in a value that is not finite: Inf and Inf of the other sign give NaN, NaN stays.
+__device__ __forceinline__ float take_in(float sum, float v) { return fabsf(sum) < INFINITY ? v : sum + v; }
+
+// The values of keys [key0, key1) that are not finite, to those of the pairs [pair0, pair0 + pairs) of a sequence that see them:
+// put(pair - pair0, dimension, value), a dimension per lane, the keys in ascending order.  For the keys a kernel has left out; by
+// one wave, so that the order is always the same.
 template <typename T, typename Put>
-__device__ __forceinline__ void put_bad_values(const PackedAttnArgs& a, const T* vpool, const int32_t* table, int g, int key0, int key1, int step,
+__device__ __forceinline__ void put_bad_values(const PackedAttnArgs& a, const T* vpool, const int32_t* table, int g, int key0, int key1,
                                             int W, int ctx, int lg, int pair0, int pairs, Put put) {
-  for (int key = key0; key < key1; key += step) {
+  for (int key = key0; key < key1; ++key) {
     const int32_t page = table[key / kPage];
     const T* vr = vpool + (((int64_t)(page >= 0 && page < a.n_pages ? page : 0) * a.Hkv + g) * kPage + key % kPage) * a.D;
     for (int x = __lane_id(); x < a.D; x += 64) {

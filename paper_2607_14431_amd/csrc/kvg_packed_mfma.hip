@@ -404,12 +404,15 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
     for (int kt = kt_begin; kt < n_tiles; ++kt) {
       const int key0 = kt * kTileKeys;
       if (!(min(key0 + kTileKeys, n_hi) - 1 > tile_first || key0 < tile_mask_lo)) continue;
-      put_bad_values(a, vpool, bt, g, max(key0, wave_lo), min(key0 + kTileKeys, wave_last + 1), 1, W, ctx, lg, pair0, pairs,
+      put_bad_values(a, vpool, bt, g, max(key0, wave_lo), min(key0 + kTileKeys, wave_last + 1), W, ctx, lg, pair0, pairs,
                      [&](int p, int x, float v) {
-                       if constexpr (kSplitKeys)
-                         a.part.acc[block * (32 * D) + part_at(p, x)] = v;
-                       else
-                         static_cast<uint16_t*>(a.out)[row_of(pair0 + p) * D + x] = (uint16_t)(__float_as_uint(v) >> 16);
+                       if constexpr (kSplitKeys) {
+                         float* to = a.part.acc + block * (32 * D) + part_at(p, x);
+                         *to = take_in(*to, v);
+                       } else {
+                         uint16_t* to = static_cast<uint16_t*>(a.out) + row_of(pair0 + p) * D + x;
+                         *to = (uint16_t)(__float_as_uint(take_in(bf16_bits_to_f32(*to), v)) >> 16);
+                       }
                      });
     }
   }

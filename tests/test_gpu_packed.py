@@ -330,6 +330,38 @@ def test_inf_and_nan_stay_with_the_rows_that_see_them(dtype, bad, heads):
                 assert not hit.isfinite().any()
 
 
+@pytest.mark.parametrize("dtype,heads,lens,ctxs", [
+    ("bf16", (4, 2, 64), [40, 3], [0, 20]), ("bf16", (2, 1, 256), [6, 60], [30, 0]), ("f32", (4, 2, 128), [50], [3]),
+    ("bf16", (16, 8, 128), [1] * 40, [20] * 40), ("bf16", (8, 2, 128), [200], [500])])
+def test_infinities_of_both_signs(dtype, heads, lens, ctxs):
+    """In one dimension a value is +Inf, two tokens later another -Inf: rows that see the first alone are +Inf there, rows that
+    see both are NaN, the same in every call.  Single tokens go in either kernel, by the batch."""
+    b = Batch(lens, ctxs, heads, dtype, seed=20)
+    q = b.rows(heads[0], 1.0)
+    scale = 0.5 / math.sqrt(heads[2])
+    want = b.attend(q, scale)
+    for s, (n, c) in enumerate(zip(lens, ctxs)):
+        first = c + n // 3                                       # some rows see neither
+        for t, v in ((first, math.inf), (first + 2, -math.inf)):
+            if t < c + n:
+                b.cache.v_pool[0, int(b.table[s, t // 16]), :, t % 16, 7] = v
+    got = b.attend(q, scale)
+    for s, (n, c) in enumerate(zip(lens, ctxs)):
+        first = c + n // 3
+        for i in range(n):
+            row, old = got[0, int(b.cu[s]) + i].clone(), want[0, int(b.cu[s]) + i]
+            if c + i >= first + 2:
+                assert row[:, 7].isnan().all(), (s, i)
+            elif c + i >= first:
+                assert (row[:, 7] == math.inf).all(), (s, i)
+            else:
+                assert torch.equal(row[:, 7], old[:, 7]), (s, i)
+            row[:, 7] = old[:, 7]
+            assert torch.equal(row, old), (s, i)
+    for _ in range(3):
+        assert torch.equal(bits(b.attend(q, scale)), bits(got))
+
+
 def test_attention_skips_bad_metadata():
     for what in ("ctx", "negative", "cu", "order", "page"):
         b = Batch([4, 50, 6, 70], [0, 16, 3, 600], (4, 2, 64), "bf16", seed=18)
