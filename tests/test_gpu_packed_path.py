@@ -362,3 +362,57 @@ def test_workspace_covers_any_layers(kvg):
             kvg.kvg_packed_attn(b.cache, b.seqs, b.packed, l0, n, q[l0:l0 + n], 0.1, out, ws)
             rows = torch.from_numpy(np.concatenate([np.arange(b.cu[s], b.cu[s + 1]) for s in range(3)]).astype(np.int64)).cuda()
             assert torch.equal(bits(out[:, rows]), bits(want[l0:l0 + n][:, rows])), (n, l0)
+
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", (8, 4, 128)), ("fp8", (4, 2, 256)), ("f32", (4, 2, 64))])
+def test_a_graph_replays_with_other_lengths(kvg, dtype, heads):
+    """The lengths are the device's: a graph captured for its bounds serves every batch within them."""
+    Hq, Hkv, D = heads
+    B, rows_max, max_len, max_ctx, pages = 4, 140, 100, 1400, 95
+    m = Model(kvg, heads, dtype, 1, None, B * pages)
+    for pool in (m.cache.k_pool, m.cache.v_pool):
+        pool.copy_(torch.randn(pool.shape, device="cuda"))
+    table = torch.randperm(B * pages, device="cuda").to(torch.int32).view(B, pages)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    cu, ctx, start = torch.zeros(B + 1, **i32), torch.zeros(B, **i32), torch.zeros(B, dtype=torch.int64, device="cuda")
+    seqs, packed = kvg.Seqs(table, ctx, start, max_ctx), kvg.Packed(cu, rows_max, max_len)
+    rows = token_rows(m, list(range(rows_max)), 9)
+    out, q = (torch.full((1, rows_max, Hq, D), 7.0, dtype=rows.dtype, device="cuda") for _ in range(2))
+    ws = kvg.packed_attn_workspace(m.cache, seqs, packed, 1)
+    m.run(seqs, packed, rows, out, q, ws)                        # nothing to do: all lengths are 0
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all()) and bool((q == 7.0).all())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        m.run(seqs, packed, rows, out, q, ws)
+    for lens, ctxs, st in (([1, 1, 1, 1], [1400, 3, 0, 700], [0, 5, 9, 2]), ([100, 0, 33, 7], [0, 9, 1300, 511], [1, 1, 1, 1]),
+                           ([0, 0, 0, 1], [0, 0, 0, 0], [0, 0, 0, 3]), ([40, 60, 1, 39], [1000, 1400, 64, 0], [7, 0, 0, 0])):
+        cu.copy_(torch.from_numpy(np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)))
+        ctx.copy_(torch.tensor(ctxs, dtype=torch.int32))
+        start.copy_(torch.tensor(st))
+        want, wq = torch.full_like(out, 7.0), torch.full_like(q, 7.0)
+        m.run(seqs, packed, rows, want, wq)
+        for _ in range(2):
+            out.fill_(7.0)
+            q.fill_(7.0)
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(bits(out), bits(want)) and torch.equal(bits(q), bits(wq)), lens
+        assert bool((out[:, sum(lens):] == 7.0).all()) and out[:, :sum(lens)].float().isfinite().all()
+    del g
+
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", (8, 4, 128)), ("bf16", (16, 2, 64)), ("fp8", (4, 2, 256)), ("f32", (4, 2, 64))])
+def test_a_query_that_is_not_finite_keeps_to_its_row(dtype, heads):
+    b = Batch([70, 3, 1], [600, 40, 1000], heads, dtype, seed=95)
+    q = b.rows(heads[0], 2.0)
+    want = b.attend(q, 0.1)
+    bad = [(0, 1, 3), (69, 0, 0), (71, heads[0] - 1, 5), (73, 2, 7)]
+    for t, h, x in bad:
+        q[0, t, h, x] = float("nan") if t % 2 else float("inf")
+    got = b.attend(q, 0.1)
+    for t, h, _ in bad:
+        assert got[0, t, h].isnan().all(), (t, h)
+        got[0, t, h] = want[0, t, h]
+    assert torch.equal(bits(got), bits(want))
