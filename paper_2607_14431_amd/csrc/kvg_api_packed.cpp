@@ -101,18 +101,20 @@ kvg::PackedSeqs packed_seqs(const kvg_seqs* s, const kvg_packed* p) {
   return {p->cu_tokens, s->ctx_lens, s->block_tables, s->batch, p->n_tokens, p->max_len, s->max_ctx_len, s->max_pages};
 }
 
-// A tile launch is split over segments when its workgroups (in units of the longest walk, `segs` segments) are few beside
-// the chip and beside the segments: splitting shortens the walk, but every (row, segment) leaves D sums that are written
-// and read again, cheaply only while the last-level cache holds them.  Measured, unsplit against split with its
-// fold, us, at workgroups x segments.  bf16 and fp8, head_dim 256: 16 x 3 52 / 31, 40 x 9 116 / 53, 64 x 33 445 / 302,
-// 96 x 34 447 / 453, 104 x 3 46 / 53, 128 x 10 144 / 136, 128 x 34 456 / 571; 128: 64 x 33 334 / 134, 128 x 9 99 / 78,
-// 128 x 33 357 / 294, 160 x 2 33 / 41, 184 x 12 128-134 / 96-122 (with and without windows), 192 x 4 35 / 51, 192 x 9
-// 109 / 110, 192 x 34 363 / 442, 242 x 12 166 / 143, 250 x 4 51 / 60, 314 x 5 65 / 67, 388 x 12 167 / 189; 64: 54 x 35 271 / 63,
-// 56 x 3 27 / 17, 88 x 13 98 / 49, 176 x 13 103 / 67, 250 x 40 330 / 280, 468 x 8 78 / 70.  fp32, more work on fewer rows to a workgroup: 32 x 2 26 / 21, 104 x 3 35 / 32,
-// 184 x 3 45 / 34, 216 x 2 31 / 34, 256 x 5 73 / 81, 528 x 3 191 / 195.
+// A tile launch is split over segments when its workgroups (in units of the longest walk, `segs` segments) are few
+// beside the chip and beside the segments: splitting shortens the walk, but every (row, segment) leaves D sums that are
+// written and read again, more cheaply while the last-level cache holds them.  Measured, unsplit against split with its
+// fold, us, at workgroups x segments.  bf16 and fp8, head_dim 256: 16 x 3 52 / 31, 40 x 9 116 / 53, 56 x 65 (fp8) 1,370
+// / 493, 40 x 65 832 / 411, 64 x 33 445 / 302, 96 x 34 447 / 453, 104 x 3 46 / 53, 128 x 10 144 / 136, 128 x 34 456 /
+// 571; 128: 64 x 33 334 / 134, 128 x 9 99 / 78, 128 x 33 357 / 294, 160 x 2 33 / 41, 184 x 12 128-134 / 96-122 (with
+// and without windows), 192 x 4 35 / 51, 192 x 9 109 / 110, 192 x 34 363 / 442, 242 x 12 166 / 143, 250 x 4 51 / 60,
+// 314 x 5 65 / 67, 388 x 12 167 / 189; 64: 54 x 35 271 / 63, 56 x 3 27 / 17, 88 x 13 98 / 49, 176 x 13 103 / 67, 250 x
+// 40 330 / 280, 468 x 8 78 / 70.  fp32, more work on fewer rows to a workgroup: 32 x 2 26 / 21, 104 x 3 35 / 32, 184 x
+// 3 45 / 34, 216 x 2 31 / 34, 256 x 5 73 / 81, 528 x 3 191 / 195.
 bool split_tiles(bool f32, int64_t head_dim, int64_t workgroups, int64_t segs) {
   if (f32) return workgroups < std::min<int64_t>(256, 96 * (segs - 1));
-  return workgroups < std::min<int64_t>(256, 48 * (segs - 1)) && workgroups * segs < 576000 / head_dim;
+  const bool cached = workgroups * segs * head_dim < 576000;           // partials of about 290 MB
+  return workgroups < std::min<int64_t>({256, 48 * (segs - 1), (cached ? 32768 : 22528) / head_dim});
 }
 
 // Whether a split tile launch takes the short sequences too, whose own launch would have `workgroups`: one launch less, and its
