@@ -118,7 +118,7 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
     asm volatile("" ::: "memory");
     f32x16 s = splat(0.0f);
 #pragma unroll
-    for (int ss = 0; ss < NS; ++ss) s = mfma32(k_fragment<RB, kFp8>(kbase, ss), qf[ss], s);
+    for (int ss = 0; ss < NS; ++ss) s = mfma32(widen(k_fragment<RB, kFp8>(kbase, ss)), qf[ss], s);
     __builtin_amdgcn_s_waitcnt(kLgkmWait);           // read: the buffer takes the next unit's
     asm volatile("" ::: "memory");
     issue(KR{}, kpool, s_k, u + 1);
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int d = 0; d < NDW; ++d)
-          o[d] = mfma32(v_fragment<RB, kFp8>(vbase + (2 * w + ks) * VR::kPageBytes, d), ks ? p1 : p0, o[d]);
+          o[d] = mfma32(widen(v_fragment<RB, kFp8>(vbase + (2 * w + ks) * VR::kPageBytes, d)), ks ? p1 : p0, o[d]);
     }
     __syncthreads();                                 // V, weights and sums are read: the next unit's may come
     issue(VR{}, vpool, s_v, u + 1);

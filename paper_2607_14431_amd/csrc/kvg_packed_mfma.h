@@ -8,6 +8,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace kvg {
 
 namespace {
@@ -99,22 +101,29 @@ __device__ __forceinline__ f32x16 mfma32(const uint4& x, const uint4& y, const f
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(x), as_bf16x8(y), c, 0, 0, 0);
 }
 
-// K fragment of step ss (32 rows x 16 dims; eight values of head_dim for each lane's row, fp8 widened) at the lane's base.
+// A fragment as it is read, eight values a lane.  fp8 is widened where it is used: a conversion beside the read would wait
+// for it.
+template <bool kFp8>
+using Fragment = typename std::conditional<kFp8, uint2, uint4>::type;
+__device__ __forceinline__ uint4 widen(const uint4& x) { return x; }
+__device__ __forceinline__ uint4 widen(const uint2& x) { return widen_fp8x8(x.x, x.y); }
+
+// K fragment of step ss (32 rows x 16 dims; eight values of head_dim for each lane's row) at the lane's base.
 template <int RB, bool kFp8>
-__device__ __forceinline__ uint4 k_fragment(const lds_char* lane_base, int ss) {
+__device__ __forceinline__ Fragment<kFp8> k_fragment(const lds_char* lane_base, int ss) {
   if constexpr (kFp8) {
     const u32x2 w = *reinterpret_cast<const lds_u32x2*>(lane_base + KRows<RB>::at(0, ss));
-    return widen_fp8x8(w.x, w.y);
+    return make_uint2(w.x, w.y);
   } else {
     return __builtin_bit_cast(uint4, *reinterpret_cast<const lds_u32x4*>(lane_base + KRows<RB>::at(0, 2 * ss)));
   }
 }
 // V^T fragment of 16 rows, dims 32 d .. 32 d + 31.
 template <int RB, bool kFp8>
-__device__ __forceinline__ uint4 v_fragment(const lds_char* lane_base, int d) {
+__device__ __forceinline__ Fragment<kFp8> v_fragment(const lds_char* lane_base, int d) {
   if constexpr (kFp8) {
     const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(lane_base + VRows<RB>::at(0, 2 * d)));
-    return widen_fp8x8((uint32_t)w.x, (uint32_t)w.y);
+    return make_uint2((uint32_t)w.x, (uint32_t)w.y);
   } else {
     const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lane_base + VRows<RB>::at(0, 4 * d)));
     const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lane_base + VRows<RB>::at(8, 4 * d)));
