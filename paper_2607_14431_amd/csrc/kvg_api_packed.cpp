@@ -121,8 +121,11 @@ bool split_tiles(bool f32, int64_t head_dim, int64_t workgroups, int64_t segs) {
 // two stages of keys and values hide more of a small launch's waiting; large ones want the few kernel's smaller
 // workgroups and no empty waves.  Few kernel against tiles, each with its fold, us, at workgroups.  bf16, head_dim 256: 80
 // 26 / 24, 256 33 / 30, 512 52 / 56, 1,024 92 / 132, 8,448 536 / 1,090; 128: 128 23 / 21, 256 24 / 22, 512 31 / 32, 1,024 49 / 59; 64:
-// 64 20 / 17, 256 24 / 17, 512 27 / 23.  fp8, 256: 256 26 / 31, 512 35 / 56; 128: 64 19 / 21, 256 20 / 23.
-bool few_in_tiles(const kvg_cache* c, int64_t workgroups) { return c->dtype == KVG_BF16 && workgroups <= 256; }
+// 64 20 / 17, 256 24 / 17, 512 27 / 23.  fp8, 256: 64 21 / 24, 128 23 / 25, 256 26 / 27, 512 35 / 49; 128: 64 17 / 18, 256 29 / 23;
+// 64: 16 19 / 16, 32 18 / 15.
+bool few_in_tiles(const kvg_cache* c, int64_t workgroups) {
+  return workgroups <= 256 && (c->dtype == KVG_BF16 || c->head_dim <= 128);
+}
 
 // How an attention call runs: rows of the few kernel and tiles at most, each launch's segments (1: not
 // split), and where their partials lie in the workspace.
