@@ -137,7 +137,7 @@ struct AttnPlan {
   size_t total() const { return std::max(few_ml + few_acc + tile_ml + tile_acc, kAlign); }
 };
 
-// window: the layers' windows, or null.
+// window: the n_layers layers' windows, or null.
 AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packed* p, int32_t n_layers, const int32_t* window) {
   AttnPlan r = {0, 0, 1, 1, 0, 0, 0, 0, true};
   if (p->n_tokens == 0 || p->max_len == 0) return r;
@@ -316,7 +316,9 @@ int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_pack
                          &a.q_stride)) != KVG_OK)
     return st;
   if ((st = fill_windows(cache, layer0, n_layers, a.window)) != KVG_OK) return st;
-  const AttnPlan plan = attn_plan(cache, seqs, packed, n_layers, a.window);
+  // the caller's array, as the size query reads it: a launch carries kMaxWindowLayers windows, a call without any may
+  // have more layers
+  const AttnPlan plan = attn_plan(cache, seqs, packed, n_layers, cache->layer_window != nullptr ? cache->layer_window + layer0 : nullptr);
   if (!plan.fits || !fits_grid(packed->n_tokens, 256)) return KVG_E_SHAPE;
   if (ws == nullptr || ws_bytes < plan.total()) return KVG_E_WORKSPACE;
   if (packed->n_tokens == 0 || packed->max_len == 0) return KVG_OK;
