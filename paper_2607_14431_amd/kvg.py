@@ -427,6 +427,8 @@ def kvg_rotate(rt: kvg_rotary, positions: torch.Tensor, x: torch.Tensor, y: torc
         raise ValueError("kvg_rotate: x and y alike, heads dense")
     if T <= 1:
         sx = sy = 0
+    elif sx < H * D or sy < H * D:         # a broadcast row among them: 0 is the library's word for dense rows
+        raise ValueError("kvg_rotate: a token's rows overlap the next one's")
     assert positions.dtype is torch.int64 and positions.is_contiguous() and positions.numel() == T
     _on_current_device(positions, x, y)
     _check(_lib.kvg_rotate(ctypes.byref(rt), 1 if dtype is torch.bfloat16 else 0, D, T, H, positions.data_ptr(), x.data_ptr(), sx,

@@ -47,3 +47,17 @@ def test_plan_of_many_layers_is_the_size_querys(layers, heads, tokens, ctx, zero
     for _ in range(3):
         assert call(size) == ALIGN
         assert call(size - 1) == WORKSPACE
+
+
+def test_rotate_refuses_rows_that_overlap():
+    """A row broadcast over tokens has stride 0, which the library takes for dense rows: refused, as rows that overlap."""
+    torch = pytest.importorskip("torch")
+    pos = torch.zeros(5, dtype=torch.int64)
+    dense = torch.zeros(5, 2, 64, dtype=torch.bfloat16)
+    broadcast = torch.zeros(1, 2, 64, dtype=torch.bfloat16).expand(5, 2, 64)
+    sliding = torch.zeros(6 * 64, dtype=torch.bfloat16).as_strided((5, 2, 64), (64, 64, 1))
+    one_head = torch.zeros(1, 1, 64).expand(5, 1, 64)
+    for x, y in ((broadcast, dense), (dense, broadcast), (broadcast, broadcast), (sliding, dense), (dense, sliding),
+                 (one_head, torch.zeros(5, 1, 64))):
+        with pytest.raises(ValueError, match="overlap"):
+            kvg.kvg_rotate(kvg.rotary(), pos, x, y)
