@@ -178,7 +178,8 @@ class Cache:
         shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
         if windows is not None:
             windows = tuple(int(x) for x in windows)
-            assert len(windows) == n_layers
+            if len(windows) != n_layers:
+                raise ValueError("windows: one per layer")
         return Cache(torch.empty(shape, dtype=dtype, device=device),
                      torch.empty(shape, dtype=dtype, device=device), n_q_heads, windows)
 
@@ -215,8 +216,8 @@ class Cache:
     def struct(self) -> kvg_cache:
         k, v = self.k_pool, self.v_pool
         shape, dtype = k.shape, k.dtype
-        assert k.is_contiguous() and v.is_contiguous()
-        assert shape == v.shape and dtype == v.dtype
+        if not (k.is_contiguous() and v.is_contiguous() and shape == v.shape and dtype == v.dtype):
+            raise ValueError("pools: contiguous, of one shape and type")
         n_layers, n_pages, n_kv_heads, page_size, head_dim = shape
         c = kvg_cache(n_layers, self.n_q_heads, n_kv_heads, head_dim, page_size, _DTYPE_CODE[dtype], n_pages,
                       k.data_ptr(), v.data_ptr(), None)
@@ -240,8 +241,9 @@ class Seqs:
     def struct(self) -> kvg_seqs:
         bt, ctx, pos = self.block_tables, self.ctx_lens, self.start_pos
         shape = bt.shape
-        assert bt.dtype is torch.int32 and bt.is_contiguous() and len(shape) == 2
-        assert ctx.dtype is torch.int32 and pos.dtype is torch.int64
+        if not (bt.dtype is torch.int32 and bt.is_contiguous() and len(shape) == 2 and ctx.dtype is torch.int32 and
+                pos.dtype is torch.int64):
+            raise ValueError("block_tables: int32 [batch][max_pages], contiguous; ctx_lens: int32; start_pos: int64")
         return kvg_seqs(shape[0], shape[1], self.max_ctx_len, self.shared_tokens, bt.data_ptr(), ctx.data_ptr(),
                         pos.data_ptr())
 
@@ -283,7 +285,8 @@ def kvg_artifact_verify(hdr: kvg_artifact_hdr, payload, ws: torch.Tensor, stream
 def _raw_ok(cache: Cache, *raws):
     dtype = cache.raw_dtype
     for t in raws:
-        assert t.dtype is dtype and t.is_contiguous(), "raw inputs: the cache's raw dtype, contiguous"
+        if t.dtype is not dtype or not t.is_contiguous():
+            raise ValueError("raw inputs: the cache's raw dtype, contiguous")
 
 
 def kvg_append(cache: Cache, seqs: Seqs, rp: kvg_rope, layer0: int, n_layers: int, chunk_len: int,
@@ -295,14 +298,16 @@ def kvg_append(cache: Cache, seqs: Seqs, rp: kvg_rope, layer0: int, n_layers: in
 
 def kvg_deposit(cache: Cache, block_table_row: torch.Tensor, first_token: int, n_tokens: int,
                 payload: torch.Tensor, stream=None):
-    assert payload.nbytes >= kvg_payload_bytes(cache, n_tokens)
+    if payload.nbytes < kvg_payload_bytes(cache, n_tokens):
+        raise ValueError("payload: kvg_payload_bytes(cache, n_tokens) bytes")
     _check(_lib.kvg_deposit(ctypes.byref(cache.struct()), _ptr(block_table_row), block_table_row.numel(),
                             first_token, n_tokens, _ptr(payload), _stream(stream)), "kvg_deposit")
 
 
 def kvg_graft(cache: Cache, hdr: kvg_artifact_hdr, payload: torch.Tensor, block_table_row: torch.Tensor,
               first_token: int, target_pos: int, flags: int = 0, stream=None):
-    assert payload.nbytes >= hdr.payload_bytes
+    if payload.nbytes < hdr.payload_bytes:
+        raise ValueError("payload: the header's payload_bytes")
     _check(_lib.kvg_graft(ctypes.byref(cache.struct()), ctypes.byref(hdr), _ptr(payload), _ptr(block_table_row),
                           block_table_row.numel(), first_token, target_pos, flags, _stream(stream)), "kvg_graft")
 
@@ -368,8 +373,8 @@ class HeadNorm:
     def struct(self, cache: Cache, n_layers: int) -> kvg_head_norm:
         dtype, n = cache.raw_dtype, n_layers * cache.head_dim
         for w in (self.q_weight, self.k_weight):
-            assert w is None or (w.dtype is dtype and w.is_contiguous() and w.numel() == n), \
-                "norm weights: [n_layers][head_dim] of the cache's raw dtype, contiguous"
+            if w is not None and not (w.dtype is dtype and w.is_contiguous() and w.numel() == n):
+                raise ValueError("norm weights: [n_layers][head_dim] of the cache's raw dtype, contiguous")
         return kvg_head_norm(_ptr(self.q_weight), _ptr(self.k_weight), self.eps, self.weight_offset)
 
 
@@ -383,7 +388,8 @@ class Packed:
 
     def struct(self, seqs: Seqs, q_stride: int = 0, k_stride: int = 0, v_stride: int = 0) -> kvg_packed:
         cu = self.cu_tokens
-        assert cu.dtype is torch.int32 and cu.is_contiguous() and cu.numel() == seqs.block_tables.shape[0] + 1
+        if not (cu.dtype is torch.int32 and cu.is_contiguous() and cu.numel() == seqs.block_tables.shape[0] + 1):
+            raise ValueError("cu_tokens: int32 [batch + 1], contiguous")
         return kvg_packed(self.n_tokens, self.max_len, cu.data_ptr(), q_stride, k_stride, v_stride)
 
 
@@ -429,7 +435,8 @@ def kvg_rotate(rt: kvg_rotary, positions: torch.Tensor, x: torch.Tensor, y: torc
         sx = sy = 0
     elif sx < H * D or sy < H * D:         # a broadcast row among them: 0 is the library's word for dense rows
         raise ValueError("kvg_rotate: a token's rows overlap the next one's")
-    assert positions.dtype is torch.int64 and positions.is_contiguous() and positions.numel() == T
+    if not (positions.dtype is torch.int64 and positions.is_contiguous() and positions.numel() == T):
+        raise ValueError("positions: int64 [n_tokens], contiguous")
     _on_current_device(positions, x, y)
     _check(_lib.kvg_rotate(ctypes.byref(rt), 1 if dtype is torch.bfloat16 else 0, D, T, H, positions.data_ptr(), x.data_ptr(), sx,
                            y.data_ptr(), sy, _stream(stream)), "kvg_rotate")
@@ -445,7 +452,8 @@ def kvg_norm_append(cache: Cache, seqs: Seqs, packed: Packed, rt: kvg_rotary, no
     if q_raw is not None:
         sq = _token_stride(q_raw, n_layers, T, cache.n_q_heads, D, raw)
     if q_out is not None:
-        assert q_out.shape == (n_layers, T, cache.n_q_heads, D) and q_out.dtype is raw and q_out.is_contiguous()
+        if not (q_out.shape == (n_layers, T, cache.n_q_heads, D) and q_out.dtype is raw and q_out.is_contiguous()):
+            raise ValueError("q_out: [n_layers][n_tokens][n_q_heads][head_dim] of the raw dtype, contiguous")
     sk, sv = (_token_stride(t, n_layers, T, Hkv, D, raw) for t in (k_raw, v_raw))
     ns = None if norm is None else norm.struct(cache, n_layers)
     _on_current_device(cache.k_pool, cache.v_pool, packed.cu_tokens, seqs.block_tables, seqs.ctx_lens, seqs.start_pos, k_raw,
@@ -473,7 +481,8 @@ def kvg_packed_attn(cache: Cache, seqs: Seqs, packed: Packed, layer0: int, n_lay
     rotated, any token stride; out: the same, dense."""
     raw, T, D, Hq = cache.raw_dtype, packed.n_tokens, cache.head_dim, cache.n_q_heads
     sq = _token_stride(q, n_layers, T, Hq, D, raw)
-    assert out.shape == (n_layers, T, Hq, D) and out.dtype is raw and out.is_contiguous()
+    if not (out.shape == (n_layers, T, Hq, D) and out.dtype is raw and out.is_contiguous()):
+        raise ValueError("out: [n_layers][n_tokens][n_q_heads][head_dim] of the raw dtype, contiguous")
     _on_current_device(cache.k_pool, cache.v_pool, packed.cu_tokens, seqs.block_tables, seqs.ctx_lens, q, out, ws)
     _check(_lib.kvg_packed_attn(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()),
                                 ctypes.byref(packed.struct(seqs, sq)), layer0, n_layers, _ptr(q), scale, _ptr(out),
@@ -513,8 +522,8 @@ def kvg_logits_packed_bytes(vocab: int, hidden: int) -> int:
 def kvg_logits_pack(w: torch.Tensor, packed: torch.Tensor, stream=None):
     """w: bf16 [V][H] row-major; packed: kvg_logits_packed_bytes(V, H) bytes (device)."""
     V, H = w.shape
-    assert w.dtype == torch.bfloat16 and w.is_contiguous()
-    assert packed.nbytes >= kvg_logits_packed_bytes(V, H)
+    if not (w.dtype == torch.bfloat16 and w.is_contiguous() and packed.nbytes >= kvg_logits_packed_bytes(V, H)):
+        raise ValueError("w: bf16, contiguous; packed: kvg_logits_packed_bytes(V, H) bytes")
     _check(_lib.kvg_logits_pack(_ptr(w), V, H, _ptr(packed), _stream(stream)), "kvg_logits_pack")
 
 
@@ -526,9 +535,10 @@ def kvg_logits(hidden: torch.Tensor, w_packed: torch.Tensor, vocab: int, cap: fl
                ws: torch.Tensor, stream=None):
     """hidden: fp32 [rows][H]; w_packed: as kvg_logits_pack left it; out: fp32 [rows][vocab]."""
     rows, H = hidden.shape
-    assert tuple(out.shape) == (rows, vocab) and w_packed.nbytes >= kvg_logits_packed_bytes(vocab, H)
-    assert hidden.dtype == torch.float32 and out.dtype == torch.float32
-    assert hidden.is_contiguous() and w_packed.is_contiguous() and out.is_contiguous()
+    if not (tuple(out.shape) == (rows, vocab) and w_packed.nbytes >= kvg_logits_packed_bytes(vocab, H) and
+            hidden.dtype == torch.float32 and out.dtype == torch.float32 and
+            hidden.is_contiguous() and w_packed.is_contiguous() and out.is_contiguous()):
+        raise ValueError("hidden: fp32 [rows][H]; w_packed: kvg_logits_packed_bytes(vocab, H) bytes; out: fp32 [rows][vocab]; contiguous")
     _check(_lib.kvg_logits(_ptr(hidden), rows, H, _ptr(w_packed), vocab, cap, _ptr(out), _ptr(ws), ws.nbytes,
                            _stream(stream)), "kvg_logits")
 
@@ -537,10 +547,11 @@ def kvg_logit_compare(a: torch.Tensor, b: torch.Tensor, kl: torch.Tensor, argmax
                       argmax_b: torch.Tensor, stream=None):
     """a, b: fp32 [rows][V]; kl: fp64 [rows]; argmax_a, argmax_b: int32 [rows] (all device)."""
     rows, V = a.shape
-    assert tuple(b.shape) == (rows, V) and a.dtype == b.dtype == torch.float32
-    assert a.is_contiguous() and b.is_contiguous()
-    assert kl.dtype == torch.float64 and argmax_a.dtype == argmax_b.dtype == torch.int32
-    assert kl.numel() >= rows and argmax_a.numel() >= rows and argmax_b.numel() >= rows
+    if not (tuple(b.shape) == (rows, V) and a.dtype == b.dtype == torch.float32 and a.is_contiguous() and b.is_contiguous()):
+        raise ValueError("a, b: fp32 [rows][V], contiguous")
+    if not (kl.dtype == torch.float64 and argmax_a.dtype == argmax_b.dtype == torch.int32 and
+            kl.numel() >= rows and argmax_a.numel() >= rows and argmax_b.numel() >= rows):
+        raise ValueError("kl: fp64 [rows]; argmax_a, argmax_b: int32 [rows]")
     _check(_lib.kvg_logit_compare(_ptr(a), _ptr(b), rows, V, _ptr(kl), _ptr(argmax_a), _ptr(argmax_b),
                                   _stream(stream)), "kvg_logit_compare")
 

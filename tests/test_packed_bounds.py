@@ -61,3 +61,68 @@ def test_rotate_refuses_rows_that_overlap():
                  (one_head, torch.zeros(5, 1, 64))):
         with pytest.raises(ValueError, match="overlap"):
             kvg.kvg_rotate(kvg.rotary(), pos, x, y)
+
+
+OPTIMISED = '''
+import sys
+import torch
+from paper_2607_14431_amd import kvg
+assert False, "this must be compiled away"
+bf16 = torch.bfloat16
+z = lambda *s, dtype=bf16: torch.zeros(s, dtype=dtype)
+cache = kvg.Cache(z(1, 4, 2, 16, 64), z(1, 4, 2, 16, 64), 4)
+i32 = lambda *s: z(*s, dtype=torch.int32)
+seqs = kvg.Seqs(i32(2, 2), i32(2), z(2, dtype=torch.int64), 8)
+packed = kvg.Packed(i32(3), 5, 4)
+q, k, ws = z(1, 5, 4, 64), z(1, 5, 2, 64), z(256, dtype=torch.uint8)
+rt, rp = kvg.rotary(), kvg.rope()
+append = lambda c=cache, s=seqs, p=packed, n=None, out=q: kvg.kvg_norm_append(c, s, p, rt, n, 0, 1, q, k, k, out)
+attn = lambda c=cache, s=seqs, p=packed, out=q: kvg.kvg_packed_attn(c, s, p, 0, 1, q, 0.1, out, ws)
+hdr = kvg.kvg_artifact_header_init(cache, 20, 0, rp)
+f = lambda *s: z(*s, dtype=torch.float32)
+calls = dict(
+    cu_length=lambda: packed.struct(kvg.Seqs(i32(4, 2), i32(4), z(4, dtype=torch.int64), 8)),
+    cu_type=lambda: kvg.Packed(z(3, dtype=torch.int64), 5, 4).struct(seqs),
+    weights=lambda: kvg.HeadNorm(z(32), None, 1e-6).struct(cache, 1),
+    positions=lambda: kvg.kvg_rotate(rt, i32(5), q[0], q[0]),
+    few_positions=lambda: kvg.kvg_rotate(rt, z(4, dtype=torch.int64), q[0], q[0]),
+    q_out=lambda: append(out=z(1, 5, 2, 64)),
+    q_out_type=lambda: append(out=f(1, 5, 4, 64)),
+    out=lambda: attn(out=z(1, 4, 4, 64)),
+    out_strided=lambda: attn(out=z(1, 5, 8, 64)[:, :, ::2]),
+    pools=lambda: kvg.Cache(z(1, 4, 2, 16, 64), z(1, 3, 2, 16, 64), 4).struct(),
+    pool_strided=lambda: kvg.Cache(z(1, 8, 2, 16, 64)[:, ::2], z(1, 4, 2, 16, 64), 4).struct(),
+    table=lambda: kvg.Seqs(z(2, 2, dtype=torch.int64), i32(2), z(2, dtype=torch.int64), 8).struct(),
+    ctx=lambda: kvg.Seqs(i32(2, 2), z(2, dtype=torch.int64), z(2, dtype=torch.int64), 8).struct(),
+    raw=lambda: kvg.kvg_append(cache, seqs, rp, 0, 1, 1, f(1, 2, 1, 2, 64), f(1, 2, 1, 2, 64)),
+    deposit=lambda: kvg.kvg_deposit(cache, i32(2), 0, 20, z(8)),
+    graft=lambda: kvg.kvg_graft(cache, hdr, z(8), i32(2), 0, 0),
+    windows=lambda: kvg.Cache.allocate(2, 4, 4, 2, 64, bf16, "cpu", windows=(8,)),
+    pack=lambda: kvg.kvg_logits_pack(z(10, 128), z(8)),
+    logits=lambda: kvg.kvg_logits(f(3, 128), z(8), 10, 1.0, f(3, 10), ws),
+    compare=lambda: kvg.kvg_logit_compare(f(3, 10), f(2, 10), z(3, dtype=torch.float64), i32(3), i32(3)),
+    compare_out=lambda: kvg.kvg_logit_compare(f(3, 10), f(3, 10), f(3), i32(3), i32(3)),
+)
+kept = []
+for name, call in calls.items():
+    try:
+        call()
+    except ValueError:
+        continue
+    except Exception as e:
+        name += " " + repr(e)
+    kept.append(name)
+if kept:
+    sys.exit(", ".join(kept))
+'''
+
+
+def test_the_binding_refuses_when_optimised():
+    """Its checks stand where python drops assertions, too (-O)."""
+    import os
+    import subprocess
+    import sys
+    pytest.importorskip("torch")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    res = subprocess.run([sys.executable, "-O", "-c", OPTIMISED], cwd=root, capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, res.stderr[-2000:]
