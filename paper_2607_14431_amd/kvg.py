@@ -222,6 +222,8 @@ class Cache:
         c = kvg_cache(n_layers, self.n_q_heads, n_kv_heads, head_dim, page_size, _DTYPE_CODE[dtype], n_pages,
                       k.data_ptr(), v.data_ptr(), None)
         if self.windows is not None and any(self.windows):
+            if len(self.windows) != n_layers:
+                raise ValueError("windows: one per layer")
             arr = (ctypes.c_int32 * len(self.windows))(*self.windows)
             c.layer_window = ctypes.cast(arr, ctypes.POINTER(ctypes.c_int32))
             c._windows_keepalive = arr        # the struct holds a raw pointer into this array
@@ -244,6 +246,8 @@ class Seqs:
         if not (bt.dtype is torch.int32 and bt.is_contiguous() and len(shape) == 2 and ctx.dtype is torch.int32 and
                 pos.dtype is torch.int64):
             raise ValueError("block_tables: int32 [batch][max_pages], contiguous; ctx_lens: int32; start_pos: int64")
+        if not (ctx.numel() >= shape[0] <= pos.numel() and ctx.is_contiguous() and pos.is_contiguous()):
+            raise ValueError("ctx_lens, start_pos: [batch], contiguous")
         return kvg_seqs(shape[0], shape[1], self.max_ctx_len, self.shared_tokens, bt.data_ptr(), ctx.data_ptr(),
                         pos.data_ptr())
 
@@ -483,6 +487,8 @@ def kvg_packed_attn(cache: Cache, seqs: Seqs, packed: Packed, layer0: int, n_lay
     sq = _token_stride(q, n_layers, T, Hq, D, raw)
     if not (out.shape == (n_layers, T, Hq, D) and out.dtype is raw and out.is_contiguous()):
         raise ValueError("out: [n_layers][n_tokens][n_q_heads][head_dim] of the raw dtype, contiguous")
+    if not ws.is_contiguous():
+        raise ValueError("ws: contiguous")
     _on_current_device(cache.k_pool, cache.v_pool, packed.cu_tokens, seqs.block_tables, seqs.ctx_lens, q, out, ws)
     _check(_lib.kvg_packed_attn(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()),
                                 ctypes.byref(packed.struct(seqs, sq)), layer0, n_layers, _ptr(q), scale, _ptr(out),

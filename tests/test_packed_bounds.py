@@ -126,3 +126,24 @@ def test_the_binding_refuses_when_optimised():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     res = subprocess.run([sys.executable, "-O", "-c", OPTIMISED], cwd=root, capture_output=True, text=True, timeout=300)
     assert res.returncode == 0, res.stderr[-2000:]
+
+
+def test_metadata_covers_the_batch():
+    """A workspace, windows or sequence metadata shorter than what the library reads or writes of them are refused."""
+    torch = pytest.importorskip("torch")
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    i64 = lambda *s: torch.zeros(s, dtype=torch.int64)  # noqa: E731
+    kvg.Seqs(i32(3, 2), i32(3), i64(3), 8).struct()
+    for ctx, pos in ((i32(2), i64(3)), (i32(3), i64(2)), (i32(3, 2)[:, 0], i64(3)), (i32(3), i64(3, 2)[:, 1]),
+                     (i32(1).expand(3), i64(3)), (i32(3), i64(1).expand(3))):
+        with pytest.raises(ValueError, match="batch"):
+            kvg.Seqs(i32(3, 2), ctx, pos, 8).struct()
+    pool = torch.zeros(3, 4, 2, 16, 64, dtype=torch.bfloat16)
+    for windows in ((8,), (0, 8), (8, 0, 0, 0)):
+        with pytest.raises(ValueError, match="per layer"):
+            kvg.Cache(pool, pool, 4, windows).struct()
+    cache, seqs = kvg.Cache(pool, pool, 4), kvg.Seqs(i32(1, 2), i32(1), i64(1), 8)
+    q = torch.zeros(3, 5, 4, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="ws"):
+        kvg.kvg_packed_attn(cache, seqs, kvg.Packed(i32(2), 5, 5), 0, 3, q, 0.1, torch.zeros_like(q),
+                            torch.zeros(1, dtype=torch.uint8).expand(1 << 20))
