@@ -309,7 +309,8 @@ int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_pack
   if (st != KVG_OK) return st;
   if ((st = check_layers(cache, layer0, n_layers)) != KVG_OK) return st;
   if ((st = check_packed(cache, seqs, packed)) != KVG_OK) return st;
-  if (!(scale > 0.0f) || !std::isfinite(scale)) return KVG_E_INVAL;
+  const float scale_log2 = scale * 1.4426950408889634f;
+  if (!(scale > 0.0f) || !std::isfinite(scale_log2)) return KVG_E_INVAL;      // scores go in log2 units
   kvg::PackedAttnArgs a;
   std::memset(&a, 0, sizeof(a));
   if ((st = check_stride(packed->q_stride, (int64_t)cache->n_q_heads * cache->head_dim, raw_bytes(cache->dtype),
@@ -332,7 +333,7 @@ int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_pack
   a.n_pages = cache->n_pages;
   a.q = q;
   a.out = out;
-  a.scale_log2 = scale * 1.4426950408889634f;
+  a.scale_log2 = scale_log2;
   a.Hq = cache->n_q_heads;
   a.Hkv = cache->n_kv_heads;
   a.D = cache->head_dim;

@@ -147,3 +147,11 @@ def test_metadata_covers_the_batch():
     with pytest.raises(ValueError, match="ws"):
         kvg.kvg_packed_attn(cache, seqs, kvg.Packed(i32(2), 5, 5), 0, 3, q, 0.1, torch.zeros_like(q),
                             torch.zeros(1, dtype=torch.uint8).expand(1 << 20))
+
+
+@pytest.mark.parametrize("scale,status", [(2.3e38, 0), (2.4e38, -1), (3.4e38, -1), (1e-45, 0)])
+def test_scales_whose_product_with_log2_e_overflows(scale, status):
+    """Scores are taken in log2 units: a scale that is finite but not in those is refused."""
+    c, s, p = _cache(), _seqs(), _packed()
+    size = kvg.raw_call("kvg_packed_attn_workspace_bytes", R(c), R(s), R(p), 2)
+    assert kvg.raw_call("kvg_packed_attn", R(c), R(s), R(p), 0, 2, 0x10000, scale, 0x20000, 0x30000, size, None) == status
