@@ -79,6 +79,8 @@ typedef enum { KVG_F32 = 0, KVG_BF16 = 1, KVG_FP8_E4M3 = 2 } kvg_dtype;
 /* Rotary pairing of the D components: HALF pairs i with i + D/2, INTERLEAVED pairs
  * 2i with 2i + 1.  theta_i = base^(-2i/D), i in [0, D/2). */
 typedef enum { KVG_ROPE_HALF = 0, KVG_ROPE_INTERLEAVED = 1 } kvg_rope_pairing;
+/* rope_pairing of a block whose keys no kvg_rope has rotated (kvg_artifact_header_init_rotary): it cannot be relocated */
+#define KVG_ROPE_OTHER 2
 
 typedef struct {
   double base;          /* e.g. 10000.0 */
@@ -150,6 +152,8 @@ typedef struct {
  *   [n_layers][2 (K, V)][ceil(n_tokens / page_size)][n_kv_heads][page_size][head_dim]
  * elements of `dtype` in logical page order; rows at or beyond n_tokens in the last
  * page are zero.
+ * rope_base, rope_pairing: the rotary of the keys, which a relocation turns further; pairing KVG_ROPE_OTHER: not one
+ * that it can (rope_base is then not used).
  * digest: the payload's content digest (block digests, Sec. 4.11), filled by
  * kvg_artifact_seal: the payload is cut into leaves of digest_leaf_bytes bytes (one
  * page of one KV head, page_size * head_dim elements: the layout's natural unit), each
@@ -244,7 +248,8 @@ int kvg_artifact_verify(const kvg_artifact_hdr* hdr, const void* payload, void* 
  *   d != 0: requires KVG_GRAFT_ALLOW_RELOCATE; keys are re-rotated by d (fp32
  *           rotation with cos/sin of d * theta_i computed in fp64 on the host,
  *           rounded to the storage dtype), values copied.  Not byte-exact against a
- *           fresh computation at the new offset (Sec. 4.2).
+ *           fresh computation at the new offset (Sec. 4.2).  A block of rope_pairing
+ *           KVG_ROPE_OTHER is refused (KVG_E_POSITION).
  * payload: device memory or host-pinned memory the device can read.  The graft is a plain
  * asynchronous copy: it does not read the digest (kvg_artifact_verify checks the payload
  * against it first).
@@ -334,9 +339,8 @@ int kvg_decode_attn_noalloc(const kvg_cache* cache, const kvg_seqs* seqs, const 
  * and key heads, rotate part of a head, or scale the rotation for long contexts.
  * kvg_norm_append writes the new tokens' keys and values to the cache and their queries, normed
  * and rotated, to q_out; kvg_packed_attn attends over the cache from them.  The blocks deposited
- * from such a cache graft like any other at their own position (a byte move); kvg_graft's
- * relocation re-rotates keys with the header's base over the whole head, so it is right
- * only for a rotary without scaling and with rotary_dim = head_dim. */
+ * from such a cache graft like any other at their own position (a byte move); their headers come from
+ * kvg_artifact_header_init_rotary, which leaves open to relocation those that it can be right for. */
 
 /* How a rotary's frequencies follow from theta_i = base^(-2i/r), i in [0, r/2), r = rotary_dim,
  * for a context `factor` times longer than the original_len tokens they were made for. */
@@ -400,6 +404,13 @@ typedef struct {
 /* The rotary's frequencies as the calls below use them: head_dim's rotary_dim / 2 values into
  * theta_out (host).  Errors: KVG_E_INVAL, KVG_E_SHAPE (rotary_dim). */
 int kvg_rotary_frequencies(const kvg_rotary* rotary, int32_t head_dim, double* theta_out);
+
+/* kvg_artifact_header_init for a block whose keys were rotated by `rotary`.  kvg_graft's relocation turns keys by one base's
+ * frequencies over the whole head: where the rotary has these (rotary_dim = head_dim or 0, and no scaling, KVG_ROTARY_BASE or a
+ * factor of 1; any amplitude) the header carries them, otherwise its rope_pairing is KVG_ROPE_OTHER and the block
+ * grafts at its own position alone.  Errors: KVG_E_INVAL, KVG_E_SHAPE, KVG_E_DTYPE. */
+int kvg_artifact_header_init_rotary(const kvg_cache* cache, int32_t n_tokens, int64_t own_pos, const kvg_rotary* rotary,
+                                    kvg_artifact_hdr* hdr_out);
 
 /* Rotary positions of packed rows: y[t][h] = the rotation of x[t][h] at positions[t], for n_tokens rows
  * of n_heads heads of head_dim (64, 128 or 256) components of `dtype` (KVG_F32 or KVG_BF16),

@@ -527,13 +527,14 @@ int kvg_graft(const kvg_cache* cache, const kvg_artifact_hdr* hdr, const void* p
       hdr->head_dim != cache->head_dim || hdr->page_size != cache->page_size)
     return KVG_E_SHAPE;
   if (hdr->payload_bytes != kvg_payload_bytes(cache, hdr->n_tokens)) return KVG_E_CORRUPT;
-  if (hdr->rope_pairing != KVG_ROPE_HALF && hdr->rope_pairing != KVG_ROPE_INTERLEAVED) return KVG_E_CORRUPT;
+  if (hdr->rope_pairing != KVG_ROPE_HALF && hdr->rope_pairing != KVG_ROPE_INTERLEAVED && hdr->rope_pairing != KVG_ROPE_OTHER)
+    return KVG_E_CORRUPT;
   if (!(hdr->rope_base > 0.0) || !std::isfinite(hdr->rope_base)) return KVG_E_CORRUPT;
   if (first_token % cache->page_size != 0) return KVG_E_ALIGN;
   const int32_t n_pages = (hdr->n_tokens + cache->page_size - 1) / cache->page_size;
   if ((int64_t)first_token / cache->page_size + n_pages > table_len) return KVG_E_CAPACITY;
   const int64_t d = target_pos - hdr->own_pos;
-  if (d != 0 && !(flags & KVG_GRAFT_ALLOW_RELOCATE)) return KVG_E_POSITION;
+  if (d != 0 && (!(flags & KVG_GRAFT_ALLOW_RELOCATE) || hdr->rope_pairing == KVG_ROPE_OTHER)) return KVG_E_POSITION;
 
   kvg::CopyArgs a;
   std::memset(&a, 0, sizeof(a));

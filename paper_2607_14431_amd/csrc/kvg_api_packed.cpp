@@ -34,8 +34,12 @@ int check_rotary(const kvg_rotary* r, int32_t head_dim) {
   return KVG_OK;
 }
 
+double scaled_base(const kvg_rotary* r, int dim) {
+  return r->scaling == KVG_ROTARY_BASE ? r->base * std::pow(r->factor, dim / (dim - 2.0)) : r->base;
+}
+
 void frequencies(const kvg_rotary* r, int dim, double* theta) {
-  const double base = r->scaling == KVG_ROTARY_BASE ? r->base * std::pow(r->factor, dim / (dim - 2.0)) : r->base;
+  const double base = scaled_base(r, dim);
   double lo = 0.0, hi = 0.0;
   if (r->scaling == KVG_ROTARY_INDEX) {
     auto index = [&](double turns) { return dim * std::log(r->original_len / (kTwoPi * turns)) / (2.0 * std::log(r->base)); };
@@ -209,6 +213,20 @@ int kvg_rotary_frequencies(const kvg_rotary* rotary, int32_t head_dim, double* t
   if (head_dim != 64 && head_dim != 128 && head_dim != 256) return KVG_E_SHAPE;
   const int st = check_rotary(rotary, head_dim);
   if (st == KVG_OK) frequencies(rotary, rotary_dim(rotary, head_dim), theta_out);
+  return st;
+}
+
+int kvg_artifact_header_init_rotary(const kvg_cache* cache, int32_t n_tokens, int64_t own_pos, const kvg_rotary* rotary,
+                                    kvg_artifact_hdr* hdr) {
+  int st = check_cache(cache);
+  if (st != KVG_OK) return st;
+  if ((st = check_rotary(rotary, cache->head_dim)) != KVG_OK) return st;
+  const int dim = rotary_dim(rotary, cache->head_dim);
+  const double base = scaled_base(rotary, dim);
+  const bool one_base = rotary->scaling == KVG_ROTARY_PLAIN || rotary->scaling == KVG_ROTARY_BASE || rotary->factor == 1.0;
+  const kvg_rope rope = {std::isfinite(base) ? base : rotary->base, rotary->pairing, 0};
+  st = kvg_artifact_header_init(cache, n_tokens, own_pos, &rope, hdr);
+  if (st == KVG_OK && (!one_base || dim != cache->head_dim || !std::isfinite(base))) hdr->rope_pairing = KVG_ROPE_OTHER;
   return st;
 }
 

@@ -20,7 +20,7 @@ if not os.path.exists(LIB_PATH):
 _lib = ctypes.CDLL(LIB_PATH)
 
 KVG_F32, KVG_BF16, KVG_FP8_E4M3 = 0, 1, 2
-KVG_ROPE_HALF, KVG_ROPE_INTERLEAVED = 0, 1
+KVG_ROPE_HALF, KVG_ROPE_INTERLEAVED, KVG_ROPE_OTHER = 0, 1, 2
 KVG_GRAFT_ALLOW_RELOCATE = 1
 KVG_ROTARY_PLAIN, KVG_ROTARY_LINEAR, KVG_ROTARY_BASE, KVG_ROTARY_ROTATIONS, KVG_ROTARY_INDEX = range(5)
 KVG_ARTIFACT_MAGIC = 0x4147564B
@@ -106,6 +106,7 @@ _SIGS = {
     "kvg_decode_attn_noalloc": (ctypes.c_int, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_rope), _i32, _i32, _vp, _vp, _vp,
                                                _f32, _vp, _vp]),
     "kvg_rotary_frequencies": (ctypes.c_int, [_P(kvg_rotary), _i32, _P(ctypes.c_double)]),
+    "kvg_artifact_header_init_rotary": (ctypes.c_int, [_P(kvg_cache), _i32, _i64, _P(kvg_rotary), _P(kvg_artifact_hdr)]),
     "kvg_rotate": (ctypes.c_int, [_P(kvg_rotary), _i32, _i32, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _vp]),
     "kvg_norm_append": (ctypes.c_int, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_packed), _P(kvg_rotary), _P(kvg_head_norm),
                                        _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
@@ -422,6 +423,13 @@ def kvg_rotary_frequencies(rt: kvg_rotary, head_dim: int) -> list[float]:
     theta = (ctypes.c_double * 128)()
     _check(_lib.kvg_rotary_frequencies(ctypes.byref(rt), head_dim, theta), "kvg_rotary_frequencies")
     return list(theta[: (rt.rotary_dim or head_dim) // 2])
+
+
+def kvg_artifact_header_init_rotary(cache: Cache, n_tokens: int, own_pos: int, rt: kvg_rotary) -> kvg_artifact_hdr:
+    hdr = kvg_artifact_hdr()
+    _check(_lib.kvg_artifact_header_init_rotary(ctypes.byref(cache.struct()), n_tokens, own_pos, ctypes.byref(rt),
+                                                ctypes.byref(hdr)), "kvg_artifact_header_init_rotary")
+    return hdr
 
 
 def kvg_rotate(rt: kvg_rotary, positions: torch.Tensor, x: torch.Tensor, y: torch.Tensor, stream=None):

@@ -155,3 +155,47 @@ def test_scales_whose_product_with_log2_e_overflows(scale, status):
     c, s, p = _cache(), _seqs(), _packed()
     size = kvg.raw_call("kvg_packed_attn_workspace_bytes", R(c), R(s), R(p), 2)
     assert kvg.raw_call("kvg_packed_attn", R(c), R(s), R(p), 0, 2, 0x10000, scale, 0x20000, 0x30000, size, None) == status
+
+
+# rotary of a block, and whether its keys are those of one base over the whole head (the base), so that a relocation is right
+ROTARIES = [
+    (dict(base=500.0), 500.0), (dict(base=500.0, rotary_dim=64, pairing=1), 500.0), (dict(amplitude=1.3), 10000.0),
+    (dict(scaling=2, factor=8.0), 10000.0 * 8.0 ** (64 / 62)), (dict(scaling=1, factor=1.0), 10000.0),
+    (dict(scaling=3, factor=1.0, original_len=100.0, fast=4.0, slow=1.0), 10000.0),
+    (dict(rotary_dim=32), None), (dict(rotary_dim=48, scaling=2, factor=8.0), None), (dict(scaling=1, factor=8.0), None),
+    (dict(scaling=3, factor=8.0, original_len=100.0, fast=4.0, slow=1.0), None),
+    (dict(scaling=4, factor=8.0, original_len=4096.0, fast=32.0, slow=1.0), None), (dict(base=1e300, scaling=2, factor=1e300), None),
+]
+
+
+@pytest.mark.parametrize("kw,base", ROTARIES)
+def test_headers_of_scaled_rotaries_refuse_what_relocation_cannot_do(kw, base):
+    rt, c = kvg.rotary(**kw), _cache()
+    hdr, plain = kvg.kvg_artifact_hdr(), kvg.kvg_artifact_hdr()
+    assert kvg.raw_call("kvg_artifact_header_init_rotary", R(c), 40, 128, R(rt), R(hdr)) == 0
+    rp = kvg.rope(hdr.rope_base, rt.pairing)
+    assert kvg.raw_call("kvg_artifact_header_init", R(c), 40, 128, R(rp), R(plain)) == 0
+    if base is None:
+        assert hdr.rope_pairing == kvg.KVG_ROPE_OTHER
+        plain.rope_pairing = hdr.rope_pairing
+    else:
+        assert abs(hdr.rope_base / base - 1) < 1e-14
+        theta = kvg.kvg_rotary_frequencies(rt, 64)
+        assert all(abs(t / hdr.rope_base ** (-i / 32) - 1) < 1e-13 for i, t in enumerate(theta))
+    assert bytes(hdr) == bytes(plain)                      # else as kvg_artifact_header_init's
+    graft = lambda target, flags, first=0: kvg.raw_call("kvg_graft", R(c), R(hdr), 0x8000, 0x9000, 3, first, target, flags, None)  # noqa: E731
+    assert graft(128, 0, first=16) == -5 and graft(129, 0) == -4
+    if base is None:
+        assert graft(129, kvg.KVG_GRAFT_ALLOW_RELOCATE) == -4
+    hdr.rope_pairing = 3
+    assert graft(128, 0) == -7
+
+
+def test_header_of_a_rotary_refusals():
+    c, hdr = _cache(), kvg.kvg_artifact_hdr()
+    init = lambda c=c, n=40, rt=kvg.rotary(), out=R(hdr): kvg.raw_call(  # noqa: E731
+        "kvg_artifact_header_init_rotary", R(c), n, 0, None if rt is None else R(rt), out)
+    assert init() == 0
+    assert init(rt=None) == -1 and init(n=0) == -1 and init(out=None) == -1
+    assert init(rt=kvg.rotary(base=0.5)) == -1 and init(rt=kvg.rotary(rotary_dim=80)) == -2
+    assert init(c=_cache(head_dim=96)) == -2 and init(c=_cache(dtype=7)) == -3
