@@ -32,7 +32,8 @@
  *    workspace extents the arguments describe: block-table entries outside
  *    [0, n_pages) and context lengths outside [0, max_ctx_len] are skipped (the
  *    affected outputs are then unspecified), never dereferenced.
- *  - Cached and raw values are expected to be finite.  An Inf or NaN makes the outputs of the
+ *  - Cached and raw values are expected to be finite.  An Inf or NaN (an Inf that an fp8 cache
+ *    stores becomes +-448) makes the outputs of the
  *    rows that see its token Inf or NaN, and of no others, with one exception: a prefill of a
  *    bf16 or fp8 cache with at most 4 query heads per KV head weighs the values of tokens that a
  *    row does not see by 0, and 0 times such a value is NaN for the rows of the same tile.
@@ -71,7 +72,7 @@ typedef enum {
  * 7, 3 mantissa bits; largest finite 448, codes 0x7F / 0xFF NaN), the KV-cache
  * quantization the paper lists among the serving settings that shape a block (Sec. 4.4):
  * its raw q/k/v inputs are bf16, stored keys (after rotation) and values are rounded once
- * to nearest even and saturate at +-448, and attention reads them back exactly (every
+ * to nearest even and saturate at +-448 (an Inf too; a NaN stays a NaN), and attention reads them back exactly (every
  * E4M3 value is a bf16 value).  A block's payload keeps the cache's bytes, so an fp8 block
  * is half the size of a bf16 one and its graft is the same byte copy. */
 typedef enum { KVG_F32 = 0, KVG_BF16 = 1, KVG_FP8_E4M3 = 2 } kvg_dtype;

@@ -48,11 +48,14 @@ template <> struct Elem<float> {               // fp32 storage
 };
 
 // fp8 storage: OCP FP8 E4M3 (the chip's native fp8 conversions).  Stored values saturate at
-// +-448 (the conversion instruction itself turns overflow into NaN); rounding is to nearest
+// +-448 (the conversion instruction itself turns overflow into NaN), a NaN stays one (fmaxf and fminf would make it
+// -448; the instructions of the maximum and minimum that keep it cost the same); rounding is to nearest
 // even, subnormals included.  The raw q/k/v handed to an fp8 cache are bf16.
 constexpr float kFp8Max = 448.0f;
 
-__device__ __forceinline__ float fp8_clamp(float f) { return fminf(fmaxf(f, -kFp8Max), kFp8Max); }
+__device__ __forceinline__ float fp8_clamp(float f) {
+  return __builtin_elementwise_minimum(__builtin_elementwise_maximum(f, -kFp8Max), kFp8Max);
+}
 
 // two values into the low (HI = false) or high 16-bit half of `old`
 template <bool HI>

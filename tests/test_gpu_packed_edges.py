@@ -52,3 +52,66 @@ def test_blocks_of_scaled_rotaries_relocate_rightly_or_not_at_all(kvg, pairing, 
     # stored value by u more; the second rotation takes in the first one's error from both components (sqrt 2 of it)
     assert np.all(np.abs(there.keys_values(0, 0)[0] - want) <= 5 * U * (1 + math.sqrt(2)) * 1.01 * size)
     assert np.array_equal(there.keys_values(0, 0)[1], b.keys_values(0, 0)[1])
+
+
+# ---------------------------------------------------------------------------- values fp8 cannot hold
+
+@pytest.mark.parametrize("call", ["packed", "packed, normed", "append", "decode"])
+@pytest.mark.parametrize("pairing", [0, 1])
+def test_fp8_caches_saturate_and_keep_nan(kvg, call, pairing):
+    """Values beyond +-448 and infinities are stored as +-448, NaN as NaN (in a key: in its pair; in a normed one: in its
+    head); everything else is stored as ever."""
+    B, D = 3, 64
+    n = 1 if call == "decode" else 4
+    fresh = lambda: Batch([n] * B, [0, 20, 5], (4, 2, D), "fp8", seed=23, poison=3.0)  # noqa: E731
+    weight = torch.ones(1, D, dtype=torch.bfloat16, device="cuda")
+
+    def stored(b, k, v):
+        if call.startswith("packed"):
+            append(b, kvg.rotary(10000.0, pairing), None if call == "packed" else kvg.HeadNorm(None, weight, 1e-6), None, k, v, None)
+        else:
+            kk, vv = (x.view(1, B, n, 2, D) for x in (k, v))
+            if call == "append":
+                kvg.kvg_append(b.cache, b.seqs, kvg.rope(10000.0, pairing), 0, 1, n, kk, vv)
+            else:
+                out = torch.empty(1, B, 4, D, device="cuda")
+                kvg.kvg_decode_attn(b.cache, b.seqs, kvg.rope(10000.0, pairing), 0, 1, b.rows(4).view(1, B, 4, D), kk[:, :, 0],
+                                    vv[:, :, 0], 0.1, out, kvg.decode_workspace(b.cache, b.seqs, 1))
+        return [np.stack([b.keys_values(0, s)[j][b.ctxs[s]:] for s in range(B)]) for j in range(2)]
+
+    a = fresh()
+    k, v = a.rows(2), a.rows(2)
+    k[0, 1, 0, 9], v[0, 1, 1, 9] = 300.0, 500.0                # sequence 0 or 1: large, and beyond the type's range
+    want_k, want_v = stored(a, k, v)
+    assert np.array_equal(want_v.reshape(v[0].shape), host(v[0].float().clamp(-448, 448).to(torch.float8_e4m3fn)))
+    assert (want_v == 448).any() and np.isfinite(want_k).all()
+    at, nan, inf = n * B - 1, float("nan"), float("inf")        # the last token
+    v[0, at, 0, 3:7] = torch.tensor([inf, -inf, nan, 1e30], device="cuda", dtype=v.dtype)
+    k[0, at, 1, 5] = nan
+    got_k, got_v = (x.reshape(-1, 2, D) for x in stored(fresh(), k, v))
+    want_k, want_v = (x.reshape(-1, 2, D) for x in (want_k, want_v))
+    assert np.array_equal(got_v[at, 0, [3, 4, 6]], [448, -448, 448]) and np.isnan(got_v[at, 0, 5])
+    want_v[at, 0, 3:7] = got_v[at, 0, 3:7]
+    assert np.array_equal(got_v, want_v, equal_nan=True)
+    pair = range(D) if call.endswith("normed") else (5, 5 + D // 2) if pairing == 0 else (4, 5)
+    assert np.isnan(got_k[at, 1, list(pair)]).all()
+    want_k[at, 1, list(pair)] = nan
+    assert np.array_equal(got_k, want_k, equal_nan=True)
+
+
+def test_relocated_fp8_keys_keep_nan(kvg):
+    b = Batch([20], [0], (4, 2, 64), "fp8", seed=24, poison=3.0)
+    append(b, kvg.rotary(), None, None, b.rows(2), b.rows(2), None)
+    hdr = kvg.kvg_artifact_header_init(b.cache, 20, 0, kvg.rope())
+    payload = torch.empty(hdr.payload_bytes, dtype=torch.uint8, device="cuda")
+
+    def moved():
+        kvg.kvg_deposit(b.cache, b.seqs.block_tables[0], 0, 20, payload)
+        there = Batch([20], [0], (4, 2, 64), "fp8", seed=25, poison=3.0)
+        kvg.kvg_graft(there.cache, hdr, payload, there.seqs.block_tables[0], 0, 77, kvg.KVG_GRAFT_ALLOW_RELOCATE)
+        return there.keys_values(0, 0)[0]
+
+    want = moved()
+    b.cache.k_pool.view(torch.uint8)[0, int(b.table[0, 1]), 1, 2, 40] = 0x7F       # token 18
+    want[18, 1, [8, 40]] = np.nan
+    assert np.isfinite(want[:18]).all() and np.array_equal(moved(), want, equal_nan=True)
