@@ -455,8 +455,8 @@ size_t kvg_packed_attn_workspace_bytes(const kvg_cache* cache, const kvg_seqs* s
  * A row's bytes depend on its own query, keys and values alone: neither on how its sequence was cut
  * into calls, nor on the other sequences or the pages.  A whole prompt and a suffix over its grafted
  * prefix give the same bytes for the same token.  Inf and NaN among the keys and values reach
- * the rows that see their token and no others (a row that sees one is not finite there, and whether
- * Inf or NaN may depend on the cut).  seqs->start_pos is not read; seqs->shared_tokens is
+ * the rows that see their token and no others: a row that sees such a value is not finite in its dimension (whether
+ * Inf or NaN may depend on the cut); a score of NaN or +Inf makes a row NaN, one of -Inf has weight 0.  seqs->start_pos is not read; seqs->shared_tokens is
  * ignored.  ws_dev: kvg_packed_attn_workspace_bytes() bytes of scratch; nothing is kept in it from call to
  * call, and calls that may run at once need one each.
  * Errors: as kvg_norm_append, and KVG_E_WORKSPACE. */

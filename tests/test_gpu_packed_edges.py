@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from oracle import packed as oracle
-from tests.packed_helpers import U, Batch, host
+from tests.packed_helpers import U, Batch, attention_bound, check_attention, host
 from tests.test_gpu_packed import append, bits, make_rotary, pair_size
 
 pytestmark = pytest.mark.gpu
@@ -115,3 +115,98 @@ def test_relocated_fp8_keys_keep_nan(kvg):
     b.cache.k_pool.view(torch.uint8)[0, int(b.table[0, 1]), 1, 2, 40] = 0x7F       # token 18
     want[18, 1, [8, 40]] = np.nan
     assert np.isfinite(want[:18]).all() and np.array_equal(moved(), want, equal_nan=True)
+
+
+# ---------------------------------------------------------------------------- attention over one segment, few rows
+
+@pytest.mark.parametrize("dtype,heads", [("bf16", (16, 8, 256)), ("bf16", (16, 2, 128)), ("bf16", (4, 4, 128)), ("bf16", (4, 2, 64)),
+                                         ("fp8", (8, 4, 128)), ("fp8", (16, 8, 256))],
+                         ids=lambda x: x if isinstance(x, str) else "x".join(map(str, x)))
+@pytest.mark.parametrize("window", [0, 300])
+@pytest.mark.parametrize("lens", ["tokens", "chunks"])
+def test_few_rows_over_one_segment(kvg, dtype, heads, window, lens):
+    """Batches that one segment holds, so that no launch is split: a small one takes four waves a workgroup (over up to four
+    units of 128 keys; two waves at head_dim 64), one of many layers two.  Every row against the oracle, and the same bytes."""
+    L, ctxs = 48, [0, 129, 256, 399, 480, 510, 127, 330]
+    most = 32 * heads[1] // heads[0]                            # rows of 32 pairs
+    n = [1] * 8 if lens == "tokens" else [1, most, 3, most - 1, 2, 1, most, 4]
+    n = [min(x, most, 512 - c) for x, c in zip(n, ctxs)]
+    one = Batch(n, ctxs, heads, dtype, layers=1, windows=(window,), seed=26)
+    assert one.max_pages * 16 <= 512
+    q = one.rows(heads[0], 2.0)
+    want = one.attend(q, 0.1)
+    check_attention(one, q, want, 0.1)
+    pools = [p.view(torch.uint8).repeat(L, 1, 1, 1, 1).view(p.dtype) for p in (one.cache.k_pool, one.cache.v_pool)]
+    cache = kvg.Cache(pools[0], pools[1], heads[0], (window,) * L)
+    out = torch.full((L, *want.shape[1:]), 7.0, dtype=want.dtype, device="cuda")
+    kvg.kvg_packed_attn(cache, one.seqs, one.packed, 0, L, q.repeat(L, 1, 1, 1), 0.1, out,
+                        kvg.packed_attn_workspace(cache, one.seqs, one.packed, L))
+    for l in range(L):
+        assert torch.equal(bits(out[l]), bits(want[0])), l
+
+
+# ---------------------------------------------------------------------------- attention over values that are not finite
+
+@pytest.mark.parametrize("heads,lens,ctxs", [
+    ((4, 2, 64), [200, 3], [10, 100]), ((8, 1, 128), [200, 3], [10, 100]), ((2, 1, 256), [200, 3], [10, 100]),    # tiles
+    ((4, 2, 256), [300], [900]), ((8, 2, 128), [150, 1], [1500, 700]),                                            # split tiles
+    ((16, 8, 256), [1, 2, 9, 1], [90, 70, 63, 400]), ((4, 4, 128), [32, 1], [60, 200]), ((8, 2, 64), [8, 1], [64, 71]),   # few rows
+    ((16, 8, 256), [1, 4, 1], [1500, 700, 71])], ids=lambda x: "x".join(map(str, x)))
+@pytest.mark.parametrize("window", [0, 60])
+def test_fp8_nan_stays_with_the_rows_that_see_it(heads, lens, ctxs, window):
+    """NaN codes (of both signs) among the values and keys of token 70 of every sequence that has it: rows that do not see it keep
+    their bytes, rows that do are NaN, in that dimension (a value) or whole (a key)."""
+    group = heads[0] // heads[1]
+    for which, code in (("v", 0x7F), ("v", 0xFF), ("k", 0x7F), ("k", 0xFF)):
+        b = Batch(lens, ctxs, heads, "fp8", windows=(window,) if window else None, seed=27)
+        q = b.rows(heads[0], 2.0)
+        want = b.attend(q, 0.1)
+        assert want.float().isfinite().all()
+        pool = (b.cache.v_pool if which == "v" else b.cache.k_pool).view(torch.uint8)
+        for s, (n, c) in enumerate(zip(lens, ctxs)):
+            if c + n > 70:
+                pool[0, int(b.table[s, 70 // 16]), 0, 70 % 16, 5] = code
+        got = b.attend(q, 0.1)
+        for s, (n, c) in enumerate(zip(lens, ctxs)):
+            for i in range(n):
+                if c + i >= 70 and (not window or c + i < 70 + window):
+                    hit = got[0, int(b.cu[s]) + i, :group]
+                    assert (hit[:, 5] if which == "v" else hit).isnan().all(), (which, code, s, i)
+                    hit[:, 5 if which == "v" else slice(None)] = want[0, int(b.cu[s]) + i, :group, 5 if which == "v" else slice(None)]
+        assert torch.equal(bits(got), bits(want)), (which, code)
+
+
+@pytest.mark.parametrize("dtype,heads,lens,ctxs", [
+    ("bf16", (4, 2, 64), [100, 3], [0, 100]), ("bf16", (2, 1, 256), [130], [800]), ("bf16", (16, 8, 128), [1, 2], [90, 200]),
+    ("f32", (4, 2, 64), [100, 1], [0, 300])], ids=lambda x: x if isinstance(x, str) else "x".join(map(str, x)))
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_keys_that_are_infinite(dtype, heads, lens, ctxs, sign):
+    """A key with an infinite component scores Inf of one sign or the other: -Inf weighs 0, as if the key were not there; Inf leaves
+    the row NaN."""
+    b = Batch(lens, ctxs, heads, dtype, seed=28)
+    q = b.rows(heads[0], 2.0)
+    group, at = heads[0] // heads[1], 70
+    want = b.attend(q, 0.1)
+    for s in range(len(lens)):
+        b.cache.k_pool[0, int(b.table[s, at // 16]), 0, at % 16, 5] = sign * math.inf
+    got = b.attend(q, 0.1)
+    seen = 0
+    for s, (n, c) in enumerate(zip(lens, ctxs)):
+        k, v = b.keys_values(0, s)
+        without = np.arange(len(k)) != at
+        k[at] = 0.0
+        for i in range(n):
+            t = int(b.cu[s]) + i
+            if c + i < at:
+                assert torch.equal(bits(got[0, t]), bits(want[0, t])), (s, i)
+                continue
+            assert torch.equal(bits(got[0, t, group:]), bits(want[0, t, group:])), (s, i)
+            row = host(q[0, t:t + 1])[:, :group]
+            exact, tol = attention_bound(row, np.array([c + i - 1]), k[without, :1], v[without, :1], 0.1, 0, dtype)
+            for h in range(group):
+                if float(q[0, t, h, 5]) * sign > 0:
+                    assert got[0, t, h].isnan().all(), (s, i, h)
+                else:
+                    seen += 1
+                    assert np.all(np.abs(host(got[0, t, h]) - exact[0, h]) <= tol[0, h]), (s, i, h)
+    assert seen > 0
