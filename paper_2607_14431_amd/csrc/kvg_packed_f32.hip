@@ -44,7 +44,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_f32_kernel(const Packed
   constexpr int NJ = D / 8;            // 16-byte K loads per block and lane
   constexpr int ND = D / 32;           // blocks of O^T
   constexpr int LK = 8, LV = D == 256 ? 4 : 8;        // K and V loads ahead
-  constexpr int kChains = 4;           // accumulation chains of a score
+  constexpr int kChains = 4;           // accumulation chains of a score, one for each value of a load
   constexpr bool kQInLds = D == 256;   // the tile's queries, in registers where they fit
   constexpr int kPitch = 36;
   __shared__ __attribute__((aligned(16))) float s_o[kWaves][32][kPitch];
@@ -162,11 +162,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_f32_kernel(const Packed
         const Floats<4> k = kf[j % LK], qj = query(j);
         kf[j % LK] = load_floats<4>((j + LK < NJ ? kp : kp_next) + 8 * ((j + LK) % NJ));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c[e % kChains] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.x[e], qj.x[e], c[e % kChains], 0, 0, 0);
+        for (int e = 0; e < kChains; ++e) c[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.x[e], qj.x[e], c[e], 0, 0, 0);
       }
       kp = kp_next;
-      f32x16 s = c[0] + c[1];
-      if constexpr (kChains == 4) s += c[2] + c[3];
+      f32x16 s = (c[0] + c[1]) + (c[2] + c[3]);
       const bool edge = kb + 31 > first || kb < mask_lo;       // keys that some row does not see
       if (edge) {
 #pragma unroll

@@ -310,13 +310,16 @@ __device__ __forceinline__ void fold_tiles(const PackedAttnArgs& a, const Packed
       {(T)(o_run[0] * inv), (T)(o_run[1] * inv), (T)(o_run[2] * inv), (T)(o_run[3] * inv)}};
 }
 
-// Both in one launch: the few kernel's rows first, in few_workgroups workgroups.
+// Both in one launch: the few kernel's rows first, in few_workgroups workgroups (none beside fp32 caches, which it does not take).
 template <typename T, int D, int kPairs>
 __global__ __launch_bounds__(256) void packed_fold_kernel(const PackedAttnArgs a, const PackedPartials few, const uint32_t few_workgroups) {
-  if (blockIdx.x < few_workgroups)
-    fold_few<D>(a, few, blockIdx.x);
-  else
-    fold_tiles<T, D, kPairs>(a, a.part, blockIdx.x - few_workgroups);
+  if constexpr (!std::is_same<T, float>::value) {
+    if (blockIdx.x < few_workgroups) {
+      fold_few<D>(a, few, blockIdx.x);
+      return;
+    }
+  }
+  fold_tiles<T, D, kPairs>(a, a.part, blockIdx.x - few_workgroups);
 }
 
 // Waves of a workgroup: four take a segment of a launch that leaves CUs idle soonest, two leave room for more

@@ -5,7 +5,7 @@
 // logical index) in two LDS stages, loaded with buffer_load ... lds while the tile before is computed.
 //
 // A row's sums have one order, whatever the launch: keys in blocks of 32, an online softmax over the blocks of a
-// segment of kSeg keys (absolute multiples), and the segments' states folded in ascending order.  A
+// segment of kPackedSeg keys (absolute multiples), and the segments' states folded in ascending order.  A
 // workgroup that walks all keys folds in registers; split launches leave one partial per segment for
 // packed_fold_kernel (kvg_packed_few.hip), which folds them with the same operations.  Sequences of at most kFewPairs
 // pairs are left to packed_few_kernel, which takes the same operations too.
