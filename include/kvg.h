@@ -14,7 +14,7 @@
  *  - All pointers named *_dev, and every pointer inside kvg_cache / kvg_seqs, are
  *    device pointers unless stated.  The caller allocates and owns all memory
  *    (pools, tables, payloads, outputs, workspaces).  The library allocates no
- *    device memory, and nothing but a thread's table of its last rotary base's powers (and
+ *    device memory, and nothing but a thread's tables of its last rotary's frequencies (and
  *    kvg_decode_attn_noalloc's scratch array) outlives a call; calls are re-entrant.
  *  - `stream` is a hipStream_t (NULL = the null stream).  Kernels are enqueued on
  *    it and the call returns after enqueueing; results are visible after the

@@ -114,7 +114,8 @@ kvg::PackedSeqs packed_seqs(const kvg_seqs* s, const kvg_packed* p) {
 // and without windows), 192 x 4 35 / 51, 192 x 9 109 / 110, 192 x 34 363 / 442, 242 x 12 166 / 143, 250 x 4 51 / 60,
 // 314 x 5 65 / 67, 388 x 12 167 / 189; 64: 54 x 35 271 / 63, 56 x 3 27 / 17, 88 x 13 98 / 49, 176 x 13 103 / 67, 250 x
 // 40 330 / 280, 468 x 8 78 / 70.  fp32, more work on fewer rows to a workgroup: 32 x 2 26 / 21, 104 x 3 35 / 32, 184 x
-// 3 45 / 34, 216 x 2 31 / 34, 256 x 5 73 / 81, 528 x 3 191 / 195.
+// 3 45 / 34, 216 x 2 31 / 34, 256 x 5 73 / 81, 528 x 3 191 / 195.  The rule takes the slower side of two of
+// these: 128 x 10 at 256 and 468 x 8 at 64.
 bool split_tiles(bool f32, int64_t head_dim, int64_t workgroups, int64_t segs) {
   if (f32) return workgroups < std::min<int64_t>(256, 96 * (segs - 1));
   const bool cached = workgroups * segs * head_dim < 576000;           // partials of about 290 MB
@@ -126,7 +127,7 @@ bool split_tiles(bool f32, int64_t head_dim, int64_t workgroups, int64_t segs) {
 // workgroups and no empty waves.  Few kernel against tiles, each with its fold, us, at workgroups.  bf16, head_dim 256: 80
 // 26 / 24, 256 33 / 30, 512 52 / 56, 1,024 92 / 132, 8,448 536 / 1,090; 128: 128 23 / 21, 256 24 / 22, 512 31 / 32, 1,024 49 / 59; 64:
 // 64 20 / 17, 256 24 / 17, 512 27 / 23.  fp8, 256: 64 21 / 24, 128 23 / 25, 256 26 / 27, 512 35 / 49; 128: 64 17 / 18, 256 29 / 23;
-// 64: 16 19 / 16, 32 18 / 15.
+// 64: 16 19 / 16, 32 18 / 15.  One limit for all: at 512 it takes the slower side at head_dim 64.
 bool few_in_tiles(const kvg_cache* c, int64_t workgroups) {
   return workgroups <= 256 && (c->dtype == KVG_BF16 || c->head_dim <= 128);
 }

@@ -78,8 +78,9 @@ __device__ __forceinline__ SeqUnit find_token(const PackedSeqs& s, int tok) {
 }
 
 // Keys of a segment of the attention's sums (absolute multiples of the logical index).  Short ones spread few rows over the
-// chip, long ones fold less.  256 / 512 / 1,024 keys, us (of the first kernels): one token over 4.6k keys 21 / 23 / 34, 16 over 33k
-// 787 / 673 / 614, eight prompts 517 / 498 / 486, 12,288 tokens 1,526 / 1,445 / 1,380.
+// chip, long ones fold less.  256 / 512 / 1,024 keys, us: one token over 4.6k keys 20 / 24 / 35, 16 over 33k 579 / 531 / 523,
+// chunks of 35 rows over 32k (fp8) 181 / 145 / 124, a mixed batch with a window of 1,024 175 / 164 / 196, ragged fp32 chunks over
+// 1k 37 / 33 / 54, eight prompts 478 / 475 / 465, 12,288 tokens 1,211 / 1,159 / 1,132.
 constexpr int kPackedSeg = 512;
 
 // The rotation of a launch: frequencies and what cos and sin are multiplied with.

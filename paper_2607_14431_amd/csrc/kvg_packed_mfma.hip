@@ -20,9 +20,10 @@
 //
 // What bounds it: the matrix cores and the LDS together.  A fragment of 1 KiB takes the LDS 8 cycles and feeds one matrix
 // step of 32, and four waves read at a time: both are busy alike, with the softmax's vector work (at head_dim 128 as many
-// cycles again) and the waits between them.  A prompt of 12,288 tokens (16 / 8 heads x 256, bf16) takes 1,190 us: 1.04 PFLOP/s,
-// matrix cores 48% busy at 2.1 GHz; eight of up to 4,096 (32 / 16 x 128) 475 us: 0.81 PFLOP/s, 37%.  Two blocks of 32 pairs a
-// wave, which halve the fragments, are slower (12,288 tokens at head_dim 128, one wave a SIMD then: 1,844 us, 1,480; 64: 236, 170).
+// cycles again) and the waits between them.  A prompt of 12,288 tokens (16 / 8 heads x 256, bf16) takes 1,242 us: 1.00 PFLOP/s,
+// matrix cores 48% busy; eight of up to 4,096 (32 / 16 x 128) 480 us: 0.81 PFLOP/s, 37% (medians of 200 calls in a row; the
+// first ones of a run take up to a sixth longer, and cards differ by as much as 8%).  Two blocks of 32 pairs a wave, which halve the
+// fragments, were slower when tried: 1.25 times at head_dim 128 (one wave a SIMD then), 1.4 times at 64.
 #include "kvg_launch.h"
 #include "kvg_packed_mfma.h"
 
@@ -47,10 +48,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
   constexpr int BM = kTilePairs;
   static_assert(BM == 32 * kWaves, "a block of 32 pairs per wave");
   // Fragments ahead of their use at D <= 128: a row block's worth where the registers hold it (the others: prompts of up
-  // to 4,096 tokens, 32 / 16 heads x 128: four 598 us, six 579, eight, with spills, 841).
+  // to 4,096 tokens, 32 / 16 heads x 128: four, five or six 465 to 478 us, with seven registers spilled each; eight 764).
   constexpr int kRing = kSplitKeys || D == 64 ? NS : 6;
-  // A tile's loads among the matrix steps, or all at its start: 12,288 tokens at head_dim 256 1,306 us / 1,476; 64 236 / 247;
-  // 128 584 / 579.
+  // A tile's loads among the matrix steps, or all at its start: 12,288 tokens at head_dim 256 1,158 us / 1,310 (fp8 1,244 /
+  // 1,303); those prompts at 128 464 to 476 / 466, at 64 273 / 274 (fp8 280 / 271).
   constexpr bool kSpread = D != 128;
   using KR = KRows<RB>;
   using VR = VRows<RB>;
@@ -243,8 +244,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void packed_tiles_ke
       fresh = false;
     };
     // K fragments of both blocks form one stream read LK ahead of their MFMAs, V^T fragments one read LV ahead, whose first
-    // LV are issued with block 1's scores (bf16, four or six ahead: the same time; fp8 fragments are half as large: 12,288 tokens
-    // 1,531 us with four, 1,497 with eight; widened beside their reads 1,803)
+    // LV are issued with block 1's scores (four, six or eight ahead: 12,288 tokens 1,252 to 1,258 us, fp8 1,313 to 1,319; fp8
+    // fragments widened beside their reads, when tried, a fifth more)
     if constexpr (D <= 128) {
       // Two waves a SIMD: one's softmax runs beside the other's matrix steps.  The tile's K and V^T fragments, in the order of
       // their use, pass through one ring: a fragment's place is refilled with the one LR steps on.

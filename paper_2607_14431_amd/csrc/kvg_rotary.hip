@@ -8,7 +8,8 @@
 // keeps its place in the head, and with it its weights, from head to head.
 //
 // What bounds them: HBM in large calls, where each raw value is read and each result written once (eight prompts up to 4,096
-// tokens, 32 + 2 x 16 heads x 128: 78 us, 6.1 TB/s; a 4,096-token block of 48 heads x 128 rotated: 17 us, 6.0); the round
+// tokens, 32 + 2 x 16 heads x 128: 101 us, 4.7 TB/s, and 78 to 90 when the last-level cache holds inputs and pages of a repeated
+// call; a 4,096-token block of 48 heads x 128 rotated: 16.5 us, 6.1 TB/s); the round
 // trips in small ones (metadata, then angles; the first rows are requested before either: 16 single tokens of 16 + 2 x 8
 // heads x 256 5 to 6 us, one token's 24 heads rotated in 3.0).  Partners read from memory cost their second load and the registers
 // of two waves a SIMD (those prompts 89 us; fp8, 1,063 tokens x 6 layers 40, then 34).  Four tokens a workgroup, whose tables fill all
@@ -28,8 +29,8 @@ constexpr int kThreads = 256;
 // 5.2 us, 8 layers of them -, 6.8, 6.0; 300 tokens of 48 heads rotated -, 4.6, 4.0.
 constexpr int64_t kSmallGrid = 1024;
 
-// Results are written past the caches (those prompts 134 us with plain stores, 90, with partners from memory), raw rows are read
-// through them: a projection has just written them (nontemporal 95 us, 78 when the last-level cache holds some of them).
+// Results are written past the caches (those prompts 102.5 us, 106.5 with plain stores; the block rotated 16.5, 19.6), raw rows are
+// read through them, where a projection may just have written them (nontemporal: the prompts 101.7, the block 19.2).
 __device__ __forceinline__ void st16s(void* p, const uint4& v) {
   __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(p));
 }
