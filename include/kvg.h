@@ -464,6 +464,39 @@ int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_pack
                     int32_t n_layers, const void* q_dev, float scale, void* out_dev, void* ws_dev, size_t ws_bytes,
                     void* stream);
 
+/* ---------------------------------------------------------------------------------
+ * Positions with several axes (time, height and width of images and video, beside text): a token has a position on
+ * every axis, and each pair of a head's rotated components turns by one of them. */
+#define KVG_MAX_AXES 4
+
+/* Which axis a pair takes.  SECTIONS: the first pairs[0] pairs axis 0, the next pairs[1] axis 1, ...  TURNS: the axes take
+ * pairs in turn (pair 0 axis 0, pair 1 axis 1, ...), an axis that has had its pairs dropping out. */
+typedef enum { KVG_AXES_SECTIONS = 0, KVG_AXES_TURNS = 1 } kvg_axes_order;
+
+/* own_frequencies 0: pair i turns by theta_i of the whole rotary.  1 (SECTIONS alone): pair j of an axis with n pairs turns by
+ * theta_j of a rotary over 2 n components (base, scaling and factor as the rotary's). */
+typedef struct {
+  const int64_t* positions;     /* device [n_axes][n_tokens], any sign */
+  int32_t n_axes;               /* 1 to KVG_MAX_AXES */
+  int32_t order;                /* kvg_axes_order */
+  int32_t own_frequencies;
+  int32_t reserved;             /* must be 0 */
+  int32_t pairs[KVG_MAX_AXES];  /* of each axis, >= 1; rotary_dim / 2 together */
+} kvg_axes;
+
+/* kvg_rotate at positions with several axes.  The rotation at the negated positions is the gradient's: with amplitude 1 it
+ * undoes this one.  Errors: as kvg_rotate, KVG_E_INVAL (axes), KVG_E_SHAPE (pairs). */
+int kvg_rotate_axes(const kvg_rotary* rotary, const kvg_axes* axes, int32_t dtype, int32_t head_dim, int32_t n_tokens,
+                    int32_t n_heads, const void* x_dev, int64_t x_stride, void* y_dev, int64_t y_stride, void* stream);
+
+/* kvg_norm_append at positions with several axes: token row t of the packed tensors is at axes->positions[.][t]
+ * (seqs->start_pos is not read).  Blocks of such a cache graft at their own position: their header is
+ * kvg_artifact_header_init's with rope_pairing set to KVG_ROPE_OTHER.  Errors: as kvg_norm_append, KVG_E_INVAL (axes),
+ * KVG_E_SHAPE (pairs). */
+int kvg_norm_append_axes(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, const kvg_rotary* rotary,
+                         const kvg_axes* axes, const kvg_head_norm* norm, int32_t layer0, int32_t n_layers,
+                         const void* q_raw_dev, const void* k_raw_dev, const void* v_raw_dev, void* q_out_dev, void* stream);
+
 /* ---- Content digests of an artifact (block digests, Sec. 4.11; the paper's deposit-side
  * hashing is closed, Sec. 3.1).  These calls work on any device buffer, typically a
  * deposited payload.  SHA-256 is FIPS 180-4.  All three launch on `stream`, clear their

@@ -53,6 +53,33 @@ def rotate(x: np.ndarray, pos: np.ndarray, theta: np.ndarray, pairing: str, ampl
     return out
 
 
+def axis_of_pairs(pairs, order: str) -> np.ndarray:
+    """The axis of each pair: contiguous sections, or in turn until an axis has had its pairs."""
+    if order == "sections":
+        return np.repeat(np.arange(len(pairs)), pairs)
+    # pair j of axis k comes in turn j, after that turn's pairs of the axes before k
+    turns = sorted((j, k) for k, n in enumerate(pairs) for j in range(n))
+    return np.array([k for _, k in turns])
+
+
+def axes_frequencies(pairs, base, own: bool, **scaling) -> np.ndarray:
+    """theta of each pair: the whole rotary's, or every axis' own (sections)."""
+    if not own:
+        return frequencies(2 * sum(pairs), base, **scaling)
+    return np.concatenate([frequencies(2 * n, base, **scaling) for n in pairs])
+
+
+def rotate_axes(x, pos, theta, axis, pairing, amplitude=1.0) -> np.ndarray:
+    """x[..., T, H, D]: pair i turned by pos[axis[i]][T] * theta[i]."""
+    out = np.array(x, dtype=np.float64)
+    ia, ib = pair_index(2 * len(theta), pairing)
+    for i, t in enumerate(theta):
+        phi = np.asarray(pos[axis[i]], dtype=np.float64)[:, None] * t
+        z = (x[..., ia[i]] + 1j * x[..., ib[i]]) * (amplitude * np.exp(1j * phi))
+        out[..., ia[i]], out[..., ib[i]] = z.real, z.imag
+    return out
+
+
 def rms_norm(x: np.ndarray, weight: np.ndarray, eps: float, offset: float) -> np.ndarray:
     return x / np.sqrt(np.mean(np.square(x), axis=-1, keepdims=True) + eps) * (weight + offset)
 

@@ -90,6 +90,13 @@ struct RotaryArgs {
   double theta[kMaxHalfDim];
 };
 
+// Positions with several axes: the axis of each pair, and [axes][rows] positions.
+struct AxesArgs {
+  const int64_t* positions;
+  uint8_t axis[kMaxHalfDim];
+};
+struct NoAxes {};
+
 struct RotateArgs {
   const void* x;
   void* y;
@@ -145,8 +152,9 @@ struct PackedAttnArgs {
   int32_t window[kMaxWindowLayers];
 };
 
-hipError_t launch_rotate(const RotateArgs& a, int dtype, hipStream_t stream);
-hipError_t launch_norm_append(const NormAppendArgs& a, int dtype, hipStream_t stream);
+// axes: null where a token has one position
+hipError_t launch_rotate(const RotateArgs& a, const AxesArgs* axes, int dtype, hipStream_t stream);
+hipError_t launch_norm_append(const NormAppendArgs& a, const AxesArgs* axes, int dtype, hipStream_t stream);
 // bf16 and fp8 caches: pairs of a tile, workgroups of the launches
 constexpr int kFewPairs = 32;
 __device__ __forceinline__ bool is_few(const PackedAttnArgs& a, const SeqRange& s) {

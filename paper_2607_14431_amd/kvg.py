@@ -23,6 +23,8 @@ KVG_F32, KVG_BF16, KVG_FP8_E4M3 = 0, 1, 2
 KVG_ROPE_HALF, KVG_ROPE_INTERLEAVED, KVG_ROPE_OTHER = 0, 1, 2
 KVG_GRAFT_ALLOW_RELOCATE = 1
 KVG_ROTARY_PLAIN, KVG_ROTARY_LINEAR, KVG_ROTARY_BASE, KVG_ROTARY_ROTATIONS, KVG_ROTARY_INDEX = range(5)
+KVG_AXES_SECTIONS, KVG_AXES_TURNS = 0, 1
+KVG_MAX_AXES = 4
 KVG_ARTIFACT_MAGIC = 0x4147564B
 KVG_ARTIFACT_VERSION = 2
 
@@ -73,6 +75,11 @@ class kvg_packed(ctypes.Structure):
                 ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
 
 
+class kvg_axes(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("n_axes", ctypes.c_int32), ("order", ctypes.c_int32),
+                ("own_frequencies", ctypes.c_int32), ("reserved", ctypes.c_int32), ("pairs", ctypes.c_int32 * 4)]
+
+
 class kvg_artifact_hdr(ctypes.Structure):
     _fields_ = [("magic", ctypes.c_uint32), ("version", ctypes.c_uint32), ("dtype", ctypes.c_int32),
                 ("n_layers", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
@@ -110,6 +117,9 @@ _SIGS = {
     "kvg_rotate": (ctypes.c_int, [_P(kvg_rotary), _i32, _i32, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _vp]),
     "kvg_norm_append": (ctypes.c_int, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_packed), _P(kvg_rotary), _P(kvg_head_norm),
                                        _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
+    "kvg_rotate_axes": (ctypes.c_int, [_P(kvg_rotary), _P(kvg_axes), _i32, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp]),
+    "kvg_norm_append_axes": (ctypes.c_int, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_packed), _P(kvg_rotary), _P(kvg_axes),
+                                            _P(kvg_head_norm), _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
     "kvg_packed_attn_workspace_bytes": (_sz, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_packed), _i32]),
     "kvg_packed_attn": (ctypes.c_int, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_packed), _i32, _i32, _vp, _f32, _vp, _vp, _sz,
                                        _vp]),
@@ -432,34 +442,66 @@ def kvg_artifact_header_init_rotary(cache: Cache, n_tokens: int, own_pos: int, r
     return hdr
 
 
-def kvg_rotate(rt: kvg_rotary, positions: torch.Tensor, x: torch.Tensor, y: torch.Tensor, stream=None):
-    """y[t][h] = x[t][h] rotated at positions[t] (int64); x, y: [n_tokens][n_heads][head_dim], fp32 or bf16, heads
-    dense, any token stride; y may be x."""
+@dataclasses.dataclass
+class Axes:
+    """Positions with several axes: int64 [n_axes][n_tokens] (device); pairs of a head's rotated components for each axis,
+    in contiguous sections or in turn (kvg.h)."""
+    positions: torch.Tensor
+    pairs: tuple
+    order: int = KVG_AXES_SECTIONS
+    own_frequencies: bool = False
+
+    def struct(self, n_tokens: int) -> kvg_axes:
+        pos, n = self.positions, len(self.pairs)
+        if not 1 <= n <= KVG_MAX_AXES:
+            raise ValueError(f"pairs: of 1 to {KVG_MAX_AXES} axes")
+        if not (pos.dtype is torch.int64 and pos.is_contiguous() and pos.shape == (n, n_tokens)):
+            raise ValueError("positions: int64 [n_axes][n_tokens], contiguous")
+        return kvg_axes(pos.data_ptr(), n, self.order, int(self.own_frequencies), 0, (ctypes.c_int32 * 4)(*self.pairs))
+
+
+def _rotate_strides(where: str, x: torch.Tensor, y: torch.Tensor):
+    """Token strides of x and y, [n_tokens][n_heads][head_dim] with dense heads."""
     shape, dtype = x.shape, x.dtype
     T, H, D = shape
     if dtype is not torch.bfloat16 and dtype is not torch.float32:
-        raise KvgError(-3, "kvg_rotate")
+        raise KvgError(-3, where)
     sx, hx, dx = x.stride()
     sy, hy, dy = y.stride()
     if y.dtype is not dtype or y.shape != shape or dx != 1 or dy != 1 or H > 1 and (hx != D or hy != D):
-        raise ValueError("kvg_rotate: x and y alike, heads dense")
+        raise ValueError(f"{where}: x and y alike, heads dense")
     if T <= 1:
-        sx = sy = 0
-    elif sx < H * D or sy < H * D:         # a broadcast row among them: 0 is the library's word for dense rows
-        raise ValueError("kvg_rotate: a token's rows overlap the next one's")
+        return 0, 0
+    if sx < H * D or sy < H * D:           # a broadcast row among them: 0 is the library's word for dense rows
+        raise ValueError(f"{where}: a token's rows overlap the next one's")
+    return sx, sy
+
+
+def kvg_rotate(rt: kvg_rotary, positions: torch.Tensor, x: torch.Tensor, y: torch.Tensor, stream=None):
+    """y[t][h] = x[t][h] rotated at positions[t] (int64); x, y: [n_tokens][n_heads][head_dim], fp32 or bf16, heads
+    dense, any token stride; y may be x."""
+    T, H, D = x.shape
+    sx, sy = _rotate_strides("kvg_rotate", x, y)
     if not (positions.dtype is torch.int64 and positions.is_contiguous() and positions.numel() == T):
         raise ValueError("positions: int64 [n_tokens], contiguous")
     _on_current_device(positions, x, y)
-    _check(_lib.kvg_rotate(ctypes.byref(rt), 1 if dtype is torch.bfloat16 else 0, D, T, H, positions.data_ptr(), x.data_ptr(), sx,
+    _check(_lib.kvg_rotate(ctypes.byref(rt), 1 if x.dtype is torch.bfloat16 else 0, D, T, H, positions.data_ptr(), x.data_ptr(), sx,
                            y.data_ptr(), sy, _stream(stream)), "kvg_rotate")
 
 
-def kvg_norm_append(cache: Cache, seqs: Seqs, packed: Packed, rt: kvg_rotary, norm: HeadNorm | None, layer0: int,
-                    n_layers: int, q_raw: torch.Tensor | None, k_raw: torch.Tensor, v_raw: torch.Tensor,
-                    q_out: torch.Tensor | None, stream=None):
-    """Norm, rotation and append of packed tokens.  q_raw, k_raw, v_raw: [n_layers][n_tokens][heads][head_dim] of the raw
-    dtype, views into wider rows allowed; q_out: dense (q_raw and q_out: both None for keys and values alone)."""
-    raw, T, D, Hkv = cache.raw_dtype, packed.n_tokens, cache.head_dim, cache.n_kv_heads
+def kvg_rotate_axes(rt: kvg_rotary, axes: Axes, x: torch.Tensor, y: torch.Tensor, stream=None):
+    """kvg_rotate at positions with several axes."""
+    T, H, D = x.shape
+    sx, sy = _rotate_strides("kvg_rotate_axes", x, y)
+    _on_current_device(axes.positions, x, y)
+    _check(_lib.kvg_rotate_axes(ctypes.byref(rt), ctypes.byref(axes.struct(T)), 1 if x.dtype is torch.bfloat16 else 0, D, T, H,
+                                x.data_ptr(), sx, y.data_ptr(), sy, _stream(stream)), "kvg_rotate_axes")
+
+
+def _append_args(cache, raw, seqs: Seqs, packed: Packed, norm: HeadNorm | None, n_layers: int, q_raw, k_raw, v_raw, q_out,
+                 *others):
+    """Checked structs of the calls that append packed tokens: sequences, packed rows, norm."""
+    T, D, Hkv = packed.n_tokens, cache.head_dim, cache.n_kv_heads
     sq = 0
     if q_raw is not None:
         sq = _token_stride(q_raw, n_layers, T, cache.n_q_heads, D, raw)
@@ -469,11 +511,28 @@ def kvg_norm_append(cache: Cache, seqs: Seqs, packed: Packed, rt: kvg_rotary, no
     sk, sv = (_token_stride(t, n_layers, T, Hkv, D, raw) for t in (k_raw, v_raw))
     ns = None if norm is None else norm.struct(cache, n_layers)
     _on_current_device(cache.k_pool, cache.v_pool, packed.cu_tokens, seqs.block_tables, seqs.ctx_lens, seqs.start_pos, k_raw,
-                       v_raw, q_raw, q_out, *(() if norm is None else (norm.q_weight, norm.k_weight)))
-    _check(_lib.kvg_norm_append(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()),
-                                ctypes.byref(packed.struct(seqs, sq, sk, sv)), ctypes.byref(rt),
-                                None if ns is None else ctypes.byref(ns), layer0, n_layers, _ptr(q_raw), _ptr(k_raw),
-                                _ptr(v_raw), _ptr(q_out), _stream(stream)), "kvg_norm_append")
+                       v_raw, q_raw, q_out, *(() if norm is None else (norm.q_weight, norm.k_weight)), *others)
+    return (ctypes.byref(seqs.struct()), ctypes.byref(packed.struct(seqs, sq, sk, sv)), None if ns is None else ctypes.byref(ns))
+
+
+def kvg_norm_append(cache: Cache, seqs: Seqs, packed: Packed, rt: kvg_rotary, norm: HeadNorm | None, layer0: int,
+                    n_layers: int, q_raw: torch.Tensor | None, k_raw: torch.Tensor, v_raw: torch.Tensor,
+                    q_out: torch.Tensor | None, stream=None):
+    """Norm, rotation and append of packed tokens.  q_raw, k_raw, v_raw: [n_layers][n_tokens][heads][head_dim] of the raw
+    dtype, views into wider rows allowed; q_out: dense (q_raw and q_out: both None for keys and values alone)."""
+    s, p, ns = _append_args(cache, cache.raw_dtype, seqs, packed, norm, n_layers, q_raw, k_raw, v_raw, q_out)
+    _check(_lib.kvg_norm_append(ctypes.byref(cache.struct()), s, p, ctypes.byref(rt), ns, layer0, n_layers, _ptr(q_raw),
+                                _ptr(k_raw), _ptr(v_raw), _ptr(q_out), _stream(stream)), "kvg_norm_append")
+
+
+def kvg_norm_append_axes(cache: Cache, seqs: Seqs, packed: Packed, rt: kvg_rotary, axes: Axes, norm: HeadNorm | None,
+                         layer0: int, n_layers: int, q_raw: torch.Tensor | None, k_raw: torch.Tensor, v_raw: torch.Tensor,
+                         q_out: torch.Tensor | None, stream=None):
+    """kvg_norm_append at positions with several axes (seqs.start_pos is not read)."""
+    s, p, ns = _append_args(cache, cache.raw_dtype, seqs, packed, norm, n_layers, q_raw, k_raw, v_raw, q_out, axes.positions)
+    _check(_lib.kvg_norm_append_axes(ctypes.byref(cache.struct()), s, p, ctypes.byref(rt),
+                                     ctypes.byref(axes.struct(packed.n_tokens)), ns, layer0, n_layers, _ptr(q_raw), _ptr(k_raw),
+                                     _ptr(v_raw), _ptr(q_out), _stream(stream)), "kvg_norm_append_axes")
 
 
 def kvg_packed_attn_workspace_bytes(cache: Cache, seqs: Seqs, packed: Packed, n_layers: int) -> int:
