@@ -76,6 +76,8 @@ typedef enum {
  * E4M3 value is a bf16 value).  A block's payload keeps the cache's bytes, so an fp8 block
  * is half the size of a bf16 one and its graft is the same byte copy. */
 typedef enum { KVG_F32 = 0, KVG_BF16 = 1, KVG_FP8_E4M3 = 2 } kvg_dtype;
+/* storage of a kvg_int8_cache alone: 8-bit integers with a scale for each page and KV head */
+#define KVG_INT8 3
 
 /* Rotary pairing of the D components: HALF pairs i with i + D/2, INTERLEAVED pairs
  * 2i with 2i + 1.  theta_i = base^(-2i/D), i in [0, D/2). */
@@ -496,6 +498,59 @@ int kvg_rotate_axes(const kvg_rotary* rotary, const kvg_axes* axes, int32_t dtyp
 int kvg_norm_append_axes(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, const kvg_rotary* rotary,
                          const kvg_axes* axes, const kvg_head_norm* norm, int32_t layer0, int32_t n_layers,
                          const void* q_raw_dev, const void* k_raw_dev, const void* v_raw_dev, void* q_out_dev, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * Caches of 8-bit integers: a stored value is n * scale, n in [-127, 127], with a scale for the keys and one for the
+ * values of every page (block of 16 tokens) and KV head.  Half the bytes of a bf16 cache, as an fp8 one; for rows without
+ * outliers a third of its rounding (half a step is 1/254 of a block's largest value, where E4M3 rounds each value by up to
+ * 2^-4 of it).  Raw rows, queries and outputs are bf16.  Other entry points refuse such a cache (KVG_E_DTYPE). */
+typedef struct {
+  kvg_cache pages;              /* dtype KVG_INT8 */
+  float* k_scale;               /* device [n_layers][n_pages][n_kv_heads] */
+  float* v_scale;
+} kvg_int8_cache;
+
+/* Norm, rotation and append of packed tokens: kvg_norm_append into an int8 cache (axes: NULL, positions are start_pos[b] + t;
+ * otherwise kvg_norm_append_axes).  For every page that the call's tokens fall into, layer and KV head, with x the new
+ * tokens' (normed, rotated) keys, or their values, in fp32:
+ *   scale <- max(largest |x| / 127, the scale before if the page held tokens of the sequence)
+ *   n <- rint(n * scale before / scale)  for the tokens it held,   n <- rint(x / scale)  for the new ones
+ * so a page's tokens are rounded once, and again when a later call's raise its scale: the bytes depend on where a
+ * sequence was cut into calls, in the pages of the cuts (off by half a step of the scale then more each time).  A block
+ * of zeros has scale 0, scales below 2^-126 are raised to it.  An Inf or NaN among the raw rows makes the
+ * scale of its block NaN, and the rows that see a token of the block NaN, as long as the page holds it.  A sequence's pages are its
+ * own: two sequences that append into one page race.
+ * Errors: as kvg_norm_append and kvg_norm_append_axes; KVG_E_DTYPE (not KVG_INT8), KVG_E_INVAL (scales NULL). */
+int kvg_int8_append(const kvg_int8_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, const kvg_rotary* rotary,
+                    const kvg_axes* axes, const kvg_head_norm* norm, int32_t layer0, int32_t n_layers, const void* q_raw_dev,
+                    const void* k_raw_dev, const void* v_raw_dev, void* q_out_dev, void* stream);
+
+/* Workspace bytes kvg_int8_attn needs: kvg_packed_attn_workspace_bytes for an int8 cache. */
+size_t kvg_int8_attn_workspace_bytes(const kvg_int8_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed,
+                                     int32_t n_layers);
+
+/* kvg_packed_attn over an int8 cache: q_dev and out_dev bf16.  Scores are exact products of the integers with the query
+ * rounded to 15 bits of its head's largest component (two bytes, on the int8 matrix cores); softmax and sums fp32; weights
+ * times the values' scales round to fp16 relative to the row's largest, on the fp16 matrix cores; one rounding of the result.
+ * A row's bytes depend on its own query and the cached integers and scales of the tokens it sees alone.  A query that is not
+ * finite, or a scale of NaN or Inf of a page of which it sees a token, makes a row NaN.
+ * Errors: as kvg_packed_attn; KVG_E_DTYPE (not KVG_INT8), KVG_E_INVAL (scales NULL). */
+int kvg_int8_attn(const kvg_int8_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, int32_t layer0,
+                  int32_t n_layers, const void* q_dev, float scale, void* out_dev, void* ws_dev, size_t ws_bytes, void* stream);
+
+/* Blocks of an int8 cache.  The payload is that of kvg_artifact_hdr with one byte an element, followed by the scales:
+ * [n_layers][2 (K, V)][ceil(n_tokens / page_size)][n_kv_heads] fp32.  Header: dtype KVG_INT8, rope_pairing KVG_ROPE_OTHER
+ * (not to be relocated: it grafts at its own position).  kvg_artifact_seal and kvg_artifact_verify take it like any other. */
+size_t kvg_int8_payload_bytes(const kvg_int8_cache* cache, int32_t n_tokens);
+int kvg_int8_header_init(const kvg_int8_cache* cache, int32_t n_tokens, int64_t own_pos, kvg_artifact_hdr* hdr_out);
+
+/* kvg_deposit and kvg_graft of such a block, byte moves.  kvg_int8_graft sets the scale of a page that the block fills in part
+ * too: rows past the block keep their integers, and stand for other values.  Errors: as kvg_deposit and kvg_graft
+ * (KVG_E_POSITION where target_pos is not the block's own), KVG_E_DTYPE, KVG_E_INVAL (scales NULL). */
+int kvg_int8_deposit(const kvg_int8_cache* cache, const int32_t* block_table_dev, int32_t table_len, int32_t first_token,
+                     int32_t n_tokens, void* payload_dev, void* stream);
+int kvg_int8_graft(const kvg_int8_cache* cache, const kvg_artifact_hdr* hdr, const void* payload,
+                   const int32_t* block_table_dev, int32_t table_len, int32_t first_token, int64_t target_pos, void* stream);
 
 /* ---- Content digests of an artifact (block digests, Sec. 4.11; the paper's deposit-side
  * hashing is closed, Sec. 3.1).  These calls work on any device buffer, typically a

@@ -22,7 +22,8 @@ BUILD = os.path.join(ROOT, "_build")
 KVG_SOURCES = ["kvg_api.cpp", "kvg_api_digest.cpp", "kvg_api_logits.cpp", "kvg_api_noalloc.cpp", "kvg_append.hip",
                "kvg_copy.hip",
                "kvg_attn_valu.hip", "kvg_decode_mfma.hip", "kvg_prefill_mfma.hip", "kvg_prefill_f32.hip", "kvg_digest.hip", "kvg_logits.hip",
-               "kvg_api_packed.cpp", "kvg_rotary.hip", "kvg_packed_mfma.hip", "kvg_packed_few.hip", "kvg_packed_f32.hip"]
+               "kvg_api_packed.cpp", "kvg_rotary.hip", "kvg_packed_mfma.hip", "kvg_packed_few.hip", "kvg_packed_f32.hip",
+               "kvg_api_int8.cpp", "kvg_int8_append.hip", "kvg_int8_tiles.hip", "kvg_int8_few.hip"]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed fp32 VALU instructions are disabled for all device code.
@@ -31,7 +32,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-Wall", "-Wno
 # Per-source extras.  The MFMA prefill keeps its accumulators in VGPRs: left to choose, the
 # register allocator splits them between AGPRs and VGPRs and copies them every key tile.
 EXTRA = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for src in ("kvg_prefill_mfma.hip", "kvg_prefill_f32.hip", "kvg_decode_mfma.hip", "kvg_packed_mfma.hip",
-                                                       "kvg_packed_few.hip", "kvg_packed_f32.hip")}
+                                                       "kvg_packed_few.hip", "kvg_packed_f32.hip", "kvg_int8_tiles.hip",
+                                                       "kvg_int8_few.hip")}
 
 
 def _run(cmd):

@@ -31,7 +31,7 @@ size_t dedup_ws(uint64_t n_leaves) {
 
 // Element bytes of a storage dtype code, 0 for an unknown code.
 size_t dtype_bytes(int32_t dtype) {
-  return dtype == KVG_F32 ? 4 : dtype == KVG_BF16 ? 2 : dtype == KVG_FP8_E4M3 ? 1 : 0;
+  return dtype == KVG_F32 ? 4 : dtype == KVG_BF16 ? 2 : dtype == KVG_FP8_E4M3 || dtype == KVG_INT8 ? 1 : 0;
 }
 
 // Leaf bytes of a header's digest (one page of one KV head), 0 when the geometry is invalid
@@ -44,7 +44,9 @@ uint32_t header_leaf_bytes(const kvg_artifact_hdr* h) {
   const uint64_t leaf = (uint64_t)h->page_size * h->head_dim * e;
   const uint64_t pages = ((uint64_t)h->n_tokens + h->page_size - 1) / h->page_size;
   if (leaf % 64 != 0 || leaf > UINT32_MAX) return 0;
-  if (h->payload_bytes != (uint64_t)h->n_layers * 2 * pages * h->n_kv_heads * leaf) return 0;
+  // an int8 block: the scales of its slabs behind them
+  const uint64_t slab = leaf + (h->dtype == KVG_INT8 ? sizeof(float) : 0);
+  if (h->payload_bytes != (uint64_t)h->n_layers * 2 * pages * h->n_kv_heads * slab) return 0;
   return (uint32_t)leaf;
 }
 

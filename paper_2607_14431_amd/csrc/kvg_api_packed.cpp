@@ -6,23 +6,6 @@ namespace {
 using namespace kvg::host;
 using kvg::fits_grid;
 
-// The tiles' launch, the few kernel's, and the fold of those that are split.
-int attn_launch(kvg::PackedAttnArgs a, const AttnPlan& plan, int32_t dtype, char* ws, hipStream_t stream) {
-  a.few_rows = (int32_t)plan.few_rows;
-  a.n_tiles = (int32_t)plan.n_tiles;
-  kvg::PackedAttnArgs few = a, tiles = a;
-  few.part = {reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + plan.few_ml), plan.few_seg};
-  ws += plan.few_ml + plan.few_acc;
-  tiles.part = {reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + plan.tile_ml), plan.tile_seg};
-  int st = KVG_OK;
-  if (a.n_tiles > 0)
-    st = hip_status(dtype == KVG_F32 ? kvg::launch_packed_f32(tiles, stream) : kvg::launch_packed_tiles(tiles, dtype, stream));
-  if (st == KVG_OK && a.few_rows > 0) st = hip_status(kvg::launch_packed_few(few, dtype, stream));
-  if (st == KVG_OK && (plan.tile_seg > 1 || plan.few_seg > 1))
-    st = hip_status(kvg::launch_packed_fold(tiles, few.part, dtype, stream));
-  return st;
-}
-
 // kvg_rotate, and kvg_rotate_axes (axes given, positions NULL)
 int rotate(const kvg_rotary* rotary, const kvg_axes* axes, int32_t dtype, int32_t head_dim, int32_t n_tokens, int32_t n_heads,
            const int64_t* positions, const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream) {
@@ -59,50 +42,12 @@ int norm_append(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* 
                 const void* k_raw, const void* v_raw, void* q_out, void* stream) {
   int st = check_cache(cache);
   if (st != KVG_OK) return st;
-  if ((st = check_rotary(rotary, cache->head_dim)) != KVG_OK) return st;
-  if ((st = check_layers(cache, layer0, n_layers)) != KVG_OK) return st;
-  if ((st = check_packed(cache, seqs, packed)) != KVG_OK) return st;
-  if (axes != nullptr && (st = check_axes(rotary, cache->head_dim, axes, packed->n_tokens)) != KVG_OK) return st;
-  if (norm != nullptr && (!(norm->eps >= 0.0f) || !std::isfinite(norm->eps) || !std::isfinite(norm->weight_offset)))
-    return KVG_E_INVAL;
   kvg::NormAppendArgs a;
-  std::memset(&a, 0, sizeof(a));
-  const size_t raw = raw_bytes(cache->dtype);
-  const int64_t q_dense = (int64_t)cache->n_q_heads * cache->head_dim, kv_dense = (int64_t)cache->n_kv_heads * cache->head_dim;
-  if ((st = check_stride(packed->q_stride, q_dense, raw, &a.q_stride)) != KVG_OK) return st;
-  if ((st = check_stride(packed->k_stride, kv_dense, raw, &a.k_stride)) != KVG_OK) return st;
-  if ((st = check_stride(packed->v_stride, kv_dense, raw, &a.v_stride)) != KVG_OK) return st;
-  if ((q_raw == nullptr) != (q_out == nullptr)) return KVG_E_INVAL;
-  if (packed->n_tokens == 0 || packed->max_len == 0) return KVG_OK;
-  if (k_raw == nullptr || v_raw == nullptr || (q_raw != nullptr && q_raw == q_out && a.q_stride != q_dense)) return KVG_E_INVAL;
-  const void* w_q = norm != nullptr ? norm->q_weight : nullptr;
-  const void* w_k = norm != nullptr ? norm->k_weight : nullptr;
-  if (!aligned16(q_raw) || !aligned16(k_raw) || !aligned16(v_raw) || !aligned16(q_out) || !aligned16(w_q) || !aligned16(w_k) ||
-      !aligned16(cache->k_pool) || !aligned16(cache->v_pool))
-    return KVG_E_ALIGN;
-  if (!fits_grid(packed->n_tokens, 256)) return KVG_E_SHAPE;
-  a.seqs = packed_seqs(seqs, packed);
-  a.start_pos = seqs->start_pos;
-  a.k_pool = cache->k_pool;
-  a.v_pool = cache->v_pool;
-  a.layer_elems = layer_elems(cache);
-  a.n_pages = cache->n_pages;
-  a.q_raw = q_raw;
-  a.k_raw = k_raw;
-  a.v_raw = v_raw;
-  a.q_out = q_out;
-  a.q_weight = w_q;
-  a.k_weight = w_k;
-  a.eps = norm != nullptr ? norm->eps : 0.0f;
-  a.weight_offset = norm != nullptr ? norm->weight_offset : 0.0f;
-  a.Hq = cache->n_q_heads;
-  a.Hkv = cache->n_kv_heads;
-  a.D = cache->head_dim;
-  a.layer0 = layer0;
-  a.n_layers = n_layers;
-  fill_rotary(rotary, cache->head_dim, &a.rot);
   kvg::AxesArgs turn;
-  if (axes != nullptr) fill_axes(rotary, axes, &a.rot, &turn);
+  bool empty = false;
+  st = append_args(cache, seqs, packed, rotary, axes, norm, layer0, n_layers, q_raw, k_raw, v_raw, q_out, &a, &turn, &empty);
+  if (st != KVG_OK || empty) return st;
+  if (!fits_grid(packed->n_tokens, 256)) return KVG_E_SHAPE;
   return hip_status(kvg::launch_norm_append(a, axes != nullptr ? &turn : nullptr, cache->dtype, static_cast<hipStream_t>(stream)));
 }
 
@@ -158,58 +103,25 @@ int kvg_norm_append_axes(const kvg_cache* cache, const kvg_seqs* seqs, const kvg
 
 size_t kvg_packed_attn_workspace_bytes(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed,
                                        int32_t n_layers) {
-  if (check_cache(cache) != KVG_OK || check_packed(cache, seqs, packed) != KVG_OK || n_layers <= 0 ||
-      n_layers > cache->n_layers)
-    return 0;
-  // whichever layers the call is for
-  size_t most = 0;
-  const bool windowed = cache->layer_window != nullptr;
-  for (int32_t l = 0; l <= (windowed ? cache->n_layers - n_layers : 0); ++l) {
-    const AttnPlan plan = attn_plan(cache, seqs, packed, n_layers, windowed ? cache->layer_window + l : nullptr);
-    if (!plan.fits) return 0;
-    most = std::max(most, plan.total());
-  }
-  return most;
+  return check_cache(cache) == KVG_OK ? attn_workspace_bytes(cache, seqs, packed, n_layers) : 0;
 }
 
 int kvg_packed_attn(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, int32_t layer0, int32_t n_layers,
                     const void* q, float scale, void* out, void* ws, size_t ws_bytes, void* stream) {
   int st = check_cache(cache);
   if (st != KVG_OK) return st;
-  if ((st = check_layers(cache, layer0, n_layers)) != KVG_OK) return st;
-  if ((st = check_packed(cache, seqs, packed)) != KVG_OK) return st;
-  const float scale_log2 = scale * 1.4426950408889634f;
-  if (!(scale > 0.0f) || !std::isfinite(scale_log2)) return KVG_E_INVAL;      // scores go in log2 units
   kvg::PackedAttnArgs a;
-  std::memset(&a, 0, sizeof(a));
-  if ((st = check_stride(packed->q_stride, (int64_t)cache->n_q_heads * cache->head_dim, raw_bytes(cache->dtype),
-                         &a.q_stride)) != KVG_OK)
-    return st;
-  if ((st = fill_windows(cache, layer0, n_layers, a.window)) != KVG_OK) return st;
-  // the caller's array, as the size query reads it: a launch carries kMaxWindowLayers windows, a call without any may
-  // have more layers
-  const AttnPlan plan = attn_plan(cache, seqs, packed, n_layers, cache->layer_window != nullptr ? cache->layer_window + layer0 : nullptr);
-  if (!plan.fits || !fits_grid(packed->n_tokens, 256)) return KVG_E_SHAPE;
-  if (ws == nullptr || ws_bytes < plan.total()) return KVG_E_WORKSPACE;
-  if (packed->n_tokens == 0 || packed->max_len == 0) return KVG_OK;
-  if (q == nullptr || out == nullptr || q == out) return KVG_E_INVAL;
-  if (!aligned16(q) || !aligned16(out) || !aligned16(ws) || !aligned16(cache->k_pool) || !aligned16(cache->v_pool))
-    return KVG_E_ALIGN;
-  a.seqs = packed_seqs(seqs, packed);
-  a.k_pool = cache->k_pool;
-  a.v_pool = cache->v_pool;
-  a.layer_elems = layer_elems(cache);
-  a.n_pages = cache->n_pages;
-  a.q = q;
-  a.out = out;
-  a.scale_log2 = scale_log2;
-  a.Hq = cache->n_q_heads;
-  a.Hkv = cache->n_kv_heads;
-  a.D = cache->head_dim;
-  a.group = cache->n_q_heads / cache->n_kv_heads;
-  a.layer0 = layer0;
-  a.n_layers = n_layers;
-  return attn_launch(a, plan, cache->dtype, static_cast<char*>(ws), static_cast<hipStream_t>(stream));
+  AttnPlan plan;
+  bool empty = false;
+  st = attn_args(cache, seqs, packed, layer0, n_layers, q, scale, out, ws, ws_bytes, &a, &plan, &empty);
+  if (st != KVG_OK || empty) return st;
+  const int32_t dtype = cache->dtype;
+  return attn_launch(
+      a, plan, dtype, static_cast<char*>(ws), static_cast<hipStream_t>(stream),
+      [dtype](const kvg::PackedAttnArgs& t, hipStream_t s) {
+        return dtype == KVG_F32 ? kvg::launch_packed_f32(t, s) : kvg::launch_packed_tiles(t, dtype, s);
+      },
+      [dtype](const kvg::PackedAttnArgs& t, hipStream_t s) { return kvg::launch_packed_few(t, dtype, s); });
 }
 
 }  // extern "C"

@@ -15,7 +15,9 @@ constexpr size_t kAlign = 256;
 
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
-inline size_t elem_bytes(const kvg_cache* c) { return c->dtype == KVG_BF16 ? 2 : c->dtype == KVG_FP8_E4M3 ? 1 : 4; }
+inline size_t elem_bytes(const kvg_cache* c) {
+  return c->dtype == KVG_BF16 ? 2 : c->dtype == KVG_FP8_E4M3 || c->dtype == KVG_INT8 ? 1 : 4;
+}
 
 inline int check_cache(const kvg_cache* c) {
   if (c == nullptr || c->k_pool == nullptr || c->v_pool == nullptr) return KVG_E_INVAL;
@@ -31,6 +33,16 @@ inline int check_cache(const kvg_cache* c) {
     for (int l = 0; l < c->n_layers; ++l)
       if (c->layer_window[l] < 0) return KVG_E_INVAL;
   return KVG_OK;
+}
+
+inline int check_int8_cache(const kvg_int8_cache* c) {
+  if (c == nullptr) return KVG_E_INVAL;
+  kvg_cache pages = c->pages;
+  if (pages.dtype != KVG_INT8) return KVG_E_DTYPE;
+  pages.dtype = KVG_FP8_E4M3;              // the same geometry
+  const int st = check_cache(&pages);
+  if (st != KVG_OK) return st;
+  return c->k_scale != nullptr && c->v_scale != nullptr ? KVG_OK : KVG_E_INVAL;
 }
 
 // Windows of layers [layer0, layer0 + n_layers) as a launch carries them (all zero when none

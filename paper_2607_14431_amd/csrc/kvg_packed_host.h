@@ -234,5 +234,131 @@ inline AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packe
   return r;
 }
 
+// The checks of an append to `cache` (checked by the caller) and its launch's arguments; *empty: nothing to do.
+inline int append_args(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, const kvg_rotary* rotary,
+                       const kvg_axes* axes, const kvg_head_norm* norm, int32_t layer0, int32_t n_layers, const void* q_raw,
+                       const void* k_raw, const void* v_raw, void* q_out, kvg::NormAppendArgs* out, kvg::AxesArgs* turn, bool* empty) {
+  int st;
+  if ((st = check_rotary(rotary, cache->head_dim)) != KVG_OK) return st;
+  if ((st = check_layers(cache, layer0, n_layers)) != KVG_OK) return st;
+  if ((st = check_packed(cache, seqs, packed)) != KVG_OK) return st;
+  if (axes != nullptr && (st = check_axes(rotary, cache->head_dim, axes, packed->n_tokens)) != KVG_OK) return st;
+  if (norm != nullptr && (!(norm->eps >= 0.0f) || !std::isfinite(norm->eps) || !std::isfinite(norm->weight_offset)))
+    return KVG_E_INVAL;
+  kvg::NormAppendArgs& a = *out;
+  std::memset(&a, 0, sizeof(a));
+  const size_t raw = raw_bytes(cache->dtype);
+  const int64_t q_dense = (int64_t)cache->n_q_heads * cache->head_dim, kv_dense = (int64_t)cache->n_kv_heads * cache->head_dim;
+  if ((st = check_stride(packed->q_stride, q_dense, raw, &a.q_stride)) != KVG_OK) return st;
+  if ((st = check_stride(packed->k_stride, kv_dense, raw, &a.k_stride)) != KVG_OK) return st;
+  if ((st = check_stride(packed->v_stride, kv_dense, raw, &a.v_stride)) != KVG_OK) return st;
+  if ((q_raw == nullptr) != (q_out == nullptr)) return KVG_E_INVAL;
+  *empty = packed->n_tokens == 0 || packed->max_len == 0;
+  if (*empty) return KVG_OK;
+  if (k_raw == nullptr || v_raw == nullptr || (q_raw != nullptr && q_raw == q_out && a.q_stride != q_dense)) return KVG_E_INVAL;
+  const void* w_q = norm != nullptr ? norm->q_weight : nullptr;
+  const void* w_k = norm != nullptr ? norm->k_weight : nullptr;
+  if (!aligned16(q_raw) || !aligned16(k_raw) || !aligned16(v_raw) || !aligned16(q_out) || !aligned16(w_q) || !aligned16(w_k) ||
+      !aligned16(cache->k_pool) || !aligned16(cache->v_pool))
+    return KVG_E_ALIGN;
+  a.seqs = packed_seqs(seqs, packed);
+  a.start_pos = seqs->start_pos;
+  a.k_pool = cache->k_pool;
+  a.v_pool = cache->v_pool;
+  a.layer_elems = layer_elems(cache);
+  a.n_pages = cache->n_pages;
+  a.q_raw = q_raw;
+  a.k_raw = k_raw;
+  a.v_raw = v_raw;
+  a.q_out = q_out;
+  a.q_weight = w_q;
+  a.k_weight = w_k;
+  a.eps = norm != nullptr ? norm->eps : 0.0f;
+  a.weight_offset = norm != nullptr ? norm->weight_offset : 0.0f;
+  a.Hq = cache->n_q_heads;
+  a.Hkv = cache->n_kv_heads;
+  a.D = cache->head_dim;
+  a.layer0 = layer0;
+  a.n_layers = n_layers;
+  fill_rotary(rotary, cache->head_dim, &a.rot);
+  if (axes != nullptr) fill_axes(rotary, axes, &a.rot, turn);
+  return KVG_OK;
+}
+
+// Workspace bytes of a call, whichever n_layers layers it is for.
+inline size_t attn_workspace_bytes(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, int32_t n_layers) {
+  if (check_packed(cache, seqs, packed) != KVG_OK || n_layers <= 0 || n_layers > cache->n_layers) return 0;
+  size_t most = 0;
+  const bool windowed = cache->layer_window != nullptr;
+  for (int32_t l = 0; l <= (windowed ? cache->n_layers - n_layers : 0); ++l) {
+    const AttnPlan plan = attn_plan(cache, seqs, packed, n_layers, windowed ? cache->layer_window + l : nullptr);
+    if (!plan.fits) return 0;
+    most = std::max(most, plan.total());
+  }
+  return most;
+}
+
+// The checks of an attention call over `cache` (checked by the caller), its plan and its launches' arguments; *empty: nothing to
+// do.
+inline int attn_args(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, int32_t layer0, int32_t n_layers,
+                     const void* q, float scale, void* out, void* ws, size_t ws_bytes, kvg::PackedAttnArgs* args, AttnPlan* plan_out,
+                     bool* empty) {
+  int st;
+  if ((st = check_layers(cache, layer0, n_layers)) != KVG_OK) return st;
+  if ((st = check_packed(cache, seqs, packed)) != KVG_OK) return st;
+  const float scale_log2 = scale * 1.4426950408889634f;
+  if (!(scale > 0.0f) || !std::isfinite(scale_log2)) return KVG_E_INVAL;      // scores go in log2 units
+  kvg::PackedAttnArgs& a = *args;
+  std::memset(&a, 0, sizeof(a));
+  if ((st = check_stride(packed->q_stride, (int64_t)cache->n_q_heads * cache->head_dim, raw_bytes(cache->dtype),
+                         &a.q_stride)) != KVG_OK)
+    return st;
+  if ((st = fill_windows(cache, layer0, n_layers, a.window)) != KVG_OK) return st;
+  // the caller's array, as the size query reads it: a launch carries kMaxWindowLayers windows, a call without any may
+  // have more layers
+  const AttnPlan plan = *plan_out = attn_plan(cache, seqs, packed, n_layers, cache->layer_window != nullptr ? cache->layer_window + layer0 : nullptr);
+  if (!plan.fits || !fits_grid(packed->n_tokens, 256)) return KVG_E_SHAPE;
+  if (ws == nullptr || ws_bytes < plan.total()) return KVG_E_WORKSPACE;
+  *empty = packed->n_tokens == 0 || packed->max_len == 0;
+  if (*empty) return KVG_OK;
+  if (q == nullptr || out == nullptr || q == out) return KVG_E_INVAL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(ws) || !aligned16(cache->k_pool) || !aligned16(cache->v_pool))
+    return KVG_E_ALIGN;
+  a.seqs = packed_seqs(seqs, packed);
+  a.k_pool = cache->k_pool;
+  a.v_pool = cache->v_pool;
+  a.layer_elems = layer_elems(cache);
+  a.n_pages = cache->n_pages;
+  a.q = q;
+  a.out = out;
+  a.scale_log2 = scale_log2;
+  a.Hq = cache->n_q_heads;
+  a.Hkv = cache->n_kv_heads;
+  a.D = cache->head_dim;
+  a.group = cache->n_q_heads / cache->n_kv_heads;
+  a.layer0 = layer0;
+  a.n_layers = n_layers;
+  return KVG_OK;
+}
+
+// The tiles' launch, the few kernel's, and the fold of those that are split; launch_tiles(args, stream) and launch_few(args,
+// stream) are the cache's.
+template <typename Tiles, typename Few>
+int attn_launch(kvg::PackedAttnArgs a, const AttnPlan& plan, int32_t dtype, char* ws, hipStream_t stream, Tiles launch_tiles,
+                Few launch_few) {
+  a.few_rows = (int32_t)plan.few_rows;
+  a.n_tiles = (int32_t)plan.n_tiles;
+  kvg::PackedAttnArgs few = a, tiles = a;
+  few.part = {reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + plan.few_ml), plan.few_seg};
+  ws += plan.few_ml + plan.few_acc;
+  tiles.part = {reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + plan.tile_ml), plan.tile_seg};
+  int st = KVG_OK;
+  if (a.n_tiles > 0) st = hip_status(launch_tiles(tiles, stream));
+  if (st == KVG_OK && a.few_rows > 0) st = hip_status(launch_few(few, stream));
+  if (st == KVG_OK && (plan.tile_seg > 1 || plan.few_seg > 1))
+    st = hip_status(kvg::launch_packed_fold(tiles, few.part, dtype, stream));
+  return st;
+}
+
 }  // namespace host
 }  // namespace kvg

@@ -19,7 +19,7 @@ if not os.path.exists(LIB_PATH):
                       "(there is no fallback path)")
 _lib = ctypes.CDLL(LIB_PATH)
 
-KVG_F32, KVG_BF16, KVG_FP8_E4M3 = 0, 1, 2
+KVG_F32, KVG_BF16, KVG_FP8_E4M3, KVG_INT8 = 0, 1, 2, 3
 KVG_ROPE_HALF, KVG_ROPE_INTERLEAVED, KVG_ROPE_OTHER = 0, 1, 2
 KVG_GRAFT_ALLOW_RELOCATE = 1
 KVG_ROTARY_PLAIN, KVG_ROTARY_LINEAR, KVG_ROTARY_BASE, KVG_ROTARY_ROTATIONS, KVG_ROTARY_INDEX = range(5)
@@ -50,6 +50,10 @@ class kvg_cache(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("n_pages", ctypes.c_int64), ("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p),
                 ("layer_window", ctypes.POINTER(ctypes.c_int32))]
+
+
+class kvg_int8_cache(ctypes.Structure):
+    _fields_ = [("pages", kvg_cache), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
 class kvg_seqs(ctypes.Structure):
@@ -123,6 +127,15 @@ _SIGS = {
     "kvg_packed_attn_workspace_bytes": (_sz, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_packed), _i32]),
     "kvg_packed_attn": (ctypes.c_int, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_packed), _i32, _i32, _vp, _f32, _vp, _vp, _sz,
                                        _vp]),
+    "kvg_int8_append": (ctypes.c_int, [_P(kvg_int8_cache), _P(kvg_seqs), _P(kvg_packed), _P(kvg_rotary), _P(kvg_axes),
+                                       _P(kvg_head_norm), _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
+    "kvg_int8_attn_workspace_bytes": (_sz, [_P(kvg_int8_cache), _P(kvg_seqs), _P(kvg_packed), _i32]),
+    "kvg_int8_attn": (ctypes.c_int, [_P(kvg_int8_cache), _P(kvg_seqs), _P(kvg_packed), _i32, _i32, _vp, _f32, _vp, _vp, _sz,
+                                     _vp]),
+    "kvg_int8_payload_bytes": (_sz, [_P(kvg_int8_cache), _i32]),
+    "kvg_int8_header_init": (ctypes.c_int, [_P(kvg_int8_cache), _i32, _i64, _P(kvg_artifact_hdr)]),
+    "kvg_int8_deposit": (ctypes.c_int, [_P(kvg_int8_cache), _vp, _i32, _i32, _i32, _vp, _vp]),
+    "kvg_int8_graft": (ctypes.c_int, [_P(kvg_int8_cache), _P(kvg_artifact_hdr), _vp, _vp, _i32, _i32, _i64, _vp]),
     "kvg_leaf_digests": (ctypes.c_int, [_vp, _u64, ctypes.c_uint32, _vp, _vp]),
     "kvg_merkle_workspace_bytes": (_sz, [_u64]),
     "kvg_merkle_root": (ctypes.c_int, [_vp, _u64, _vp, _vp, _sz, _vp]),
@@ -175,6 +188,22 @@ def rope(base: float = 10000.0, pairing: int = KVG_ROPE_HALF) -> kvg_rope:
 _DTYPE_CODE = {torch.float32: KVG_F32, torch.bfloat16: KVG_BF16, torch.float8_e4m3fn: KVG_FP8_E4M3}
 
 
+def _pages_struct(k: torch.Tensor, v: torch.Tensor, n_q_heads: int, code: int, windows) -> kvg_cache:
+    """The struct of two paged pools."""
+    shape = k.shape
+    if not (k.is_contiguous() and v.is_contiguous() and shape == v.shape and k.dtype == v.dtype):
+        raise ValueError("pools: contiguous, of one shape and type")
+    n_layers, n_pages, n_kv_heads, page_size, head_dim = shape
+    c = kvg_cache(n_layers, n_q_heads, n_kv_heads, head_dim, page_size, code, n_pages, k.data_ptr(), v.data_ptr(), None)
+    if windows is not None and any(windows):
+        if len(windows) != n_layers:
+            raise ValueError("windows: one per layer")
+        arr = (ctypes.c_int32 * len(windows))(*windows)
+        c.layer_window = ctypes.cast(arr, ctypes.POINTER(ctypes.c_int32))
+        c._windows_keepalive = arr        # the struct holds a raw pointer into this array
+    return c
+
+
 @dataclasses.dataclass
 class Cache:
     """Paged pools [n_layers][n_pages][n_kv_heads][page_size][head_dim] (torch tensors)."""
@@ -225,20 +254,7 @@ class Cache:
         return torch.bfloat16 if dtype is torch.float8_e4m3fn else dtype
 
     def struct(self) -> kvg_cache:
-        k, v = self.k_pool, self.v_pool
-        shape, dtype = k.shape, k.dtype
-        if not (k.is_contiguous() and v.is_contiguous() and shape == v.shape and dtype == v.dtype):
-            raise ValueError("pools: contiguous, of one shape and type")
-        n_layers, n_pages, n_kv_heads, page_size, head_dim = shape
-        c = kvg_cache(n_layers, self.n_q_heads, n_kv_heads, head_dim, page_size, _DTYPE_CODE[dtype], n_pages,
-                      k.data_ptr(), v.data_ptr(), None)
-        if self.windows is not None and any(self.windows):
-            if len(self.windows) != n_layers:
-                raise ValueError("windows: one per layer")
-            arr = (ctypes.c_int32 * len(self.windows))(*self.windows)
-            c.layer_window = ctypes.cast(arr, ctypes.POINTER(ctypes.c_int32))
-            c._windows_keepalive = arr        # the struct holds a raw pointer into this array
-        return c
+        return _pages_struct(self.k_pool, self.v_pool, self.n_q_heads, _DTYPE_CODE[self.k_pool.dtype], self.windows)
 
 
 @dataclasses.dataclass
@@ -560,6 +576,140 @@ def kvg_packed_attn(cache: Cache, seqs: Seqs, packed: Packed, layer0: int, n_lay
     _check(_lib.kvg_packed_attn(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()),
                                 ctypes.byref(packed.struct(seqs, sq)), layer0, n_layers, _ptr(q), scale, _ptr(out),
                                 _ptr(ws), ws.nbytes, _stream(stream)), "kvg_packed_attn")
+
+
+@dataclasses.dataclass
+class Int8Cache:
+    """Paged pools of 8-bit integers [n_layers][n_pages][n_kv_heads][page_size][head_dim] (torch.int8) and the scale of every page and
+    KV head, fp32 [n_layers][n_pages][n_kv_heads]: a value is its integer times its scale."""
+    k_pool: torch.Tensor
+    v_pool: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    n_q_heads: int
+    windows: tuple | None = None       # per-layer sliding window (0 = full causal), or None
+
+    @staticmethod
+    def allocate(n_layers, n_pages, n_q_heads, n_kv_heads, head_dim, device="cuda", page_size=16, windows=None):
+        pages = Cache.allocate(n_layers, n_pages, n_q_heads, n_kv_heads, head_dim, torch.int8, device, page_size, windows)
+        scales = [torch.empty((n_layers, n_pages, n_kv_heads), dtype=torch.float32, device=device) for _ in range(2)]
+        return Int8Cache(pages.k_pool, pages.v_pool, *scales, n_q_heads, pages.windows)
+
+    @property
+    def n_layers(self):
+        return self.k_pool.shape[0]
+
+    @property
+    def n_pages(self):
+        return self.k_pool.shape[1]
+
+    @property
+    def n_kv_heads(self):
+        return self.k_pool.shape[2]
+
+    @property
+    def page_size(self):
+        return self.k_pool.shape[3]
+
+    @property
+    def head_dim(self):
+        return self.k_pool.shape[4]
+
+    @property
+    def raw_dtype(self) -> torch.dtype:
+        return torch.bfloat16
+
+    def struct(self) -> kvg_int8_cache:
+        k, v, ks, vs = self.k_pool, self.v_pool, self.k_scale, self.v_scale
+        if k.dtype is not torch.int8:
+            raise ValueError("pools: torch.int8")
+        shape = k.shape[:3]
+        if not (ks.dtype is vs.dtype is torch.float32 and ks.shape == vs.shape == shape and ks.is_contiguous() and
+                vs.is_contiguous()):
+            raise ValueError("scales: fp32 [n_layers][n_pages][n_kv_heads], contiguous")
+        pages = _pages_struct(k, v, self.n_q_heads, KVG_INT8, self.windows)
+        c = kvg_int8_cache(pages, ks.data_ptr(), vs.data_ptr())
+        c._windows_keepalive = getattr(pages, "_windows_keepalive", None)     # the copy holds the raw pointer too
+        return c
+
+    def tensors(self):
+        return self.k_pool, self.v_pool, self.k_scale, self.v_scale
+
+
+def kvg_int8_append(cache: Int8Cache, seqs: Seqs, packed: Packed, rt: kvg_rotary, norm: HeadNorm | None, layer0: int,
+                    n_layers: int, q_raw: torch.Tensor | None, k_raw: torch.Tensor, v_raw: torch.Tensor,
+                    q_out: torch.Tensor | None, axes: Axes | None = None, stream=None):
+    """Norm, rotation and append of packed tokens to an int8 cache; rows as kvg_norm_append's, bf16.  axes: positions with
+    several axes in the place of seqs.start_pos + index."""
+    s, p, ns = _append_args(cache, torch.bfloat16, seqs, packed, norm, n_layers, q_raw, k_raw, v_raw, q_out, cache.k_scale,
+                            cache.v_scale, None if axes is None else axes.positions)
+    _check(_lib.kvg_int8_append(ctypes.byref(cache.struct()), s, p, ctypes.byref(rt),
+                                None if axes is None else ctypes.byref(axes.struct(packed.n_tokens)), ns, layer0, n_layers,
+                                _ptr(q_raw), _ptr(k_raw), _ptr(v_raw), _ptr(q_out), _stream(stream)), "kvg_int8_append")
+
+
+def kvg_int8_attn_workspace_bytes(cache: Int8Cache, seqs: Seqs, packed: Packed, n_layers: int) -> int:
+    return _lib.kvg_int8_attn_workspace_bytes(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()),
+                                              ctypes.byref(packed.struct(seqs)), n_layers)
+
+
+def int8_attn_workspace(cache: Int8Cache, seqs: Seqs, packed: Packed, n_layers: int) -> torch.Tensor:
+    """Scratch for kvg_int8_attn calls of this batch's bounds."""
+    return torch.empty(max(kvg_int8_attn_workspace_bytes(cache, seqs, packed, n_layers), 256), dtype=torch.uint8,
+                       device=cache.k_pool.device)
+
+
+def kvg_int8_attn(cache: Int8Cache, seqs: Seqs, packed: Packed, layer0: int, n_layers: int, q: torch.Tensor, scale: float,
+                  out: torch.Tensor, ws: torch.Tensor, stream=None):
+    """kvg_packed_attn over an int8 cache.  q: bf16 [n_layers][n_tokens][n_q_heads][head_dim], rotated, any token stride;
+    out: the same, dense."""
+    T, D, Hq = packed.n_tokens, cache.head_dim, cache.n_q_heads
+    sq = _token_stride(q, n_layers, T, Hq, D, torch.bfloat16)
+    if not (out.shape == (n_layers, T, Hq, D) and out.dtype is torch.bfloat16 and out.is_contiguous()):
+        raise ValueError("out: bf16 [n_layers][n_tokens][n_q_heads][head_dim], contiguous")
+    if not ws.is_contiguous():
+        raise ValueError("ws: contiguous")
+    _on_current_device(*cache.tensors(), packed.cu_tokens, seqs.block_tables, seqs.ctx_lens, q, out, ws)
+    _check(_lib.kvg_int8_attn(ctypes.byref(cache.struct()), ctypes.byref(seqs.struct()), ctypes.byref(packed.struct(seqs, sq)),
+                              layer0, n_layers, _ptr(q), scale, _ptr(out), _ptr(ws), ws.nbytes, _stream(stream)),
+           "kvg_int8_attn")
+
+
+def kvg_int8_payload_bytes(cache: Int8Cache, n_tokens: int) -> int:
+    return _lib.kvg_int8_payload_bytes(ctypes.byref(cache.struct()), n_tokens)
+
+
+def kvg_int8_header_init(cache: Int8Cache, n_tokens: int, own_pos: int) -> kvg_artifact_hdr:
+    hdr = kvg_artifact_hdr()
+    _check(_lib.kvg_int8_header_init(ctypes.byref(cache.struct()), n_tokens, own_pos, ctypes.byref(hdr)), "kvg_int8_header_init")
+    return hdr
+
+
+def _block_table(row: torch.Tensor):
+    if not (row.dtype is torch.int32 and row.is_contiguous()):
+        raise ValueError("block table: int32, contiguous")
+
+
+def kvg_int8_deposit(cache: Int8Cache, block_table_row: torch.Tensor, first_token: int, n_tokens: int, payload: torch.Tensor,
+                     stream=None):
+    """kvg_deposit of an int8 block: its integers, then its scales."""
+    _block_table(block_table_row)
+    if not payload.is_contiguous() or payload.nbytes < kvg_int8_payload_bytes(cache, n_tokens):
+        raise ValueError("payload: kvg_int8_payload_bytes(cache, n_tokens) bytes, contiguous")
+    _on_current_device(*cache.tensors(), block_table_row)
+    _check(_lib.kvg_int8_deposit(ctypes.byref(cache.struct()), _ptr(block_table_row), block_table_row.numel(), first_token,
+                                 n_tokens, _ptr(payload), _stream(stream)), "kvg_int8_deposit")
+
+
+def kvg_int8_graft(cache: Int8Cache, hdr: kvg_artifact_hdr, payload, block_table_row: torch.Tensor, first_token: int,
+                   target_pos: int, stream=None):
+    """kvg_graft of an int8 block, at its own position."""
+    _block_table(block_table_row)
+    if payload.nbytes < hdr.payload_bytes:
+        raise ValueError("payload: the header's payload_bytes")
+    _on_current_device(*cache.tensors(), block_table_row)
+    _check(_lib.kvg_int8_graft(ctypes.byref(cache.struct()), ctypes.byref(hdr), _payload_ptr(payload), _ptr(block_table_row),
+                               block_table_row.numel(), first_token, target_pos, _stream(stream)), "kvg_int8_graft")
 
 
 def kvg_leaf_digests(data: torch.Tensor, leaf_bytes: int, digests: torch.Tensor, n_bytes: int | None = None,
