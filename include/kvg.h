@@ -633,6 +633,35 @@ int kvg_logits(const float* hidden_dev, int32_t rows, int32_t hidden, const uint
 int kvg_logit_compare(const float* a_dev, const float* b_dev, int32_t rows, int32_t vocab, double* kl_dev,
                       int32_t* argmax_a_dev, int32_t* argmax_b_dev, void* stream);
 
+/* ---------------------------------------------------------------------------------
+ * Sampling: the next tokens of a batch from its logits and given random numbers.  Per row, every array NULL-able but
+ * temperature; all device, so a captured call replays with other values. */
+typedef struct {
+  const float* temperature;     /* [rows] > 0, or 0: the first maximum, whatever the filters */
+  const int32_t* top_k;         /* [rows]; <= 0: no limit */
+  const float* top_p;           /* [rows]; >= 1: no limit */
+  const float* min_p;           /* [rows]; <= 0: no limit, above 1 as 1 */
+} kvg_sampling;
+
+/* Workspace bytes kvg_sample needs (0 on bad args). */
+size_t kvg_sample_workspace_bytes(int32_t rows, int32_t vocab);
+
+/* tokens_dev[r] (int32): with e_i = exp((l_i - max l) / temperature), among
+ *   the top_k likeliest tokens (of equal logits the lowest index first),
+ *   of these the fewest, from the likeliest on, whose sum is at least top_p of their sum (one at least),
+ *   of these the ones with e_i >= min_p (min_p of the likeliest's probability),
+ * the first, in the order of their index, whose running sum of e exceeds uniform_dev[r] (fp64, [0, 1)) of the total.
+ * logprobs_dev (fp32 or NULL): the log of its share of that total (0 for a temperature of 0).  Differences, exponentials
+ * and comparisons are fp64; sums are of e rounded to fixed point with 62 - ceil(log2 vocab) bits after the point, so that
+ * they have no order: equal inputs give equal tokens whatever the batch.
+ * A logit of -Inf has weight 0.  A row without a finite logit or with one of NaN or +Inf, a temperature that is negative or not
+ * finite, and a top_p, min_p or random number of NaN give token -1 and NaN.  Random numbers outside [0, 1) count as its ends.
+ * logits_dev: fp32, row r at r * row_stride (0: vocab).  ws_dev: kvg_sample_workspace_bytes() bytes, nothing kept in it.
+ * Errors: KVG_E_INVAL (NULL, rows < 0, vocab <= 0, stride below vocab), KVG_E_SHAPE (vocab above 2^24, rows above 65,535),
+ * KVG_E_ALIGN (ws_dev not on 16 bytes), KVG_E_WORKSPACE, KVG_E_HIP. */
+int kvg_sample(const float* logits_dev, int64_t row_stride, int32_t rows, int32_t vocab, const kvg_sampling* sampling,
+               const double* uniform_dev, int32_t* tokens_dev, float* logprobs_dev, void* ws_dev, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

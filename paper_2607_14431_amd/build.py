@@ -23,7 +23,8 @@ KVG_SOURCES = ["kvg_api.cpp", "kvg_api_digest.cpp", "kvg_api_logits.cpp", "kvg_a
                "kvg_copy.hip",
                "kvg_attn_valu.hip", "kvg_decode_mfma.hip", "kvg_prefill_mfma.hip", "kvg_prefill_f32.hip", "kvg_digest.hip", "kvg_logits.hip",
                "kvg_api_packed.cpp", "kvg_rotary.hip", "kvg_packed_mfma.hip", "kvg_packed_few.hip", "kvg_packed_f32.hip",
-               "kvg_api_int8.cpp", "kvg_int8_append.hip", "kvg_int8_tiles.hip", "kvg_int8_few.hip"]
+               "kvg_api_int8.cpp", "kvg_int8_append.hip", "kvg_int8_tiles.hip", "kvg_int8_few.hip",
+               "kvg_api_sample.cpp", "kvg_sample.hip"]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed fp32 VALU instructions are disabled for all device code.

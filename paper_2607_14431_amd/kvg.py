@@ -84,6 +84,11 @@ class kvg_axes(ctypes.Structure):
                 ("own_frequencies", ctypes.c_int32), ("reserved", ctypes.c_int32), ("pairs", ctypes.c_int32 * 4)]
 
 
+class kvg_sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p),
+                ("min_p", ctypes.c_void_p)]
+
+
 class kvg_artifact_hdr(ctypes.Structure):
     _fields_ = [("magic", ctypes.c_uint32), ("version", ctypes.c_uint32), ("dtype", ctypes.c_int32),
                 ("n_layers", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
@@ -145,6 +150,8 @@ _SIGS = {
     "kvg_logits_pack": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp]),
     "kvg_logits_workspace_bytes": (_sz, [_i32, _i32]),
     "kvg_logits": (ctypes.c_int, [_vp, _i32, _i32, _vp, _i32, _f32, _vp, _vp, _sz, _vp]),
+    "kvg_sample_workspace_bytes": (_sz, [_i32, _i32]),
+    "kvg_sample": (ctypes.c_int, [_vp, _i64, _i32, _i32, _P(kvg_sampling), _vp, _vp, _vp, _vp, _sz, _vp]),
     "kvg_logit_compare": (ctypes.c_int, [_vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -777,6 +784,39 @@ def kvg_logit_compare(a: torch.Tensor, b: torch.Tensor, kl: torch.Tensor, argmax
         raise ValueError("kl: fp64 [rows]; argmax_a, argmax_b: int32 [rows]")
     _check(_lib.kvg_logit_compare(_ptr(a), _ptr(b), rows, V, _ptr(kl), _ptr(argmax_a), _ptr(argmax_b),
                                   _stream(stream)), "kvg_logit_compare")
+
+
+def kvg_sample_workspace_bytes(rows: int, vocab: int) -> int:
+    return _lib.kvg_sample_workspace_bytes(rows, vocab)
+
+
+def sample_workspace(rows: int, vocab: int, device="cuda") -> torch.Tensor:
+    """Scratch for kvg_sample calls of these sizes."""
+    return torch.empty(max(kvg_sample_workspace_bytes(rows, vocab), 256), dtype=torch.uint8, device=device)
+
+
+def kvg_sample(logits: torch.Tensor, temperature: torch.Tensor, uniform: torch.Tensor, tokens: torch.Tensor, ws: torch.Tensor,
+               top_k: torch.Tensor | None = None, top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None,
+               logprobs: torch.Tensor | None = None, stream=None):
+    """tokens (int32 [rows]) sampled from logits (fp32 [rows][vocab], any row stride) with one random number a row (uniform: fp64 [rows]);
+    temperature, top_p, min_p: fp32 [rows], top_k: int32 [rows] (None: no such limit); logprobs: fp32 [rows] or None."""
+    rows, V = logits.shape
+    if logits.dtype is not torch.float32 or V > 1 and logits.stride(1) != 1:
+        raise ValueError("logits: fp32 [rows][vocab], rows dense")
+    stride = logits.stride(0) if rows > 1 else V
+    if stride < V:                         # a broadcast row among them: 0 is the library's word for dense rows
+        raise ValueError("logits: a row overlaps the next one")
+    for name, t, dtype in (("temperature", temperature, torch.float32), ("uniform", uniform, torch.float64),
+                           ("tokens", tokens, torch.int32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                           ("min_p", min_p, torch.float32), ("logprobs", logprobs, torch.float32)):
+        if t is not None and not (t.dtype is dtype and t.shape == (rows,) and t.is_contiguous()):
+            raise ValueError(f"{name}: {dtype} [rows], contiguous")
+    if not ws.is_contiguous():
+        raise ValueError("ws: contiguous")
+    _on_current_device(logits, temperature, uniform, tokens, ws, top_k, top_p, min_p, logprobs)
+    s = kvg_sampling(_ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p))
+    _check(_lib.kvg_sample(_ptr(logits), stride, rows, V, ctypes.byref(s), _ptr(uniform), _ptr(tokens), _ptr(logprobs), _ptr(ws),
+                           ws.nbytes, _stream(stream)), "kvg_sample")
 
 
 def raw_call(name: str, *args):
