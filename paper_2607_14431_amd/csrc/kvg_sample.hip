@@ -7,8 +7,14 @@
 // of weights reaches its share, min-p at a weight.  So what is kept is `code >= cut && e^x >= min_p`, and the token is the first in
 // index order whose running sum of kept weights passes the random number's.
 //
-// A workgroup takes a row.  A cut is found digit by digit (11, 11, 10 bits of the logit, twice 12 of the index): count and weight
-// of the tokens that share the digits so far, by their next digit.
+// Rows of up to kSampleListed tokens: a workgroup sorts the row's codes.  Longer ones in passes over the row, by many workgroups:
+//   top     the largest logit of every part of the row
+//   bins    count and weight of the row's tokens by weight (1,024 equal steps of the exponent down to weight 0), where a top-k or
+//           top-p may end inside the row.  The bins tell in which of them the two limits end
+//   parts   the weight of every part's tokens in the bins before those, and a list of the codes in them
+//   pick    a workgroup a row: the list, sorted, gives the cut; the parts' weights the part that holds the token, which is searched
+// Where the list would be too long (thousands of tokens of nearly equal logits) the cut is found digit by digit instead (11, 11, 10
+// bits of the logit, twice 12 of the index): count or weight of the tokens that share the digits so far, by their next digit.
 #include "kvg_exp.h"
 #include "kvg_sample.h"
 
@@ -18,7 +24,9 @@ namespace kvg {
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 1024;            // of the workgroup that picks a row's token
+constexpr int kPartThreads = 256;         // of one that takes a part of a row
+constexpr double kLn2 = 0.69314718055994530942;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 4096;
 typedef unsigned long long u64;
@@ -51,6 +59,8 @@ __device__ __forceinline__ u64 max_lanes(u64 x) {
 struct Row {
   double top, inv_t, min_p, one;      // largest logit, 1 / temperature, least e^x kept, 2^bits
   u64 cut;                            // least code kept
+  float least;                        // logits below it weigh 0
+  double bin_scale;                   // bins for each unit of x
 };
 struct Weight {
   double e;
@@ -67,13 +77,25 @@ __device__ __forceinline__ u64 kept(const Row& r, float l, int i, const double* 
   return w.e >= r.min_p ? w.n : 0;
 }
 
+struct Digits {
+  u64 weight[kBins];
+  uint32_t count[kBins];
+};
 struct Shared {
   double tab[64];
   u64 wave[kWaves];
-  u64 weight[kBins];
-  uint32_t count[kBins];
-  u64 found[3];
+  u64 found[2];
+  union {
+    Digits digits;
+    u64 list[kSampleListed];
+  };
 };
+
+// The share p of a weight, rounded up: what a running sum has to reach.
+__device__ __forceinline__ u64 share_of(float p, u64 sum) {
+  const u64 need = p > 0.0f ? (u64)(int64_t)__builtin_ceil((double)p * (double)sum) : 1;
+  return need < 1 ? 1 : need > sum && sum > 0 ? sum : need;
+}
 
 // The code at which the running count (or, by_weight, the running weight) of the tokens from the largest code on reaches `need`, of
 // those with codes of at least r.cut; there are that many.
@@ -83,8 +105,8 @@ __device__ u64 find_cut(const SampleArgs& a, const Row& r, const float* l, bool 
   for (int d = 0; d < 5; ++d) {
     const int n = 1 << kWidth[d], above = kShift[d] + kWidth[d];
     for (int i = threadIdx.x; i < n; i += kThreads) {
-      s.count[i] = 0;
-      s.weight[i] = 0;
+      s.digits.count[i] = 0;
+      s.digits.weight[i] = 0;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < a.V; i += kThreads) {
@@ -92,16 +114,16 @@ __device__ u64 find_cut(const SampleArgs& a, const Row& r, const float* l, bool 
       if (c < r.cut || c >> above != prefix >> above) continue;
       const int bin = (int)(c >> kShift[d]) & (n - 1);
       if (by_weight)
-        atomicAdd(&s.weight[bin], weight(r, l[i], s.tab).n);
+        atomicAdd(&s.digits.weight[bin], weight(r, l[i], s.tab).n);
       else
-        atomicAdd(&s.count[bin], 1u);
+        atomicAdd(&s.digits.count[bin], 1u);
     }
     __syncthreads();
     // the highest bins first: lane j of the first wave sums n / 64 of them, then finds the one that reaches `need`
     if (threadIdx.x < 64) {
       const int per = n / 64, hi = n - 1 - (int)threadIdx.x * per;
       u64 sum = 0;
-      for (int j = 0; j < per; ++j) sum += by_weight ? s.weight[hi - j] : s.count[hi - j];
+      for (int j = 0; j < per; ++j) sum += by_weight ? s.digits.weight[hi - j] : s.digits.count[hi - j];
       u64 upto = sum;
       for (int m = 1; m < 64; m <<= 1) {
         const u64 before = __shfl_up(upto, m);
@@ -111,7 +133,7 @@ __device__ u64 find_cut(const SampleArgs& a, const Row& r, const float* l, bool 
       if (reach != 0 && (int)threadIdx.x == __builtin_ctzll(reach)) {
         u64 run = upto - sum;
         for (int j = 0; j < per; ++j) {
-          const u64 x = by_weight ? s.weight[hi - j] : s.count[hi - j];
+          const u64 x = by_weight ? s.digits.weight[hi - j] : s.digits.count[hi - j];
           if (run + x >= need) {
             s.found[0] = (u64)(hi - j);
             s.found[1] = run;
@@ -144,57 +166,426 @@ __device__ u64 part_weights(const Row& r, const float* l, int i0, int i1, int pa
   return total;
 }
 
-__global__ __launch_bounds__(kThreads) void sample_row_kernel(const SampleArgs a) {
-  __shared__ Shared s;
-  const int row = blockIdx.x, tid = threadIdx.x;
-  const float* l = a.logits + (int64_t)row * a.row_stride;
-  if (tid < 64) s.tab[tid] = exp2(tid / 64.0);
-  u64 top = 0;
-  for (int i = tid; i < a.V; i += kThreads) {
-    const u64 c = token_code(l[i], i);
-    top = c > top ? c : top;
-  }
-  top = max_lanes(top);
-  if ((tid & 63) == 0) s.wave[tid >> 6] = top;
-  __syncthreads();
-  for (int w = 0; w < kWaves; ++w) top = s.wave[w] > top ? s.wave[w] : top;
-  __syncthreads();
-
+// A row's parameters from its largest code; false where the row has no token to sample, or takes its first maximum: what it gives is
+// then written (by one lane).
+__device__ __forceinline__ bool row_setup(const SampleArgs& a, int row, u64 top, bool write, Row& r) {
   const float t = a.temperature[row];
   const double u = a.uniform[row];
-  const int k = a.top_k != nullptr ? a.top_k[row] : 0;
   const float p = a.top_p != nullptr ? a.top_p[row] : 1.0f;
   const float m = a.min_p != nullptr ? a.min_p[row] : 0.0f;
-  Row r;
   const uint32_t top_code = (uint32_t)(top >> kSampleIndexBits);
-  r.top = logit_of(top_code);
   const bool ok = top_code < logit_code(INFINITY) && top_code > logit_code(-INFINITY) && t >= 0.0f && t < INFINITY && u == u && p == p && m == m;
   if (!ok || t == 0.0f) {
-    if (tid == 0) {
+    if (write) {
       a.tokens[row] = ok ? token_of(top) : -1;
       if (a.logprobs != nullptr) a.logprobs[row] = ok ? 0.0f : __uint_as_float(0x7FC00000u);
     }
-    return;
+    return false;
   }
+  r.top = logit_of(top_code);
   r.inv_t = 1.0 / (double)t;
   r.min_p = m < 1.0f ? m : 1.0;
   r.one = __builtin_ldexp(1.0, a.bits);
   r.cut = 0;
-  if (k > 0 && k < a.V) r.cut = find_cut(a, r, l, false, (u64)k, s);
-  const int part = (a.V + kWaves - 1) / kWaves;
-  if (p < 1.0f) {
-    Row all = r;
-    all.min_p = 0.0;
-    const u64 sum = part_weights(all, l, 0, a.V, part, s);
-    u64 need = p > 0.0f ? (u64)(int64_t)__builtin_ceil((double)p * (double)sum) : 1;
-    need = need < 1 ? 1 : need > sum ? sum : need;
-    r.cut = find_cut(a, r, l, true, need, s);
+  // weights below half of 2^-bits are 0: no logit further below the top than (bits + 1) ln 2 t has one
+  r.least = (float)(r.top - (a.bits + 2) * kLn2 * (double)t) ;
+  r.least = r.least - fabsf(r.least) * 0x1p-22f - 1e-37f;
+  r.bin_scale = kSampleBins / ((a.bits + 2) * kLn2);
+  return true;
+}
+__device__ __forceinline__ int bin_of(const Row& r, float l) {
+  const double b = (r.top - (double)l) * r.inv_t * r.bin_scale;
+  return b < kSampleBins - 1 ? (int)b : kSampleBins - 1;
+}
+
+// f(logit, index) for the tokens [i0, i1) of a row, by `threads` lanes; four at a time where the row lies on 16 bytes (i0 is a
+// multiple of 4)
+template <typename F>
+__device__ __forceinline__ void for_tokens(const float* l, int i0, int i1, int threads, F f) {
+  if (reinterpret_cast<uintptr_t>(l) % 16 == 0) {
+    int i = i0 + 4 * (int)threadIdx.x;
+#pragma unroll 2
+    for (; i + 3 < i1; i += 4 * threads) {
+      const float4 x = *reinterpret_cast<const float4*>(l + i);
+      f(x.x, i);
+      f(x.y, i + 1);
+      f(x.z, i + 2);
+      f(x.w, i + 3);
+    }
+    for (; i < i1; ++i) f(l[i], i);      // the lane whose four reach past the end
+  } else {
+    for (int i = i0 + (int)threadIdx.x; i < i1; i += threads) f(l[i], i);
   }
-  const u64 total = part_weights(r, l, 0, a.V, part, s);
+}
+
+// The largest code of a row's parts.
+__device__ __forceinline__ u64 row_top(const SampleArgs& a, int row) {
+  u64 top = 0;
+  for (int i = threadIdx.x & 63; i < a.n_parts; i += 64) {
+    const u64 c = a.tops[(int64_t)row * a.n_parts + i];
+    top = c > top ? c : top;
+  }
+  return max_lanes(top);
+}
+
+__global__ __launch_bounds__(kPartThreads) void sample_top_kernel(const SampleArgs a) {
+  __shared__ u64 sh[kPartThreads / 64];
+  const int row = blockIdx.y, part = blockIdx.x;
+  const float* l = a.logits + (int64_t)row * a.row_stride;
+  // the row's bins and list, emptied for the next launches
+  for (int i = part * kPartThreads + threadIdx.x; i < kSampleBins; i += a.n_parts * kPartThreads) {
+    a.bin_weights[(int64_t)row * kSampleBins + i] = 0;
+    a.bin_counts[(int64_t)row * kSampleBins + i] = 0;
+  }
+  if (part == 0 && threadIdx.x == 0) a.n_listed[row] = 0;
+  u64 top = 0;
+  for_tokens(l, part * a.part_size, min(a.V, (part + 1) * a.part_size), kPartThreads, [&](float x, int i) {
+    const u64 c = token_code(x, i);
+    top = c > top ? c : top;
+  });
+  top = max_lanes(top);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = top;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < kPartThreads / 64; ++w) top = sh[w] > top ? sh[w] : top;
+  a.tops[(int64_t)row * a.n_parts + part] = top;
+}
+
+// Whether a row's top-k or top-p may end inside it.
+__device__ __forceinline__ bool limited(const SampleArgs& a, int row) {
+  const int k = a.top_k != nullptr ? a.top_k[row] : 0;
+  return (k > 0 && k < a.V) || (a.top_p != nullptr && a.top_p[row] < 1.0f);
+}
+
+__global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(const SampleArgs a) {
+  __shared__ double tab[64];
+  __shared__ u64 weights[kSampleBins];
+  __shared__ uint32_t counts[kSampleBins];
+  const int row = blockIdx.y, part = blockIdx.x;
+  Row r;
+  if (!limited(a, row) || !row_setup(a, row, row_top(a, row), false, r)) return;
+  if (threadIdx.x < 64) tab[threadIdx.x] = exp2(threadIdx.x / 64.0);
+  for (int i = threadIdx.x; i < kSampleBins; i += kPartThreads) {
+    weights[i] = 0;
+    counts[i] = 0;
+  }
+  __syncthreads();
+  for_tokens(a.logits + (int64_t)row * a.row_stride, part * a.part_size, min(a.V, (part + 1) * a.part_size), kPartThreads, [&](float x, int) {
+    if (x < r.least) return;
+    const u64 n = weight(r, x, tab).n;
+    if (n == 0) return;
+    const int b = bin_of(r, x);
+    atomicAdd(&weights[b], n);
+    atomicAdd(&counts[b], 1u);
+  });
+  __syncthreads();
+  for (int i = threadIdx.x; i < kSampleBins; i += kPartThreads)
+    if (counts[i] != 0) {
+      atomicAdd(&a.bin_weights[(int64_t)row * kSampleBins + i], weights[i]);
+      atomicAdd(&a.bin_counts[(int64_t)row * kSampleBins + i], counts[i]);
+    }
+}
+
+// Where a row's limits end, from its bins.
+struct Ends {
+  int first, last;            // bins between which top-p ends (top-k's, where there is no top-p): all before `first` is kept
+  int k_bin;                  // the bin that top-k ends in, kSampleBins: none
+  uint32_t k_need;            // tokens that top-k takes of it
+  uint32_t listed_before_k;   // of the listed codes, those in bins before k_bin
+  u64 before_first, before_k; // weight of the bins before
+};
+struct EndsShared {
+  u64 weight[16], count[16];  // of the waves' bins
+  u64 upto_k;                 // weight up to top-k's bin, with it
+  Ends ends;
+};
+// (all lanes of a workgroup of kSampleBins lanes or fewer; bins in order, kSampleBins / threads a lane)
+template <int kT>
+__device__ void find_ends(const SampleArgs& a, int row, Ends& out, EndsShared& s) {
+  constexpr int kPer = kSampleBins / kT;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b0 = threadIdx.x * kPer;
+  u64 w[kPer], c[kPer], sw = 0, sc = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    w[i] = a.bin_weights[(int64_t)row * kSampleBins + b0 + i];
+    c[i] = a.bin_counts[(int64_t)row * kSampleBins + b0 + i];
+    sw += w[i];
+    sc += c[i];
+  }
+  u64 uw = sw, uc = sc;                                      // up to and with this lane's
+  for (int m = 1; m < 64; m <<= 1) {
+    const u64 x = __shfl_up(uw, m), y = __shfl_up(uc, m);
+    uw += lane >= m ? x : 0;
+    uc += lane >= m ? y : 0;
+  }
+  if (lane == 63) {
+    s.weight[wave] = uw;
+    s.count[wave] = uc;
+  }
+  if (threadIdx.x == 0) s.ends = {0, -1, kSampleBins, 0, 0, 0, 0};
+  __syncthreads();
+  u64 total_w = 0, total_c = 0;
+  for (int i = 0; i < kT / 64; ++i) {
+    if (i < wave) {
+      uw += s.weight[i];
+      uc += s.count[i];
+    }
+    total_w += s.weight[i];
+    total_c += s.count[i];
+  }
+  uw -= sw;                                                  // before this lane's
+  uc -= sc;
+  const int k = a.top_k != nullptr ? a.top_k[row] : 0;
+  const float p = a.top_p != nullptr ? a.top_p[row] : 1.0f;
+  const bool by_k = k > 0 && (u64)k < total_c;
+  if (by_k) {
+    u64 x = uw, y = uc;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (y < (u64)k && y + c[i] >= (u64)k) {
+        s.ends.k_bin = b0 + i;
+        s.ends.k_need = (uint32_t)((u64)k - y);
+        s.ends.before_k = x;
+        s.upto_k = x + w[i];
+      }
+      x += w[i];
+      y += c[i];
+    }
+  }
+  __syncthreads();
+  const u64 most = by_k ? s.upto_k : total_w, least = by_k ? s.ends.before_k : total_w;
+  if (p < 1.0f) {
+    const u64 need0 = share_of(p, least), need1 = share_of(p, most);
+    u64 x = uw;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (x < need0 && x + w[i] >= need0) {
+        s.ends.first = b0 + i;
+        s.ends.before_first = x;
+      }
+      if (x < need1 && x + w[i] >= need1) s.ends.last = b0 + i;
+      x += w[i];
+    }
+  } else if (by_k && threadIdx.x == 0) {
+    s.ends.first = s.ends.last = s.ends.k_bin;
+    s.ends.before_first = s.ends.before_k;
+  } else if (threadIdx.x == 0) {
+    s.ends.first = kSampleBins;                              // no limit ends in the row
+  }
+  __syncthreads();
+  if (s.ends.k_bin < kSampleBins) {                          // listed codes in front of top-k's bin
+    u64 n = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) n += b0 + i >= s.ends.first && b0 + i <= s.ends.last && b0 + i < s.ends.k_bin ? c[i] : 0;
+    n = add_lanes(n);
+    if (lane == 0 && n != 0) atomicAdd(&s.ends.listed_before_k, (uint32_t)n);
+  }
+  __syncthreads();
+  out = s.ends;
+}
+__device__ __forceinline__ bool is_listed(const Ends& e, int bin) { return (bin >= e.first && bin <= e.last) || bin == e.k_bin; }
+
+__global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(const SampleArgs a) {
+  __shared__ double tab[64];
+  __shared__ EndsShared ends_shared;
+  __shared__ u64 sh[kPartThreads / 64];
+  const int row = blockIdx.y, part = blockIdx.x;
+  Row r;
+  if (!row_setup(a, row, row_top(a, row), false, r)) return;
+  if (threadIdx.x < 64) tab[threadIdx.x] = exp2(threadIdx.x / 64.0);
+  Ends ends = {kSampleBins, -1, kSampleBins, 0, 0, 0, 0};
+  if (limited(a, row)) find_ends<kPartThreads>(a, row, ends, ends_shared);
+  __syncthreads();
+  const bool all = ends.first == kSampleBins;
+  u64 sum = 0;
+  for_tokens(a.logits + (int64_t)row * a.row_stride, part * a.part_size, min(a.V, (part + 1) * a.part_size), kPartThreads, [&](float x, int i) {
+    if (x < r.least) return;
+    const Weight w = weight(r, x, tab);
+    if (w.n == 0) return;
+    const int b = all ? 0 : bin_of(r, x);
+    if (b < ends.first) {
+      sum += w.e >= r.min_p ? w.n : 0;
+    } else if (is_listed(ends, b)) {
+      const uint32_t at = atomicAdd(&a.n_listed[row], 1u);
+      if (at < kSampleListed) a.listed[(int64_t)row * kSampleListed + at] = token_code(x, i);
+    }
+  });
+  sum = add_lanes(sum);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < kPartThreads / 64; ++w) sum += sh[w];
+  a.sums[(int64_t)row * a.n_parts + part] = sum;
+}
+
+// The n codes of a list, the largest first; the rest of the power of two that it is sorted in are 0.
+__device__ void sort_list(u64* list, int n) {
+  int size = 64;
+  while (size < n) size <<= 1;
+  for (int i = n + (int)threadIdx.x; i < size; i += kThreads) list[i] = 0;
+  __syncthreads();
+  for (int run = 2; run <= size; run <<= 1)
+    for (int d = run >> 1; d > 0; d >>= 1) {
+      for (int i = threadIdx.x; i < size / 2; i += kThreads) {
+        const int x = (i / d) * 2 * d + i % d, y = x + d;
+        const u64 u = list[x], v = list[y];
+        if ((u < v) == ((x & run) == 0)) {
+          list[x] = v;
+          list[y] = u;
+        }
+      }
+      __syncthreads();
+    }
+}
+
+// The first place of a sorted list, of n, at which `base` and the weights up to it reach `need`; n - 1 if none.  (all lanes)
+__device__ int reach(const Row& r, const u64* list, int n, u64 base, u64 need, Shared& s) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = (n + kThreads - 1) / kThreads, j0 = threadIdx.x * per;
+  u64 sum = 0;
+  for (int j = j0; j < min(n, j0 + per); ++j) sum += weight(r, logit_of((uint32_t)(list[j] >> kSampleIndexBits)), s.tab).n;
+  u64 upto = sum;
+  for (int m = 1; m < 64; m <<= 1) {
+    const u64 x = __shfl_up(upto, m);
+    upto += lane >= m ? x : 0;
+  }
+  __syncthreads();
+  if (lane == 63) s.wave[wave] = upto;
+  if (threadIdx.x == 0) s.found[0] = (u64)(n - 1);
+  __syncthreads();
+  u64 run = base + upto - sum;
+  for (int w = 0; w < wave; ++w) run += s.wave[w];
+  if (run < need)
+    for (int j = j0; j < min(n, j0 + per); ++j) {
+      run += weight(r, logit_of((uint32_t)(list[j] >> kSampleIndexBits)), s.tab).n;
+      if (run >= need) {
+        s.found[0] = (u64)j;
+        break;
+      }
+    }
+  __syncthreads();
+  return (int)s.found[0];
+}
+// The weight of the first n codes of a list.  (all lanes)
+__device__ u64 list_weight(const Row& r, const u64* list, int n, Shared& s) {
+  u64 sum = 0;
+  for (int j = threadIdx.x; j < n; j += kThreads) sum += weight(r, logit_of((uint32_t)(list[j] >> kSampleIndexBits)), s.tab).n;
+  sum = add_lanes(sum);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s.wave[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  u64 total = 0;
+  for (int w = 0; w < kWaves; ++w) total += s.wave[w];
+  return total;
+}
+
+// kListed: rows of up to kSampleListed tokens, all of them listed.
+template <bool kListed>
+__global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs a) {
+  __shared__ Shared s;
+  __shared__ EndsShared ends_shared;
+  __shared__ u64 parts[kSampleParts];
+  const int row = blockIdx.x, tid = threadIdx.x;
+  const float* l = a.logits + (int64_t)row * a.row_stride;
+  if (tid < 64) s.tab[tid] = exp2(tid / 64.0);
+  u64 top = 0;
+  if constexpr (kListed) {
+    for (int i = tid; i < a.V; i += kThreads) {
+      const u64 c = s.list[i] = token_code(l[i], i);
+      top = c > top ? c : top;
+    }
+    top = max_lanes(top);
+    if ((tid & 63) == 0) s.wave[tid >> 6] = top;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) top = s.wave[w] > top ? s.wave[w] : top;
+    __syncthreads();
+  } else {
+    top = row_top(a, row);
+  }
+  Row r;
+  if (!row_setup(a, row, top, tid == 0, r)) return;
+  const double u = a.uniform[row];
+  const int k = a.top_k != nullptr ? a.top_k[row] : 0;
+  const float p = a.top_p != nullptr ? a.top_p[row] : 1.0f;
+  __syncthreads();
+  const bool limit = limited(a, row);
+  // the tokens [i0, i1) hold the one that is picked, `target` of their kept weight before it; their parts' weights are in s.wave
+  int i0 = 0, i1 = a.V, size = (a.V + kWaves - 1) / kWaves;
+  u64 total;
+  bool searched = true;                                      // by parts of the row
+  if constexpr (kListed) {
+    if (limit) {
+      sort_list(s.list, a.V);
+      int n = k > 0 && k < a.V ? k : a.V;
+      if (p < 1.0f) n = reach(r, s.list, n, 0, share_of(p, list_weight(r, s.list, n, s)), s) + 1;
+      r.cut = s.list[n - 1];
+      __syncthreads();
+    }
+    searched = false;
+  } else {
+    Ends ends = {kSampleBins, -1, kSampleBins, 0, 0, 0, 0};
+    if (limit) find_ends<kThreads>(a, row, ends, ends_shared);
+    const uint32_t n_listed = limit ? a.n_listed[row] : 0;
+    for (int i = tid; i < a.n_parts; i += kThreads) parts[i] = a.sums[(int64_t)row * a.n_parts + i];
+    if (n_listed > kSampleListed) {
+      if (k > 0 && k < a.V) r.cut = find_cut(a, r, l, false, (u64)k, s);
+      if (p < 1.0f) {
+        Row whole = r;
+        whole.min_p = 0.0;
+        r.cut = find_cut(a, r, l, true, share_of(p, part_weights(whole, l, 0, a.V, size, s)), s);
+      }
+      searched = false;
+    } else if (ends.first < kSampleBins) {
+      int n = (int)n_listed;
+      for (int i = tid; i < n; i += kThreads) s.list[i] = a.listed[(int64_t)row * kSampleListed + i];
+      __syncthreads();
+      sort_list(s.list, n);
+      u64 sum = 0;                                           // of top-k's tokens
+      if (ends.k_bin < kSampleBins) {
+        n = (int)(ends.listed_before_k + ends.k_need);
+        sum = ends.before_k + list_weight(r, s.list + ends.listed_before_k, (int)ends.k_need, s);
+      } else if (p < 1.0f) {
+        for (int i = 0; i < kThreads / 64; ++i) sum += ends_shared.weight[i];
+      }
+      if (p < 1.0f) n = reach(r, s.list, n, ends.before_first, share_of(p, sum), s) + 1;
+      r.cut = s.list[n - 1];
+      for (int i = tid; i < n; i += kThreads) {              // the listed tokens that are kept, to their parts
+        const u64 c = s.list[i];
+        const Weight w = weight(r, logit_of((uint32_t)(c >> kSampleIndexBits)), s.tab);
+        if (w.e >= r.min_p) atomicAdd(&parts[token_of(c) / a.part_size], w.n);
+      }
+    }
+    __syncthreads();
+  }
+  static_assert(kSampleParts == 128, "two parts a lane");
+  const int pair = 2 * (tid & 63);
+  u64 even = 0, odd = 0, upto = 0;                           // every wave alike: a lane's parts, and those up to them
+  if (searched) {
+    even = pair < a.n_parts ? parts[pair] : 0;
+    odd = pair + 1 < a.n_parts ? parts[pair + 1] : 0;
+    upto = even + odd;
+    for (int d = 1; d < 64; d <<= 1) {
+      const u64 before = __shfl_up(upto, d);
+      upto += (tid & 63) >= d ? before : 0;
+    }
+    total = __shfl(upto, 63);
+  } else {
+    total = part_weights(r, l, 0, a.V, size, s);
+  }
   u64 target = u > 0.0 ? (u < 1.0 ? (u64)(int64_t)__builtin_floor(u * (double)total) : total - 1) : 0;
   target = target < total ? target : total - 1;
+  if (searched) {
+    const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > target));
+    target -= __shfl(upto - odd - even, at);
+    const u64 first = __shfl(even, at);
+    const bool second = target >= first;
+    target -= second ? first : 0;
+    i0 = (2 * at + second) * a.part_size;
+    i1 = min(a.V, i0 + a.part_size);
+    size = (a.part_size + kWaves - 1) / kWaves;
+    part_weights(r, l, i0, i1, size, s);
+  }
   // the part that holds it, ever shorter
-  int i0 = 0, i1 = a.V, size = part;
   while (true) {
     int w = 0;
     while (w < kWaves - 1 && target >= s.wave[w]) target -= s.wave[w++];
@@ -208,23 +599,30 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(const SampleArgs a
   // at most 64 tokens are left: a lane each
   if (tid >= 64) return;
   const int i = i0 + tid;
-  u64 upto = i < i1 ? kept(r, l[i], i, s.tab) : 0;
+  u64 run = i < i1 ? kept(r, l[i], i, s.tab) : 0;
   for (int d = 1; d < 64; d <<= 1) {
-    const u64 before = __shfl_up(upto, d);
-    upto += tid >= d ? before : 0;
+    const u64 before = __shfl_up(run, d);
+    run += tid >= d ? before : 0;
   }
-  const uint64_t past = __builtin_amdgcn_ballot_w64(upto > target);
+  const uint64_t past = __builtin_amdgcn_ballot_w64(run > target);
   if (past != 0 && tid == __builtin_ctzll(past)) {
     a.tokens[row] = i;
-    if (a.logprobs != nullptr)
-      a.logprobs[row] = (float)(((double)l[i] - r.top) * r.inv_t - (log((double)total) - a.bits * 0.69314718055994530942));
+    if (a.logprobs != nullptr) a.logprobs[row] = (float)(((double)l[i] - r.top) * r.inv_t - (log((double)total) - a.bits * kLn2));
   }
 }
 
 }  // namespace
 
 hipError_t launch_sample(const SampleArgs& a, hipStream_t stream) {
-  sample_row_kernel<<<a.rows, kThreads, 0, stream>>>(a);
+  if (a.V <= kSampleListed) {
+    sample_pick_kernel<true><<<a.rows, kThreads, 0, stream>>>(a);
+    return hipGetLastError();
+  }
+  const dim3 grid(a.n_parts, a.rows);
+  sample_top_kernel<<<grid, kPartThreads, 0, stream>>>(a);
+  if (a.top_k != nullptr || a.top_p != nullptr) sample_bins_kernel<<<grid, kPartThreads, 0, stream>>>(a);
+  sample_parts_kernel<<<grid, kPartThreads, 0, stream>>>(a);
+  sample_pick_kernel<false><<<a.rows, kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
