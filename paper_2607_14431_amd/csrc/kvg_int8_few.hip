@@ -59,7 +59,8 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
   const int n_units = (k_end - k_begin + kUnitKeys - 1) / kUnitKeys;
   pg = pg >= 0 && pg < a.n_pages ? pg : 0;
   const int64_t scale_at = ((int64_t)(a.layer0 + l) * a.n_pages + pg) * a.Hkv + g;
-  const float k_scale = scales.k[scale_at], v_scale = scales.v[scale_at];
+  const PageScales page = page_scales(scales.k[scale_at], scales.v[scale_at]);
+  const uint32_t bad_pages = (uint32_t)__builtin_amdgcn_ballot_w64(page.bad);
 
   const int pair = min(lrow, n_pairs - 1);
   const bool pair_ok = lrow < n_pairs;
@@ -82,11 +83,6 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
                             (lds_char*)(lds_void*)(dst + (2 * wave + p) * R::kPageBytes), source);
     }
   };
-  auto scales_at = [&](int key) -> PageScales {      // of the page that holds it
-    const int p = (key / kPage) & 31;
-    return page_scales(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scale), p)),
-                       __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scale), p)));
-  };
   issue(KR{}, kpool, s_k, 0);
   issue(VR{}, vpool, s_v, 0);
   Int8Query<D> q;
@@ -101,7 +97,7 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
   f32x16 o[NDW];
 #pragma unroll
   for (int d = 0; d < NDW; ++d) o[d] = splat(0.0f);
-  Int8State st = {-INFINITY, -INFINITY, 0.0f};
+  Int8State st = empty_state(q.finite ? 0.0f : kNaN);
 
   __builtin_amdgcn_s_waitcnt(vm_wait(0));            // the first unit, with the query requested behind it
   for (int u = 0; u < n_units; ++u) {
@@ -120,45 +116,70 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
     asm volatile("" ::: "memory");
     issue(KR{}, kpool, s_k, u + 1);
     const int kb = key0 + 32 * wave;
-    const PageScales own0 = scales_at(kb), own1 = scales_at(kb + kPage);
-    f32x16 s = int8_scores(hi, lo, q_scale * own0.k, q_scale * own1.k);
-    if (kb + 31 > first_n || kb < mask_lo) {
+    auto lv_at = [&](int key) -> float { return lane_value(page.lv, (key / kPage) & 31); };
+    const float kq0 = key_factor(q_scale, lane_value(page.k, (kb / kPage) & 31));
+    const float kq1 = key_factor(q_scale, lane_value(page.k, (kb / kPage + 1) & 31));
+    f32x16 s;
+    float mx[2] = {-INFINITY, -INFINITY};
+    const bool masked = kb + 31 > first_n || kb < mask_lo;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
+    for (int r = 0; r < 16; ++r) {
+      s[r] = (float)((hi[r] << 8) + lo[r]);
+      if (masked) {
         const int key = kb + half * 4 + (r >> 2) * 8 + (r & 3);
         s[r] = (key <= row_n && key >= row_lo) ? s[r] : -INFINITY;
       }
+      mx[r / 8] = fmaxf(mx[r / 8], s[r]);
     }
-    s_mx[wave][lrow] = page_maxima(s);               // both halves of the wave, the same values
+    {
+      const float2 m0 = halves32(mx[0]), m1 = halves32(mx[1]);
+      s_mx[wave][lrow] = make_float2(fmaxf(m0.x, m0.y) * kq0, fmaxf(m1.x, m1.y) * kq1);      // both halves of the wave, the same values
+    }
     __syncthreads();
     // ---- the references of the unit's blocks in order (every wave alike), this wave's weights
-    float alpha_l[kWaves], alpha_o[kWaves];
-    bool raised[kWaves];
-    Int8Block mine = {};
+    Int8Raise raise[kWaves];
+    bool raised[kWaves];                             // seldom: the references are coarse
+    Int8Page p0 = {}, p1 = {};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const float2 x = s_mx[w][lrow];
-      const Int8Block blk = raise_block(st, x.x, x.y, scales_at(key0 + 32 * w), scales_at(key0 + 32 * w + kPage));
-      alpha_l[w] = blk.alpha_l;
-      alpha_o[w] = blk.alpha_o;
-      raised[w] = blk.raised;
-      if (w == wave) mine = blk;
+      const float lv0 = lv_at(key0 + 32 * w), lv1 = lv_at(key0 + 32 * w + kPage);
+      raised[w] = __builtin_amdgcn_ballot_w64(is_raised(st, x.x, x.y, lv0, lv1)) != 0;
+      if (raised[w]) raise[w] = raise_block(st, x.x, x.y, lv0, lv1);
+      if (w == wave) {
+        p0 = page_weights(st, lv0);
+        p1 = page_weights(st, lv1);
+      }
     }
-    uint4 p[2];
-    s_sum[wave][lrow] = block_weights(s, mine, p);
-    s_p[wave][0][lane] = p[0];
-    s_p[wave][1][lane] = p[1];
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = weight_of(s[r], r < 8 ? kq0 : kq1, r < 8 ? p0.c : p1.c);
+      sum[r / 8] += s[r];
+    }
+    s_p[wave][0][lane] = round_weights8(s, 0);
+    s_p[wave][1][lane] = round_weights8(s, 1);
+    s_sum[wave][lrow] = block_sum(sum[0], sum[1], p0.back, p1.back);
+    if (bad_pages != 0) {
+      for (int i = 0; i < 2 * kWaves; ++i) {
+        const int key = key0 + i * kPage;
+        if ((bad_pages >> ((key / kPage) & 31) & 1) != 0 && key <= row_n && key + kPage > row_lo) st.l = kNaN;
+      }
+    }
     // V of the unit has landed (the next unit's K may be in flight)
     __builtin_amdgcn_s_waitcnt(vm_wait(kLoads));
     __syncthreads();
     // ---- this wave's dimensions over the unit's blocks
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      st.l = fmaf(st.l, alpha_l[w], s_sum[w][lrow]);
-      if ((u > 0 || w > 0) && __builtin_amdgcn_ballot_w64(raised[w]) != 0) {      // O is 0 before the first block
+      if (raised[w]) {
+        st.l *= raise[w].alpha_l;
+        if (u > 0 || w > 0) {                        // O is 0 before the first block
 #pragma unroll
-        for (int d = 0; d < NDW; ++d) o[d] *= alpha_o[w];
+          for (int d = 0; d < NDW; ++d) o[d] *= raise[w].alpha_o;
+        }
       }
+      st.l += s_sum[w][lrow];
       const uint4 p0 = s_p[w][0][lane], p1 = s_p[w][1][lane];
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)

@@ -35,6 +35,7 @@ template <int D>
 struct Int8Query {
   uint4 hi[D / 32], lo[D / 32];
   float step;
+  bool finite;
 };
 // q: the pair's query row (its first dimension), bf16; zeros for a lane without one.
 template <int D>
@@ -56,9 +57,10 @@ __device__ __forceinline__ void load_query(Int8Query<D>& x, const uint16_t* q, b
   const uint32_t bits = both[0] > both[1] ? both[0] : both[1];         // of the largest |q|; Inf and NaN above all others
   const bool finite = bits < 0x7F80u;
   // |q| < 2^e; below 2^-100 the integers get smaller
-  const int e = max(__builtin_amdgcn_frexp_expf(bf16_bits_to_f32(bits)), -100);
+  const int e = finite ? max(__builtin_amdgcn_frexp_expf(bf16_bits_to_f32(bits)), -100) : 0;
   const float up = finite ? __builtin_ldexpf(1.0f, 14 - e) : 0.0f;
-  x.step = finite ? __builtin_ldexpf(1.0f, e - 14) : __uint_as_float(0x7FC00000u);
+  x.step = __builtin_ldexpf(1.0f, e - 14);
+  x.finite = finite;
   // q up + 1.5 2^23 has the integer, rounded to nearest even, in its low bits; 128 more and its byte 1 is the upper byte that
   // goes with a signed lower one
   constexpr float kRound = 12582912.0f;
@@ -100,77 +102,78 @@ __device__ __forceinline__ uint4 widen_int8(const uint2& x) {
   return r;
 }
 
-// The scales of a block of 32 keys' two pages.  A page with a scale that is not finite makes the scores NaN: value
-// weights that are would reach rows that do not see it.
+// A page's scales as the kernels use them, a page a lane; ones that are not finite count as 0 (`bad`: rows that see a token of
+// the page get NaN).
 struct PageScales {
-  float k, v, lv;              // lv: v < 2^lv
+  float k, lv;                 // lv: log2 of the values' scale, -Inf for a block of zeros
+  bool bad;
 };
 __device__ __forceinline__ PageScales page_scales(float k, float v) {
-  const bool bad = !(fmaxf(fabsf(k), fabsf(v)) < INFINITY) || k != k || v != v;
-  return {bad ? __uint_as_float(0x7FC00000u) : k, bad ? 0.0f : v, bad || v == 0.0f ? -INFINITY : (float)__builtin_amdgcn_frexp_expf(v)};
+  const bool bad = !(fabsf(k) < INFINITY) || !(fabsf(v) < INFINITY);
+  return {bad ? 0.0f : k, bad ? -INFINITY : __builtin_amdgcn_logf(v), bad};
+}
+__device__ __forceinline__ float lane_value(float x, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
 }
 
-// Softmax state of a segment: references (log2 units, multiples of kStep) of the weights p and of p sv, and the sum of p.
+constexpr float kNaN = __builtin_nanf("");
+
+// Softmax state of a segment: references (log2 units, multiples of kStep) of the weights p = 2^(s - m) and of p sv, the sum of p (l0 at
+// first: 0, or NaN for a query that is not finite), and what follows from the references: m, or 0 before the first key, and the
+// exponent x that takes p sv to the range of fp16.
+//
+// Weights are p sv 2^x = 2^(S kq + c), the largest of a row below 2^kWeightTop, rounded to fp16: off by half a step (2^-11 of it) at
+// most, less than the result's own rounding to bf16.  p is the weight times `back`.  Values that weigh less than 2^-kLightest of
+// the row's largest may as well weigh that: it stays far below an fp16 step, and the sum of p keeps its bits.
+constexpr float kWeightTop = 15.0f, kLightest = 60.0f;
 struct Int8State {
-  float m, mt, l;
+  float m, mt, l, m_ref, x;
 };
-// What a block does to it: factors of l and of the sums of values, the reference of its exponents, and what its pages' weights are
-// multiplied with before they are rounded.
-struct Int8Block {
-  float alpha_l, alpha_o, m_ref, f0, f1;
-  bool raised;                 // alpha_o may not be 1
+__device__ __forceinline__ Int8State empty_state(float l0) { return {-INFINITY, -INFINITY, l0, 0.0f, 0.0f}; }
+
+// The steps of a block of 32 keys (two pages).  A lane's scores of a page are S kq: S an integer (as a float; -Inf for a key that
+// the row does not see), kq the query's step times the keys' scale, in log2 units (not 0, by which -Inf would be NaN).
+__device__ __forceinline__ float key_factor(float q_scale, float k) { return fmaxf(q_scale * k, 0x1p-126f); }
+// What a lane's largest scores of the pages (both halves of the wave joined) do to the state: factors of the sum of p and of the
+// sums of values, powers of two (or 0).
+struct Int8Raise {
+  float alpha_l, alpha_o;
 };
-constexpr int kWeightTop = 15;
-// mx0, mx1: a row's largest scores in the block's pages, log2 units
-__device__ __forceinline__ Int8Block raise_block(Int8State& s, float mx0, float mx1, const PageScales& p0, const PageScales& p1) {
-  Int8Block b;
+__device__ __forceinline__ bool is_raised(const Int8State& s, float mx0, float mx1, float lv0, float lv1) {
+  return fmaxf(mx0, mx1) > s.m || fmaxf(mx0 + lv0, mx1 + lv1) > s.mt;
+}
+__device__ __forceinline__ Int8Raise raise_block(Int8State& s, float mx0, float mx1, float lv0, float lv1) {
+  Int8Raise b;
   bool up;
   b.alpha_l = raise_reference(s.m, fmaxf(mx0, mx1), up);
-  b.alpha_o = raise_reference(s.mt, fmaxf(mx0 + p0.lv, mx1 + p1.lv), b.raised);
-  b.m_ref = s.m == -INFINITY ? 0.0f : s.m;
-  const int x = s.mt == -INFINITY ? 0 : (int)(b.m_ref - s.mt) + kWeightTop;
-  // a weight of 0 times a factor past fp32's range must be 0
-  b.f0 = fminf(__builtin_ldexpf(p0.v, x), 3.4e38f);
-  b.f1 = fminf(__builtin_ldexpf(p1.v, x), 3.4e38f);
+  b.alpha_o = raise_reference(s.mt, fmaxf(mx0 + lv0, mx1 + lv1), up);
+  s.m_ref = s.m == -INFINITY ? 0.0f : s.m;
+  s.x = s.mt == -INFINITY ? 0.0f : s.m_ref - s.mt + kWeightTop;
   return b;
 }
-// the power of two that takes the sums of values to the reference of the weights
-__device__ __forceinline__ int end_exponent(const Int8State& s) {
-  return s.mt == -INFINITY ? 0 : (int)(s.mt - s.m) - kWeightTop;
+struct Int8Page {
+  float c, back;
+};
+__device__ __forceinline__ Int8Page page_weights(const Int8State& s, float lv) {
+  const float f = fmaxf(lv + s.x, -kLightest);
+  return {f - s.m_ref, __builtin_amdgcn_exp2f(-f)};
 }
-
-// A lane's 16 scores of a block from the two parts of the products, log2 units; kq: query step times the scale of page 0, 1
-__device__ __forceinline__ f32x16 int8_scores(const i32x16& hi, const i32x16& lo, float kq0, float kq1) {
-  f32x16 s;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) s[r] = (float)((hi[r] << 8) + lo[r]) * (r < 8 ? kq0 : kq1);
-  return s;
+__device__ __forceinline__ float weight_of(float S, float kq, float c) { return __builtin_amdgcn_exp2f(fmaf(S, kq, c)); }
+__device__ __forceinline__ uint32_t round_pair(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, f16x2));
 }
-// the largest of each page, over both halves of the wave
-__device__ __forceinline__ float2 page_maxima(const f32x16& s) {
-  float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-  for (int r = 0; r < 16; ++r) mx[r / 8] = fmaxf(mx[r / 8], s[r]);
-  const float2 m0 = halves32(mx[0]), m1 = halves32(mx[1]);
-  return make_float2(fmaxf(m0.x, m0.y), fmaxf(m1.x, m1.y));
+// eight weights as an operand of the value steps
+__device__ __forceinline__ uint4 round_weights8(const f32x16& s, int h) {
+  return make_uint4(round_pair(s[8 * h], s[8 * h + 1]), round_pair(s[8 * h + 2], s[8 * h + 3]), round_pair(s[8 * h + 4], s[8 * h + 5]),
+                    round_pair(s[8 * h + 6], s[8 * h + 7]));
 }
-// The scores' exponentials, their sum over both halves of the wave returned, and as operands of the value steps: times the pages'
-// factors, rounded to fp16, each off by half a step (2^-11 of it) at most, less than the result's own rounding to bf16.
-__device__ __forceinline__ float block_weights(f32x16& s, const Int8Block& b, uint4 (&p)[2]) {
-  float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    s[r] = __builtin_amdgcn_exp2f(s[r] - b.m_ref);
-    sum[r & 1] += s[r];
-  }
-#pragma unroll
-  for (int w = 0; w < 8; ++w) {
-    const float f = w < 4 ? b.f0 : b.f1;
-    (&p[w / 4].x)[w % 4] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){s[2 * w] * f, s[2 * w + 1] * f}, f16x2));
-  }
-  const float2 both = halves32(sum[0] + sum[1]);
+// The block's part of the sum of p from a lane's sums of weights of the pages (both halves of the wave).
+__device__ __forceinline__ float block_sum(float sum0, float sum1, float back0, float back1) {
+  const float2 both = halves32(fmaf(sum0, back0, sum1 * back1));
   return both.x + both.y;
 }
+// End of a segment: the exponent that takes its sums of values to the reference of p (far below fp32 where every scale was 0).
+__device__ __forceinline__ int end_exponent(const Int8State& s) { return s.mt == -INFINITY ? -1000 : (int)(s.mt - s.m - kWeightTop); }
 
 }  // namespace
 

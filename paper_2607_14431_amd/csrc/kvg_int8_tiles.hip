@@ -1,15 +1,22 @@
 // Causal attention of packed sequences over int8 caches, on the int8 and fp16 matrix cores.
 //
 // Workgroup = (layer, KV head g, tile of a sequence): kTilePairs (row, query head) pairs of the sequence, heads fastest, 32 per
-// wave.  Keys come in tiles of 64 (absolute multiples of 64 of the logical index) in two LDS stages, loaded with
-// buffer_load ... lds while the tile before is computed.
+// wave.  Keys come in tiles of 64 (absolute multiples of 64 of the logical index) in two LDS stages.
 //
 // A row's sums have one order, whatever the launch: keys in blocks of 32 (two pages), an online softmax over the blocks of a segment
 // of kPackedSeg keys, and the segments' states folded in ascending order (packed_fold_kernel does the same operations).
 // References are the row's own (Int8State), so pages that it does not see change nothing.
 //
-//   S^T = K Q^T     A = K rows from LDS as they are cached, B = the pairs' queries, two bytes a value (kvg_int8_mfma.h)
-//   O^T += V^T P^T  A = V^T fragments (ds_read_b64_tr_b8) widened to fp16, B = P straight from the S^T registers
+//   S^T = K Q^T     A = K rows from LDS as they are cached (buffer_load ... lds a tile ahead), B = the pairs' queries, two bytes a
+//                   value (kvg_int8_mfma.h)
+//   O^T += V^T P^T  A = V^T fragments (ds_read_b64_tr_b16), B = P straight from the S^T registers.  V is widened to fp16 on its way:
+//                   each wave takes one page of the next tile through registers into LDS, once for the four waves that read it
+//                   (widened beside the reads, every wave spent 160 vector instructions a tile of head_dim 128 on it instead of 40)
+//
+// Bound: vector instructions beside the matrix ones (the two add up: head_dim 128 has the vector unit busy 62% of the time, the matrix
+// cores 29%), so the loop is counted in them: ids and scales once a segment, references seldom raised.  Eight prompts of up to 4,096
+// tokens, 32 heads on 16, head_dim 128: 540 us (714 TFLOP/s; ids and scales loaded a page at a time 616).  head_dim 256 has one wave a
+// SIMD and copies accumulators between the two register files: one prompt of 12,288 tokens, 16 heads on 8, 2.31 ms (536 TFLOP/s).
 #include "kvg_int8_mfma.h"
 #include "kvg_launch.h"
 
@@ -19,8 +26,17 @@ namespace kvg {
 
 namespace {
 
+// f(A), .., f(B - 1), constants: arrays that a call indexes by them stay in registers
+template <int A, int B, typename F>
+__device__ __forceinline__ void static_for(const F& f) {
+  if constexpr (A < B) {
+    f(std::integral_constant<int, A>{});
+    static_for<A + 1, B>(f);
+  }
+}
+
 constexpr int kTileKeys = 64;
-constexpr int kSegTiles = kPackedSeg / kTileKeys;
+constexpr int kSegTiles = kPackedSeg / kTileKeys, kSegPages = kPackedSeg / kPage;
 constexpr int kWaves = 4;
 // kSplitKeys: a workgroup takes one segment and leaves its partial.
 template <int D, bool kSplitKeys>
@@ -30,7 +46,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
   constexpr int BM = kTilePairs;
   static_assert(BM == 32 * kWaves, "a block of 32 pairs per wave");
   using KR = KRows<D>;
-  using VR = VRows<D>;
+  using VR = VRows<2 * D>;
   // a wave brings one page of a tile; the V stages first, where an LDS instruction's immediate offset reaches
   __shared__ __attribute__((aligned(1024))) char sA_V0[kWaves * VR::kPageBytes];
   __shared__ __attribute__((aligned(1024))) char sA_V1[kWaves * VR::kPageBytes];
@@ -88,22 +104,47 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
   const char* vpool = static_cast<const char*>(a.v_pool) + lbase;
   const int64_t sbase = (int64_t)(a.layer0 + l) * a.n_pages * a.Hkv + g;
 
-  // ---- loads: wave w brings page w of tile kt; rows past the last one the workgroup needs read as zeros.  Lane i has the id of page
-  // i % 4 of a tile and, a tile later, its scales.
-  const int source = KR::source(lane);     // the same for V
-  auto pages_of_tile = [&](int kt) -> int32_t {
-    const int32_t page = bt[min(kt * (kTileKeys / kPage) + (lane & 3), last_page)];
+  // ---- loads: wave w brings page w of tile kt; rows past the last one the workgroup needs read as zeros.  Lane i has the id and the
+  // scales of page i of a segment (its 32 pages), a segment ahead.
+  const int source = KR::source(lane);
+  int seg_now = kt_begin / kSegTiles;                  // the segment that `pages` is of
+  auto pages_of_segment = [&](int sg) -> int32_t {
+    const int32_t page = bt[min(sg * kSegPages + (lane & (kSegPages - 1)), last_page)];
     return page >= 0 && page < a.n_pages ? page : 0;
   };
-  constexpr int kTileLoads = 2 * KR::kPageLoads;       // of a wave: K and V alternate
-  auto issue = [&](int kt, int32_t pages, auto dst_stage, int j0, int j1) {
-    constexpr int DS = decltype(dst_stage)::value;
-    const int64_t off = ((int64_t)__builtin_amdgcn_readlane(pages, wave) * a.Hkv + g) * kPage * D;
-    const int rows = __builtin_amdgcn_readfirstlane(min(max(n_hi - (kt * (kTileKeys / kPage) + wave) * kPage, 0), kPage));
-    lds_char* dk = (lds_char*)(lds_void*)((DS ? sB_K1 : sB_K0) + wave * KR::kPageBytes);
-    lds_char* dv = (lds_char*)(lds_void*)((DS ? sA_V1 : sA_V0) + wave * VR::kPageBytes);
-    load_page<KR, 0>(kpool + off, rows, dk, source, (j0 + 1) / 2, (j1 + 1) / 2);
-    load_page<VR, 0>(vpool + off, rows, dv, source, j0 / 2, j1 / 2);
+  int32_t pages = pages_of_segment(kt_begin / kSegTiles), pages_next = pages_of_segment(kt_begin / kSegTiles + 1);
+  auto slab_of = [&](int kt) -> int64_t {              // of this wave's page of tile kt, which is in this segment or the next
+    const int i = kt % kSegTiles * (kTileKeys / kPage) + wave;
+    const int32_t here = __builtin_amdgcn_readlane(pages, i), there = __builtin_amdgcn_readlane(pages_next, i);
+    return ((int64_t)(kt / kSegTiles == seg_now ? here : there) * a.Hkv + g) * kPage * D;
+  };
+  auto rows_of = [&](int kt) -> int {
+    return __builtin_amdgcn_readfirstlane(min(max(n_hi - (kt * (kTileKeys / kPage) + wave) * kPage, 0), kPage));
+  };
+  auto issue_k = [&](int kt, auto stage) {
+    lds_char* dk = (lds_char*)(lds_void*)((decltype(stage)::value ? sB_K1 : sB_K0) + wave * KR::kPageBytes);
+    load_page<KR, 0>(kpool + slab_of(kt), rows_of(kt), dk, source);
+  };
+  // V: 16 bytes of a row are a lane's.  Its row and place of load j are such that the lanes' stores of widened values lie side by side.
+  constexpr int kVLoads = D / 64;
+  constexpr int kLines = VR::kRows;                      // rows whose 16-byte chunks lie side by side
+  const int v_row = lane % kLines + lane / 32 * (32 / (D / 16)), v_col = lane % 32 / kLines;
+  const int v_source = v_row * D + v_col * 16;
+  static_assert(32 / (D / 16) == kLines, "half a wave takes kLines rows");
+  const int v_store = wave * VR::kPageBytes + VR::at(v_row, 2 * v_col);
+  constexpr int kNextChunk = VR::at(0, 1), kNextLoad = 2 * VR::kLoad;
+  static_assert(1024 / D == 2 * kLines, "a load takes 2 kLines rows");
+  uint4 v_raw[kVLoads];
+  auto issue_v = [&](int kt) {
+    const __amdgpu_buffer_rsrc_t rs =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(vpool + slab_of(kt)), 0, rows_of(kt) * D, kBufferWord3);
+#pragma unroll
+    for (int j = 0; j < kVLoads; ++j) v_raw[j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, v_source, 1024 * j, 0));
+  };
+  auto widen_v = [&](auto stage, int j) {
+    char* to = (decltype(stage)::value ? sA_V1 : sA_V0) + v_store + j * kNextLoad;
+    *reinterpret_cast<uint4*>(to) = widen_int8(make_uint2(v_raw[j].x, v_raw[j].y));
+    *reinterpret_cast<uint4*>(to + kNextChunk) = widen_int8(make_uint2(v_raw[j].z, v_raw[j].w));
   };
 
   // ---- queries (B operand of S^T), zeros past the rows
@@ -115,8 +156,9 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
   }
   const float q_scale = q.step * a.scale_log2;
 
+  const float l0 = q.finite ? 0.0f : kNaN;
   f32x16 o[ND], o_run[kSplitKeys ? 1 : ND];
-  Int8State st = {-INFINITY, -INFINITY, 0.0f};
+  Int8State st = empty_state(l0);
   float m_run = -INFINITY, l_run = 0.0f;
 #pragma unroll
   for (int d = 0; d < ND; ++d) {
@@ -124,47 +166,58 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
     if constexpr (!kSplitKeys) o_run[d] = splat(0.0f);
   }
 
-  const int k_lane = k_lane_base<D, false>(lane), v_lane = v_lane_base<D, true>(lane);
+  const int k_lane = k_lane_base<D, false>(lane), v_lane = v_lane_base<2 * D, false>(lane);
 
   using Stage0 = std::integral_constant<int, 0>;
   using Stage1 = std::integral_constant<int, 1>;
-  int32_t pages_next = pages_of_tile(kt_begin);
-  float ks_next = scales.k[sbase + (int64_t)pages_next * a.Hkv], vs_next = scales.v[sbase + (int64_t)pages_next * a.Hkv];
-  issue(kt_begin, pages_next, Stage0{}, 0, kTileLoads);
-  pages_next = pages_of_tile(kt_begin + 1);
+  float ks_next, vs_next;
+  auto load_scales = [&](int32_t page) {
+    const int64_t at = sbase + (int64_t)page * a.Hkv;
+    ks_next = scales.k[at];
+    vs_next = scales.v[at];
+  };
+  issue_v(kt_begin);
+  issue_k(kt_begin, Stage0{});
+  load_scales(pages);
+  PageScales sc = page_scales(ks_next, vs_next);
+  uint32_t bad = (uint32_t)__builtin_amdgcn_ballot_w64(sc.bad);
+  load_scales(pages_next);
+#pragma unroll
+  for (int j = 0; j < kVLoads; ++j) widen_v(Stage0{}, j);
+  issue_v(kt_begin + 1);
 
   bool fresh = true;                      // no block of the segment yet
   auto tile = [&](auto stage, int kt) __attribute__((always_inline)) {
     constexpr int ST = decltype(stage)::value;
     using Next = std::integral_constant<int, 1 - ST>;
-    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's share of tile kt, its scales and the next page ids are here
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's K of tile kt and V of the next one are here, and what a segment ahead needs
     __syncthreads();                      // all of tile kt is in LDS; the other stage is no longer read
-    const int key0 = kt * kTileKeys;
-    const float ks = ks_next, vs = vs_next;
-    const int32_t pages = pages_next;
-    ks_next = scales.k[sbase + (int64_t)pages * a.Hkv];
-    vs_next = scales.v[sbase + (int64_t)pages * a.Hkv];
-    pages_next = pages_of_tile(kt + 2);
-    issue(kt + 1, pages, Next{}, 0, kTileLoads);
+    const int key0 = kt * kTileKeys, page0 = kt % kSegTiles * (kTileKeys / kPage);
+    if (kt / kSegTiles != seg_now) {
+      ++seg_now;
+      pages = pages_next;
+      sc = page_scales(ks_next, vs_next);
+      bad = (uint32_t)__builtin_amdgcn_ballot_w64(sc.bad);
+      pages_next = pages_of_segment(seg_now + 1);
+    } else if (kt % kSegTiles == 1) {
+      load_scales(pages_next);
+    }
+    issue_k(kt + 1, Next{});
+#pragma unroll
+    for (int j = 0; j < kVLoads; ++j) widen_v(Next{}, j);
+    issue_v(kt + 2);
     if (key0 > wave_last || key0 + kTileKeys <= wave_lo) return;       // unseen by this wave's rows
+    if ((bad >> page0 & 15u) != 0) {
+      for (int p = 0; p < kTileKeys / kPage; ++p)
+        if ((bad >> (page0 + p) & 1u) != 0 && key0 + p * kPage <= row_n && key0 + (p + 1) * kPage > row_lo) st.l = kNaN;
+    }
     const lds_char* kbase = (const lds_char*)(lds_void*)(ST ? sB_K1 : sB_K0) + k_lane;
     const lds_char* vbase = (const lds_char*)(lds_void*)(ST ? sA_V1 : sA_V0) + v_lane;
     const bool need_mask = key0 + kTileKeys - 1 > wave_first || key0 < mask_lo;
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      i32x16 hi = (i32x16)(0), lo = (i32x16)(0);
-#pragma unroll
-      for (int ss = 0; ss < NS; ++ss) {
-        const uint4 k = int8_k_fragment<D>(kbase + KR::at(32 * kb, 0), ss);
-        hi = mfma_i8(k, q.hi[ss], hi);
-        lo = mfma_i8(k, q.lo[ss], lo);
-      }
-      auto scales_of = [&](int p) -> PageScales {
-        return page_scales(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), p)),
-                           __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), p)));
-      };
-      const PageScales p0 = scales_of(2 * kb), p1 = scales_of(2 * kb + 1);
-      f32x16 s = int8_scores(hi, lo, q_scale * p0.k, q_scale * p1.k);
+    auto kread = [&](int f) { return int8_k_fragment<D>(kbase + KR::at(32 * (f / NS), 0), f % NS); };          // f = block * NS + step
+    auto vread = [&](int t) { return v_fragment<2 * D, false>(vbase + VR::at(16 * (t / ND), 0), t % ND); };    // t = 16-key step * ND + d
+    // -Inf where the row does not see the key
+    auto mask = [&](f32x16& s, int kb) __attribute__((always_inline)) {
       if (need_mask) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -173,22 +226,67 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
           s[r] = key <= (uint32_t)(row_n - row_lo) ? s[r] : -INFINITY;
         }
       }
-      const float2 mx = page_maxima(s);
-      const Int8Block blk = raise_block(st, mx.x, mx.y, p0, p1);
-      uint4 p[2];
-      st.l = fmaf(st.l, blk.alpha_l, block_weights(s, blk, p));
-      if (!fresh && __builtin_amdgcn_ballot_w64(blk.raised) != 0) {    // O of a segment's first block is still 0
+    };
+    // the references of block kb from a lane's largest scores of its pages, O and the sum of p with them (O of a segment's first block
+    // is still 0)
+    auto references = [&](float mx0, float mx1, float kq0, float kq1, float lv0, float lv1) __attribute__((always_inline)) {
+      const float2 m0 = halves32(mx0), m1 = halves32(mx1);
+      const float t0 = fmaxf(m0.x, m0.y) * kq0, t1 = fmaxf(m1.x, m1.y) * kq1;
+      if (__builtin_amdgcn_ballot_w64(is_raised(st, t0, t1, lv0, lv1)) != 0) {       // seldom: the references are coarse
+        const Int8Raise up = raise_block(st, t0, t1, lv0, lv1);
+        st.l *= up.alpha_l;
+        if (!fresh) {
 #pragma unroll
-        for (int d = 0; d < ND; ++d) o[d] *= blk.alpha_o;
+          for (int d = 0; d < ND; ++d) o[d] *= up.alpha_o;
+        }
       }
       fresh = false;
+    };
 #pragma unroll
-      for (int i = 0; i < 2 * ND; ++i)
-        o[i % ND] = mfma_f16(widen_int8(v_fragment<D, true>(vbase + VR::at(32 * kb + 16 * (i / ND), 0), i % ND)), p[i / ND], o[i % ND]);
+    for (int kb = 0; kb < 2; ++kb) {
+      const float kq0 = key_factor(q_scale, lane_value(sc.k, page0 + 2 * kb)), kq1 = key_factor(q_scale, lane_value(sc.k, page0 + 2 * kb + 1));
+      const float lv0 = lane_value(sc.lv, page0 + 2 * kb), lv1 = lane_value(sc.lv, page0 + 2 * kb + 1);
+      uint4 kf[NS];
+#pragma unroll
+      for (int ss = 0; ss < NS; ++ss) kf[ss] = kread(kb * NS + ss);
+      // the queries' upper bytes, then the lower ones on top of 256 times their sums
+      i32x16 acc = (i32x16)(0);
+#pragma unroll
+      for (int ss = 0; ss < NS; ++ss) acc = mfma_i8(kf[ss], q.hi[ss], acc);
+      acc <<= 8;
+#pragma unroll
+      for (int ss = 0; ss < NS; ++ss) acc = mfma_i8(kf[ss], q.lo[ss], acc);
+      f32x16 s = __builtin_convertvector(acc, f32x16);
+      mask(s, kb);
+      float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        mx0 = fmaxf(mx0, s[r]);
+        mx1 = fmaxf(mx1, s[8 + r]);
+      }
+      references(mx0, mx1, kq0, kq1, lv0, lv1);
+      const Int8Page p0 = page_weights(st, lv0), p1 = page_weights(st, lv1);
+      float sum0 = 0.0f, sum1 = 0.0f;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        s[r] = weight_of(s[r], kq0, p0.c);
+        sum0 += s[r];
+      }
+#pragma unroll
+      for (int r = 8; r < 16; ++r) {
+        s[r] = weight_of(s[r], kq1, p1.c);
+        sum1 += s[r];
+      }
+      const uint4 w0 = round_weights8(s, 0), w1 = round_weights8(s, 1);
+      st.l += block_sum(sum0, sum1, p0.back, p1.back);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] = mfma_f16(vread(kb * 2 * ND + d), w0, o[d]);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] = mfma_f16(vread(kb * 2 * ND + ND + d), w1, o[d]);
     }
   };
-  // end of a segment: its sums at the reference of the exponentials; its state folded into the running one, which
-  // packed_fold_kernel does with the same operations
+  // end of a segment: its sums taken to the reference of p, its state folded into the running one, which packed_fold_kernel does with
+  // the same operations (the power of two in the factor would give a few zeros another sign)
   auto end_segment = [&]() {
     const int e = end_exponent(st);
 #pragma unroll
@@ -202,7 +300,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
       const FoldFactors f = fold_factors(m_run, l_run, st.m, st.l);
 #pragma unroll
       for (int d = 0; d < ND; ++d) o_run[d] = __builtin_elementwise_fma(o[d], splat(f.part), o_run[d] * f.run);
-      st = {-INFINITY, -INFINITY, 0.0f};
+      st = empty_state(l0);
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d] = splat(0.0f);
       fresh = true;
