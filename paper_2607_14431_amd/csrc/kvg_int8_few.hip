@@ -4,6 +4,10 @@
 // The sums are those of the tile kernel (kvg_int8_tiles.hip), operation for operation, spread over the waves as in
 // packed_few_kernel: the scores of a unit's blocks of 32 keys (a block per wave), then the weights, then the weighted values (a
 // part of head_dim per wave, over all of the unit's blocks in order).
+//
+// Bound: many sequences, memory (16 tokens over 33k keys of 8 x 256: 306 us, 5.3 TB/s); one sequence, the chain of a workgroup: requests,
+// their latency, scores, references, values (4.6k keys of 8 x 256: 24 us, 4 of them the fold; with a read of LDS between each two
+// blocks, the query's loads under conditions and four waves it was 27).
 #include "kvg_int8_mfma.h"
 #include "kvg_launch.h"
 
@@ -16,8 +20,8 @@ constexpr int vm_wait(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
 constexpr int kLgkmWait = 0xC07F;      // lgkmcnt(0) alone
 constexpr int kStream = 2;             // buffer load policy: nontemporal (every row is read once)
 
-// kWaves: waves of a workgroup, a block of 32 keys and D / kWaves dimensions each
-template <int D, int kWaves>
+// kWaves: waves of a workgroup, a block of 32 keys and D / kWaves dimensions each.  kDepth: units in LDS or on their way.
+template <int D, int kWaves, int kDepth>
 __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnArgs a, const Int8Scales scales) {
   constexpr int NS = D / 32;
   constexpr int NDW = D / 32 / kWaves;               // 32-wide blocks of head_dim per wave
@@ -26,8 +30,11 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
   using VR = VRows<D>;
   constexpr int kLoads = 2 * KR::kPageLoads;         // direct loads of a wave's block, K or V
   static_assert(D / 32 % kWaves == 0 && kPackedSeg % kUnitKeys == 0, "units");
-  __shared__ __attribute__((aligned(1024))) char s_k[2 * kWaves * KR::kPageBytes];
-  __shared__ __attribute__((aligned(1024))) char s_v[2 * kWaves * VR::kPageBytes];
+  constexpr int kKBytes = 2 * kWaves * KR::kPageBytes, kVBytes = 2 * kWaves * VR::kPageBytes;      // of a unit
+  constexpr int kYounger = (2 * kDepth - 1) * kLoads;        // loads behind the ones that the next step reads
+  static_assert(kYounger + kLoads < 64, "vmcnt");
+  __shared__ __attribute__((aligned(1024))) char s_k[kDepth * kKBytes];
+  __shared__ __attribute__((aligned(1024))) char s_v[kDepth * kVBytes];
   __shared__ uint4 s_p[kWaves][2][64];
   __shared__ float2 s_mx[kWaves][32];
   __shared__ float s_sum[kWaves][32];
@@ -58,9 +65,6 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
   if (k_begin >= k_end) return;
   const int n_units = (k_end - k_begin + kUnitKeys - 1) / kUnitKeys;
   pg = pg >= 0 && pg < a.n_pages ? pg : 0;
-  const int64_t scale_at = ((int64_t)(a.layer0 + l) * a.n_pages + pg) * a.Hkv + g;
-  const PageScales page = page_scales(scales.k[scale_at], scales.v[scale_at]);
-  const uint32_t bad_pages = (uint32_t)__builtin_amdgcn_ballot_w64(page.bad);
 
   const int pair = min(lrow, n_pairs - 1);
   const bool pair_ok = lrow < n_pairs;
@@ -70,6 +74,16 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
   const int64_t lbase = (int64_t)(a.layer0 + l) * a.layer_elems;
   const char* kpool = static_cast<const char*>(a.k_pool) + lbase;
   const char* vpool = static_cast<const char*>(a.v_pool) + lbase;
+
+  // ---- the pages' scales and the query are requested first, and converted with the keys on their way
+  const int64_t scale_at = ((int64_t)(a.layer0 + l) * a.n_pages + pg) * a.Hkv + g;
+  const float scale_k = scales.k[scale_at], scale_v = scales.v[scale_at];
+  uint4 raw[NS][2];
+  {
+    const int64_t tok = (int64_t)l * a.seqs.n_tokens + sq.row0 + row;
+    load_query<D>(raw, static_cast<const uint16_t*>(a.q) + tok * a.q_stride + (int64_t)head * D, half);
+  }
+  asm volatile("" ::: "memory");
 
   // ---- loads of this wave's block of unit u (two pages, K or V); rows from k_end on read as zeros
   const int source = KR::source(lane);               // the same for V
@@ -83,13 +97,14 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
                             (lds_char*)(lds_void*)(dst + (2 * wave + p) * R::kPageBytes), source);
     }
   };
-  issue(KR{}, kpool, s_k, 0);
-  issue(VR{}, vpool, s_v, 0);
+  static_for<0, kDepth>([&](auto u) {
+    issue(KR{}, kpool, s_k + decltype(u)::value * kKBytes, decltype(u)::value);
+    issue(VR{}, vpool, s_v + decltype(u)::value * kVBytes, decltype(u)::value);
+  });
+  const PageScales page = page_scales(scale_k, scale_v);
+  const uint32_t bad_pages = (uint32_t)__builtin_amdgcn_ballot_w64(page.bad);
   Int8Query<D> q;
-  {
-    const int64_t tok = (int64_t)l * a.seqs.n_tokens + sq.row0 + row;
-    load_query<D>(q, static_cast<const uint16_t*>(a.q) + tok * a.q_stride + (int64_t)head * D, pair_ok, half);
-  }
+  split_query<D>(q, raw);
   const float q_scale = q.step * a.scale_log2;
 
   const lds_char* kbase = (const lds_char*)(lds_void*)s_k + 2 * wave * KR::kPageBytes + k_lane_base<D, false>(lane);
@@ -99,22 +114,22 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
   for (int d = 0; d < NDW; ++d) o[d] = splat(0.0f);
   Int8State st = empty_state(q.finite ? 0.0f : kNaN);
 
-  __builtin_amdgcn_s_waitcnt(vm_wait(0));            // the first unit, with the query requested behind it
-  for (int u = 0; u < n_units; ++u) {
+  int slot = 0;                                      // u % kDepth
+  for (int u = 0; u < n_units; ++u, slot = slot + 1 == kDepth ? 0 : slot + 1) {
     const int key0 = k_begin + u * kUnitKeys;
-    // ---- scores of this wave's block; its K has landed (V's loads may be in flight)
-    __builtin_amdgcn_s_waitcnt(vm_wait(kLoads));
+    // ---- scores of this wave's block; its K has landed (its V and later units may be in flight)
+    __builtin_amdgcn_s_waitcnt(vm_wait(kYounger));
     asm volatile("" ::: "memory");
     i32x16 hi = (i32x16)(0), lo = (i32x16)(0);
 #pragma unroll
     for (int ss = 0; ss < NS; ++ss) {
-      const uint4 k = int8_k_fragment<D>(kbase, ss);
+      const uint4 k = int8_k_fragment<D>(kbase + slot * kKBytes, ss);
       hi = mfma_i8(k, q.hi[ss], hi);
       lo = mfma_i8(k, q.lo[ss], lo);
     }
-    __builtin_amdgcn_s_waitcnt(kLgkmWait);           // read: the buffer takes the next unit's
+    __builtin_amdgcn_s_waitcnt(kLgkmWait);           // read: the buffer takes a later unit's
     asm volatile("" ::: "memory");
-    issue(KR{}, kpool, s_k, u + 1);
+    issue(KR{}, kpool, s_k + slot * kKBytes, u + kDepth);
     const int kb = key0 + 32 * wave;
     auto lv_at = [&](int key) -> float { return lane_value(page.lv, (key / kPage) & 31); };
     const float kq0 = key_factor(q_scale, lane_value(page.k, (kb / kPage) & 31));
@@ -140,9 +155,12 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
     Int8Raise raise[kWaves];
     bool raised[kWaves];                             // seldom: the references are coarse
     Int8Page p0 = {}, p1 = {};
+    float2 most[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) most[w] = s_mx[w][lrow];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float2 x = s_mx[w][lrow];
+      const float2 x = most[w];
       const float lv0 = lv_at(key0 + 32 * w), lv1 = lv_at(key0 + 32 * w + kPage);
       raised[w] = __builtin_amdgcn_ballot_w64(is_raised(st, x.x, x.y, lv0, lv1)) != 0;
       if (raised[w]) raise[w] = raise_block(st, x.x, x.y, lv0, lv1);
@@ -166,10 +184,23 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
         if ((bad_pages >> ((key / kPage) & 31) & 1) != 0 && key <= row_n && key + kPage > row_lo) st.l = kNaN;
       }
     }
-    // V of the unit has landed (the next unit's K may be in flight)
-    __builtin_amdgcn_s_waitcnt(vm_wait(kLoads));
+    // V of the unit has landed (later units may be in flight)
+    __builtin_amdgcn_s_waitcnt(vm_wait(kYounger));
     __syncthreads();
-    // ---- this wave's dimensions over the unit's blocks
+    // ---- this wave's dimensions over the unit's blocks: all reads first
+    uint2 v[kWaves][2][NDW];
+    uint4 p[kWaves][2];
+    float sums[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      sums[w] = s_sum[w][lrow];
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        p[w][ks] = s_p[w][ks][lane];
+#pragma unroll
+        for (int d = 0; d < NDW; ++d) v[w][ks][d] = v_fragment<D, true>(vbase + slot * kVBytes + (2 * w + ks) * VR::kPageBytes, d);
+      }
+    }
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       if (raised[w]) {
@@ -179,16 +210,14 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
           for (int d = 0; d < NDW; ++d) o[d] *= raise[w].alpha_o;
         }
       }
-      st.l += s_sum[w][lrow];
-      const uint4 p0 = s_p[w][0][lane], p1 = s_p[w][1][lane];
+      st.l += sums[w];
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int d = 0; d < NDW; ++d)
-          o[d] = mfma_f16(widen_int8(v_fragment<D, true>(vbase + (2 * w + ks) * VR::kPageBytes, d)), ks ? p1 : p0, o[d]);
+        for (int d = 0; d < NDW; ++d) o[d] = mfma_f16(widen_int8(v[w][ks][d]), p[w][ks], o[d]);
     }
-    __syncthreads();                                 // V, weights and sums are read: the next unit's may come
-    issue(VR{}, vpool, s_v, u + 1);
+    __syncthreads();                                 // V, weights and sums are read: a later unit's may come
+    issue(VR{}, vpool, s_v + slot * kVBytes, u + kDepth);
   }
   __builtin_amdgcn_s_waitcnt(vm_wait(0));            // the empty loads past the last unit write LDS: none may outlive the workgroup
   const int e = end_exponent(st);
@@ -225,15 +254,20 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
   }
 }
 
+// Up to this many workgroups, one a compute unit, a workgroup has waves for all of head_dim and, where LDS holds them, all keys of a
+// segment on their way at once: the time is one workgroup's, start to end.  More workgroups hide their waits from each other: two
+// waves each and one unit.  Small workgroups against large ones, each with the fold, us, at workgroups: head_dim 256: 80 30 / 25, 160
+// 33 / 26, 240 33 / 27, 320 38 / 43, 1,280 53 / 84; 128: 16 17 / 15, 80 26 / 21, 160 25-26 / 20-22, 320 28-30 / 27, 640 30-32 /
+// 42-49, 1,280 35 / 63.  At head_dim 64 it is the same kernel (a deep one of 8 units: 48 20.0 / 20.4, 576 26 / 28).
 constexpr unsigned kFewGrid = 256;
 template <int D>
 hipError_t launch_few_d(const PackedAttnArgs& a, const Int8Scales& s, hipStream_t stream) {
   const unsigned grid = (unsigned)packed_few_workgroups(a);
-  constexpr int kMost = D == 64 ? 2 : 4;
+  constexpr int kMost = D / 32, kDeep = D == 128 ? 4 : 1;
   if (grid <= kFewGrid)
-    int8_few_kernel<D, kMost><<<grid, 64 * kMost, 0, stream>>>(a, s);
+    int8_few_kernel<D, kMost, kDeep><<<grid, 64 * kMost, 0, stream>>>(a, s);
   else
-    int8_few_kernel<D, 2><<<grid, 64 * 2, 0, stream>>>(a, s);
+    int8_few_kernel<D, 2, 1><<<grid, 64 * 2, 0, stream>>>(a, s);
   return hipGetLastError();
 }
 

@@ -12,9 +12,20 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace kvg {
 
 namespace {
+
+// f(A), .., f(B - 1), constants: arrays that a call indexes by them stay in registers
+template <int A, int B, typename F>
+__device__ __forceinline__ void static_for(const F& f) {
+  if constexpr (A < B) {
+    f(std::integral_constant<int, A>{});
+    static_for<A + 1, B>(f);
+  }
+}
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
@@ -37,15 +48,17 @@ struct Int8Query {
   float step;
   bool finite;
 };
-// q: the pair's query row (its first dimension), bf16; zeros for a lane without one.
+// q: the pair's query row (its first dimension), bf16; a lane without a pair takes another's.
 template <int D>
-__device__ __forceinline__ void load_query(Int8Query<D>& x, const uint16_t* q, bool ok, int half) {
+__device__ __forceinline__ void load_query(uint4 (&raw)[D / 32][2], const uint16_t* q, int half) {
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) raw[s][j] = ld16(q + 32 * s + 16 * half + 8 * j);
+}
+template <int D>
+__device__ __forceinline__ void split_query(Int8Query<D>& x, const uint4 (&raw)[D / 32][2]) {
   constexpr int NS = D / 32;
-  uint4 raw[NS][2];
-#pragma unroll
-  for (int s = 0; s < NS; ++s)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) raw[s][j] = ok ? ld16(q + 32 * s + 16 * half + 8 * j) : make_uint4(0, 0, 0, 0);
   u16x2 most = {0, 0};
 #pragma unroll
   for (int s = 0; s < NS; ++s)

@@ -20,20 +20,9 @@
 #include "kvg_int8_mfma.h"
 #include "kvg_launch.h"
 
-#include <type_traits>
-
 namespace kvg {
 
 namespace {
-
-// f(A), .., f(B - 1), constants: arrays that a call indexes by them stay in registers
-template <int A, int B, typename F>
-__device__ __forceinline__ void static_for(const F& f) {
-  if constexpr (A < B) {
-    f(std::integral_constant<int, A>{});
-    static_for<A + 1, B>(f);
-  }
-}
 
 constexpr int kTileKeys = 64;
 constexpr int kSegTiles = kPackedSeg / kTileKeys, kSegPages = kPackedSeg / kPage;
@@ -147,12 +136,14 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
     *reinterpret_cast<uint4*>(to + kNextChunk) = widen_int8(make_uint2(v_raw[j].z, v_raw[j].w));
   };
 
-  // ---- queries (B operand of S^T), zeros past the rows
+  // ---- queries (B operand of S^T); lanes past the rows take the first row's, and store nothing
   Int8Query<D> q;
   {
     const int64_t tok = (int64_t)l * a.seqs.n_tokens + sq.row0 + (row_ok ? row : 0);
-    load_query<D>(q, static_cast<const uint16_t*>(a.q) + tok * a.q_stride + (int64_t)(g * a.group + ((pair0 + lrow) & (a.group - 1))) * D,
-                  row_ok, half);
+    uint4 raw[NS][2];
+    load_query<D>(raw, static_cast<const uint16_t*>(a.q) + tok * a.q_stride + (int64_t)(g * a.group + ((pair0 + lrow) & (a.group - 1))) * D,
+                  half);
+    split_query<D>(q, raw);
   }
   const float q_scale = q.step * a.scale_log2;
 

@@ -173,9 +173,10 @@ inline bool split_tiles(bool f32, int64_t head_dim, int64_t workgroups, int64_t 
 // workgroups and no empty waves.  Few kernel against tiles, each with its fold, us, at workgroups.  bf16, head_dim 256: 80
 // 26 / 24, 256 33 / 30, 512 52 / 56, 1,024 92 / 132, 8,448 536 / 1,090; 128: 128 23 / 21, 256 24 / 22, 512 31 / 32, 1,024 49 / 59; 64:
 // 64 20 / 17, 256 24 / 17, 512 27 / 23.  fp8, 256: 64 21 / 24, 128 23 / 25, 256 26 / 27, 512 35 / 49; 128: 64 17 / 18, 256 29 / 23;
-// 64: 16 19 / 16, 32 18 / 15.  One limit for all: at 512 it takes the slower side at head_dim 64.
+// 64: 16 19 / 16, 32 18 / 15.  One limit for all: at 512 it takes the slower side at head_dim 64.  int8, whose few kernel has all of
+// a segment on its way at once, 128: 16 15 / 16, 80 21 / 26, 160 20 / 26, 320 27 / 28; 64: 48 20 / 19, 144 22 / 19, 576 26 / 23.
 inline bool few_in_tiles(const kvg_cache* c, int64_t workgroups) {
-  return workgroups <= 256 && (c->dtype == KVG_BF16 || c->head_dim <= 128);
+  return workgroups <= 256 && (c->dtype == KVG_BF16 || c->head_dim <= (c->dtype == KVG_INT8 ? 64 : 128));
 }
 
 // How an attention call runs: rows of the few kernel and tiles at most, each launch's segments (1: not
