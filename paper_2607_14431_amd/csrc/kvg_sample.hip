@@ -10,7 +10,8 @@
 // Rows of up to kSampleListed tokens: a workgroup sorts the row's codes.  Longer ones in passes over the row, by many workgroups:
 //   top     the largest logit of every part of the row
 //   bins    count and weight of the row's tokens by weight (1,024 equal steps of the exponent down to weight 0), where a top-k or
-//           top-p may end inside the row.  The bins tell in which of them the two limits end
+//           top-p may end inside the row.  The bins tell in which of them the two limits end.  Weights are left out where top-p is 1
+//           or the tokens of top-k are few (by_list): an exponential in fp64 costs more than all else in the pass
 //   parts   the weight of every part's tokens in the bins before those, and a list of the codes in them
 //   pick    a workgroup a row: the list, sorted, gives the cut; the parts' weights the part that holds the token, which is searched
 // Where the list would be too long (thousands of tokens of nearly equal logits) the cut is found digit by digit instead (11, 11, 10
@@ -26,6 +27,7 @@ namespace {
 
 constexpr int kThreads = 1024;            // of the workgroup that picks a row's token
 constexpr int kPartThreads = 256;         // of one that takes a part of a row
+constexpr int kPartListed = 512;          // codes that it lists together
 constexpr double kLn2 = 0.69314718055994530942;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 4096;
@@ -251,10 +253,16 @@ __global__ __launch_bounds__(kPartThreads) void sample_top_kernel(const SampleAr
   a.tops[(int64_t)row * a.n_parts + part] = top;
 }
 
+// Whether top-k's tokens are few enough that all of them are listed and top-p's end is sought in the list.
+__device__ __forceinline__ bool by_list(const SampleArgs& a, int row) {
+  const int k = a.top_k != nullptr ? a.top_k[row] : 0;
+  return k > 0 && k <= kSampleListed / 4;
+}
+__device__ __forceinline__ bool has_top_p(const SampleArgs& a, int row) { return a.top_p != nullptr && a.top_p[row] < 1.0f; }
 // Whether a row's top-k or top-p may end inside it.
 __device__ __forceinline__ bool limited(const SampleArgs& a, int row) {
   const int k = a.top_k != nullptr ? a.top_k[row] : 0;
-  return (k > 0 && k < a.V) || (a.top_p != nullptr && a.top_p[row] < 1.0f);
+  return (k > 0 && k < a.V) || has_top_p(a, row);
 }
 
 __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(const SampleArgs a) {
@@ -270,25 +278,32 @@ __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(const SampleA
     counts[i] = 0;
   }
   __syncthreads();
-  for_tokens(a.logits + (int64_t)row * a.row_stride, part * a.part_size, min(a.V, (part + 1) * a.part_size), kPartThreads, [&](float x, int) {
-    if (x < r.least) return;
-    const u64 n = weight(r, x, tab).n;
-    if (n == 0) return;
-    const int b = bin_of(r, x);
-    atomicAdd(&weights[b], n);
-    atomicAdd(&counts[b], 1u);
-  });
+  const float* l = a.logits + (int64_t)row * a.row_stride;
+  const int i0 = part * a.part_size, i1 = min(a.V, i0 + a.part_size);
+  const bool weigh = has_top_p(a, row) && !by_list(a, row);
+  if (weigh)
+    for_tokens(l, i0, i1, kPartThreads, [&](float x, int) {
+      if (x < r.least) return;
+      const int b = bin_of(r, x);
+      atomicAdd(&weights[b], weight(r, x, tab).n);
+      atomicAdd(&counts[b], 1u);
+    });
+  else
+    for_tokens(l, i0, i1, kPartThreads, [&](float x, int) {
+      if (x >= r.least) atomicAdd(&counts[bin_of(r, x)], 1u);
+    });
   __syncthreads();
   for (int i = threadIdx.x; i < kSampleBins; i += kPartThreads)
     if (counts[i] != 0) {
-      atomicAdd(&a.bin_weights[(int64_t)row * kSampleBins + i], weights[i]);
+      if (weigh) atomicAdd(&a.bin_weights[(int64_t)row * kSampleBins + i], weights[i]);
       atomicAdd(&a.bin_counts[(int64_t)row * kSampleBins + i], counts[i]);
     }
 }
 
 // Where a row's limits end, from its bins.
 struct Ends {
-  int first, last;            // bins between which top-p ends (top-k's, where there is no top-p): all before `first` is kept
+  int first, last;            // bins between which top-p ends (top-k's, where there is no top-p; all from the first one on by_list):
+                              // all before `first` is kept
   int k_bin;                  // the bin that top-k ends in, kSampleBins: none
   uint32_t k_need;            // tokens that top-k takes of it
   uint32_t listed_before_k;   // of the listed codes, those in bins before k_bin
@@ -354,7 +369,12 @@ __device__ void find_ends(const SampleArgs& a, int row, Ends& out, EndsShared& s
   }
   __syncthreads();
   const u64 most = by_k ? s.upto_k : total_w, least = by_k ? s.ends.before_k : total_w;
-  if (p < 1.0f) {
+  if (p < 1.0f && by_list(a, row)) {
+    if (threadIdx.x == 0) {
+      s.ends.first = 0;
+      s.ends.last = by_k ? s.ends.k_bin : kSampleBins - 1;   // all of the row, k or fewer tokens
+    }
+  } else if (p < 1.0f) {
     const u64 need0 = share_of(p, least), need1 = share_of(p, most);
     u64 x = uw;
 #pragma unroll
@@ -389,7 +409,10 @@ __global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(const Sample
   __shared__ double tab[64];
   __shared__ EndsShared ends_shared;
   __shared__ u64 sh[kPartThreads / 64];
+  __shared__ u64 listed[kPartListed];                        // this part's, one reservation of the row's list for all
+  __shared__ uint32_t n_here, at_row;
   const int row = blockIdx.y, part = blockIdx.x;
+  if (threadIdx.x == 0) n_here = 0;
   Row r;
   if (!row_setup(a, row, row_top(a, row), false, r)) return;
   if (threadIdx.x < 64) tab[threadIdx.x] = exp2(threadIdx.x / 64.0);
@@ -397,45 +420,101 @@ __global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(const Sample
   if (limited(a, row)) find_ends<kPartThreads>(a, row, ends, ends_shared);
   __syncthreads();
   const bool all = ends.first == kSampleBins;
+  // logits below `low` are in later bins, or below min-p where that is the only limit; the rounding of these lines is below its slack
+  float low = r.least;
+  {
+    const int after = (all ? kSampleBins : max(ends.last, ends.k_bin < kSampleBins ? ends.k_bin : 0)) + 1;
+    const double span = all ? (r.min_p > 0.0 ? -log(r.min_p) : INFINITY) / r.inv_t : after / (r.inv_t * r.bin_scale);
+    if (after < kSampleBins || (all && span < INFINITY)) {
+      const float x = (float)(r.top - span);
+      low = fmaxf(low, x - (float)((fabs(r.top) + span + 1.0 / r.inv_t) * 0x1p-22) - 1e-37f);
+    }
+  }
   u64 sum = 0;
   for_tokens(a.logits + (int64_t)row * a.row_stride, part * a.part_size, min(a.V, (part + 1) * a.part_size), kPartThreads, [&](float x, int i) {
-    if (x < r.least) return;
-    const Weight w = weight(r, x, tab);
-    if (w.n == 0) return;
+    if (x < low) return;
     const int b = all ? 0 : bin_of(r, x);
     if (b < ends.first) {
+      const Weight w = weight(r, x, tab);
       sum += w.e >= r.min_p ? w.n : 0;
     } else if (is_listed(ends, b)) {
-      const uint32_t at = atomicAdd(&a.n_listed[row], 1u);
-      if (at < kSampleListed) a.listed[(int64_t)row * kSampleListed + at] = token_code(x, i);
+      const uint32_t at = atomicAdd(&n_here, 1u);
+      if (at < kPartListed) {
+        listed[at] = token_code(x, i);
+      } else {
+        const uint32_t far = atomicAdd(&a.n_listed[row], 1u);
+        if (far < kSampleListed) a.listed[(int64_t)row * kSampleListed + far] = token_code(x, i);
+      }
     }
   });
   sum = add_lanes(sum);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = sum;
   __syncthreads();
-  if (threadIdx.x != 0) return;
-  for (int w = 1; w < kPartThreads / 64; ++w) sum += sh[w];
-  a.sums[(int64_t)row * a.n_parts + part] = sum;
+  const int n = min((int)n_here, kPartListed);
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kPartThreads / 64; ++w) sum += sh[w];
+    a.sums[(int64_t)row * a.n_parts + part] = sum;
+    if (n > 0) at_row = atomicAdd(&a.n_listed[row], (uint32_t)n);
+  }
+  if (n == 0) return;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kPartThreads)
+    if (at_row + i < kSampleListed) a.listed[(int64_t)row * kSampleListed + at_row + i] = listed[i];
 }
 
-// The n codes of a list, the largest first; the rest of the power of two that it is sorted in are 0.
+// The larger (or smaller) of a code and the one that `d` places away.
+__device__ __forceinline__ u64 keep(u64 x, u64 y, bool larger) { return (x > y) == larger ? x : y; }
+
+// Sorts the n codes of a list, the largest first, `size` a power of two with zeros behind them, kPer consecutive ones a lane: pairs
+// within a lane or a wave meet in registers, others in the list.  (all lanes)
+template <int kPer>
+__device__ void sort_codes(u64* list, int n, int size) {
+  const int at = threadIdx.x * kPer;
+  u64 x[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) x[j] = at + j < n ? list[at + j] : 0;
+  for (int run = 2; run <= size; run <<= 1)
+    for (int d = run >> 1; d > 0; d >>= 1) {
+      // whether this lane's lower code of a pair is the larger one, and whether it has the lower ones (d and run of kPer or more)
+      if (d >= 64 * kPer) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+          if (at < size) list[at + j] = x[j];
+        __syncthreads();
+        if (at < size) {
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) x[j] = keep(x[j], list[(at + j) ^ d], ((at & d) == 0) == ((at & run) == 0));
+        }
+      } else if (d >= kPer) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) x[j] = keep(x[j], __shfl_xor(x[j], d / kPer), ((at & d) == 0) == ((at & run) == 0));
+      } else {
+#pragma unroll
+        for (int e = 1; e < kPer; e <<= 1)
+          if (d == e) {
+            u64 y[kPer];
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) y[j] = keep(x[j], x[j ^ e], ((j & e) == 0) == (((at + j) & run) == 0));
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) x[j] = y[j];
+          }
+      }
+    }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kPer; ++j)
+    if (at + j < n) list[at + j] = x[j];
+  __syncthreads();
+}
+// (all lanes; the list is written)
 __device__ void sort_list(u64* list, int n) {
   int size = 64;
   while (size < n) size <<= 1;
-  for (int i = n + (int)threadIdx.x; i < size; i += kThreads) list[i] = 0;
-  __syncthreads();
-  for (int run = 2; run <= size; run <<= 1)
-    for (int d = run >> 1; d > 0; d >>= 1) {
-      for (int i = threadIdx.x; i < size / 2; i += kThreads) {
-        const int x = (i / d) * 2 * d + i % d, y = x + d;
-        const u64 u = list[x], v = list[y];
-        if ((u < v) == ((x & run) == 0)) {
-          list[x] = v;
-          list[y] = u;
-        }
-      }
-      __syncthreads();
-    }
+  if (size <= kThreads)
+    sort_codes<1>(list, n, size);
+  else
+    sort_codes<kSampleListed / kThreads>(list, n, size);
 }
 
 // The first place of a sorted list, of n, at which `base` and the weights up to it reach `need`; n - 1 if none.  (all lanes)
@@ -479,27 +558,54 @@ __device__ u64 list_weight(const Row& r, const u64* list, int n, Shared& s) {
   return total;
 }
 
+// Up to and with each lane's, in order.
+__device__ __forceinline__ u64 scan_lanes(u64 x) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const u64 before = __shfl_up(x, m);
+    x += (int)(threadIdx.x & 63) >= m ? before : 0;
+  }
+  return x;
+}
+
+// Up to 64 listed codes, one a lane: the largest first.
+__device__ __forceinline__ u64 sort_lanes(u64 c, int n) {
+  const int lane = threadIdx.x & 63;
+  int rank = 0;
+  for (int j = 0; j < n; ++j) {                              // n is the wave's
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)c, j), hi = __builtin_amdgcn_readlane((int)(uint32_t)(c >> 32), j);
+    rank += ((u64)hi << 32 | lo) > c;
+  }
+  const int to = 4 * (lane < n ? rank : lane);
+  const uint32_t lo = __builtin_amdgcn_ds_permute(to, (int)(uint32_t)c), hi = __builtin_amdgcn_ds_permute(to, (int)(uint32_t)(c >> 32));
+  return (u64)hi << 32 | lo;
+}
+
 // kListed: rows of up to kSampleListed tokens, all of them listed.
 template <bool kListed>
 __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs a) {
   __shared__ Shared s;
   __shared__ EndsShared ends_shared;
   __shared__ u64 parts[kSampleParts];
-  const int row = blockIdx.x, tid = threadIdx.x;
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const float* l = a.logits + (int64_t)row * a.row_stride;
   if (tid < 64) s.tab[tid] = exp2(tid / 64.0);
-  u64 top = 0;
+  u64 top = 0, early = 0;                                    // early: the first listed codes, every wave alike
+  uint32_t n_listed = 0;
   if constexpr (kListed) {
     for (int i = tid; i < a.V; i += kThreads) {
       const u64 c = s.list[i] = token_code(l[i], i);
       top = c > top ? c : top;
     }
     top = max_lanes(top);
-    if ((tid & 63) == 0) s.wave[tid >> 6] = top;
+    if (lane == 0) s.wave[tid >> 6] = top;
     __syncthreads();
     for (int w = 0; w < kWaves; ++w) top = s.wave[w] > top ? s.wave[w] : top;
     __syncthreads();
   } else {
+    n_listed = __builtin_amdgcn_readfirstlane((int)a.n_listed[row]);
+    early = a.listed[(int64_t)row * kSampleListed + lane];
+    for (int i = tid; i < a.n_parts; i += kThreads) parts[i] = a.sums[(int64_t)row * a.n_parts + i];
     top = row_top(a, row);
   }
   Row r;
@@ -509,10 +615,7 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
   const float p = a.top_p != nullptr ? a.top_p[row] : 1.0f;
   __syncthreads();
   const bool limit = limited(a, row);
-  // the tokens [i0, i1) hold the one that is picked, `target` of their kept weight before it; their parts' weights are in s.wave
-  int i0 = 0, i1 = a.V, size = (a.V + kWaves - 1) / kWaves;
-  u64 total;
-  bool searched = true;                                      // by parts of the row
+  bool searched = false;                                     // by parts of the row
   if constexpr (kListed) {
     if (limit) {
       sort_list(s.list, a.V);
@@ -521,60 +624,69 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
       r.cut = s.list[n - 1];
       __syncthreads();
     }
-    searched = false;
   } else {
     Ends ends = {kSampleBins, -1, kSampleBins, 0, 0, 0, 0};
     if (limit) find_ends<kThreads>(a, row, ends, ends_shared);
-    const uint32_t n_listed = limit ? a.n_listed[row] : 0;
-    for (int i = tid; i < a.n_parts; i += kThreads) parts[i] = a.sums[(int64_t)row * a.n_parts + i];
-    if (n_listed > kSampleListed) {
+    searched = !limit || n_listed <= kSampleListed;
+    if (!searched) {
       if (k > 0 && k < a.V) r.cut = find_cut(a, r, l, false, (u64)k, s);
       if (p < 1.0f) {
         Row whole = r;
         whole.min_p = 0.0;
-        r.cut = find_cut(a, r, l, true, share_of(p, part_weights(whole, l, 0, a.V, size, s)), s);
+        r.cut = find_cut(a, r, l, true, share_of(p, part_weights(whole, l, 0, a.V, (a.V + kWaves - 1) / kWaves, s)), s);
       }
-      searched = false;
     } else if (ends.first < kSampleBins) {
-      int n = (int)n_listed;
-      for (int i = tid; i < n; i += kThreads) s.list[i] = a.listed[(int64_t)row * kSampleListed + i];
-      __syncthreads();
-      sort_list(s.list, n);
-      u64 sum = 0;                                           // of top-k's tokens
-      if (ends.k_bin < kSampleBins) {
-        n = (int)(ends.listed_before_k + ends.k_need);
-        sum = ends.before_k + list_weight(r, s.list + ends.listed_before_k, (int)ends.k_need, s);
-      } else if (p < 1.0f) {
-        for (int i = 0; i < kThreads / 64; ++i) sum += ends_shared.weight[i];
-      }
-      if (p < 1.0f) n = reach(r, s.list, n, ends.before_first, share_of(p, sum), s) + 1;
-      r.cut = s.list[n - 1];
-      for (int i = tid; i < n; i += kThreads) {              // the listed tokens that are kept, to their parts
-        const u64 c = s.list[i];
+      // n: listed tokens of top-k; `from` on, their weight is added to `base`, and gives what top-p has a share of
+      const bool by_k = ends.k_bin < kSampleBins, whole = by_list(a, row);
+      int n = by_k ? (int)(ends.listed_before_k + ends.k_need) : (int)n_listed;
+      const int from = by_k && !whole ? (int)ends.listed_before_k : 0;
+      u64 base = by_k ? ends.before_k : 0;
+      if (!by_k && !whole)
+        for (int i = 0; i < kWaves; ++i) base += ends_shared.weight[i];
+      const bool add = by_k || whole;
+      auto to_part = [&](u64 c) {                            // a listed token that is kept, to its part
         const Weight w = weight(r, logit_of((uint32_t)(c >> kSampleIndexBits)), s.tab);
         if (w.e >= r.min_p) atomicAdd(&parts[token_of(c) / a.part_size], w.n);
+      };
+      if (n_listed <= 64) {                                  // every wave alike, without a barrier
+        const u64 c = sort_lanes(lane < (int)n_listed ? early : 0, (int)n_listed);
+        if (p < 1.0f) {
+          const u64 upto = scan_lanes(lane < n ? weight(r, logit_of((uint32_t)(c >> kSampleIndexBits)), s.tab).n : 0);
+          const u64 before = from > 0 ? __shfl(upto, from - 1) : 0;
+          const u64 need = share_of(p, base + (add ? __shfl(upto, n - 1) - before : 0));
+          const uint64_t past = __builtin_amdgcn_ballot_w64(lane < n && ends.before_first + upto >= need);
+          if (past != 0) n = __builtin_ctzll(past) + 1;
+        }
+        r.cut = __shfl(c, n - 1);
+        if (tid < n) to_part(c);
+      } else {
+        for (int i = tid; i < (int)n_listed; i += kThreads) s.list[i] = a.listed[(int64_t)row * kSampleListed + i];
+        __syncthreads();
+        sort_list(s.list, (int)n_listed);
+        if (p < 1.0f) {
+          if (add) base += list_weight(r, s.list + from, n - from, s);
+          n = reach(r, s.list, n, ends.before_first, share_of(p, base), s) + 1;
+        }
+        r.cut = s.list[n - 1];
+        for (int i = tid; i < n; i += kThreads) to_part(s.list[i]);
       }
     }
     __syncthreads();
   }
-  static_assert(kSampleParts == 128, "two parts a lane");
-  const int pair = 2 * (tid & 63);
-  u64 even = 0, odd = 0, upto = 0;                           // every wave alike: a lane's parts, and those up to them
+  // the tokens [i0, i1) hold the one that is picked, `target` of their kept weight before it
+  int i0 = 0, i1 = a.V;
+  u64 total = 0, target = 0;
+  auto set_target = [&]() {
+    target = u > 0.0 ? (u < 1.0 ? (u64)(int64_t)__builtin_floor(u * (double)total) : total - 1) : 0;
+    target = target < total ? target : total - 1;
+  };
   if (searched) {
-    even = pair < a.n_parts ? parts[pair] : 0;
-    odd = pair + 1 < a.n_parts ? parts[pair + 1] : 0;
-    upto = even + odd;
-    for (int d = 1; d < 64; d <<= 1) {
-      const u64 before = __shfl_up(upto, d);
-      upto += (tid & 63) >= d ? before : 0;
-    }
+    static_assert(kSampleParts == 128, "two parts a lane");
+    const int pair = 2 * lane;                               // every wave alike: a lane's parts, and those up to them
+    const u64 even = pair < a.n_parts ? parts[pair] : 0, odd = pair + 1 < a.n_parts ? parts[pair + 1] : 0;
+    const u64 upto = scan_lanes(even + odd);
     total = __shfl(upto, 63);
-  } else {
-    total = part_weights(r, l, 0, a.V, size, s);
-  }
-  u64 target = u > 0.0 ? (u < 1.0 ? (u64)(int64_t)__builtin_floor(u * (double)total) : total - 1) : 0;
-  target = target < total ? target : total - 1;
-  if (searched) {
+    set_target();
     const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > target));
     target -= __shfl(upto - odd - even, at);
     const u64 first = __shfl(even, at);
@@ -582,33 +694,48 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
     target -= second ? first : 0;
     i0 = (2 * at + second) * a.part_size;
     i1 = min(a.V, i0 + a.part_size);
-    size = (a.part_size + kWaves - 1) / kWaves;
-    part_weights(r, l, i0, i1, size, s);
   }
-  // the part that holds it, ever shorter
-  while (true) {
+  constexpr int kPer = 4;                                    // tokens of a lane in the end
+  for (bool first = !kListed && !searched; i1 - i0 > kPer * kThreads; first = false) {
+    const int size = (i1 - i0 + kWaves - 1) / kWaves;
+    const u64 sum = part_weights(r, l, i0, i1, size, s);
+    if (first) {
+      total = sum;
+      set_target();
+    }
     int w = 0;
     while (w < kWaves - 1 && target >= s.wave[w]) target -= s.wave[w++];
     i0 += w * size;
     i1 = min(i1, i0 + size);
-    if (size <= 64) break;
-    size = (size + kWaves - 1) / kWaves;
-    __syncthreads();
-    part_weights(r, l, i0, i1, size, s);
   }
-  // at most 64 tokens are left: a lane each
-  if (tid >= 64) return;
-  const int i = i0 + tid;
-  u64 run = i < i1 ? kept(r, l[i], i, s.tab) : 0;
-  for (int d = 1; d < 64; d <<= 1) {
-    const u64 before = __shfl_up(run, d);
-    run += tid >= d ? before : 0;
+  // a few consecutive tokens a lane
+  const int per = (i1 - i0 + kThreads - 1) / kThreads;
+  u64 mine[kPer], sum = 0;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int i = i0 + tid * per + j;
+    mine[j] = j < per && i < i1 ? kept(r, l[i], i, s.tab) : 0;
+    sum += mine[j];
   }
-  const uint64_t past = __builtin_amdgcn_ballot_w64(run > target);
-  if (past != 0 && tid == __builtin_ctzll(past)) {
-    a.tokens[row] = i;
-    if (a.logprobs != nullptr) a.logprobs[row] = (float)(((double)l[i] - r.top) * r.inv_t - (log((double)total) - a.bits * kLn2));
+  u64 run = scan_lanes(sum);
+  __syncthreads();
+  if (lane == 63) s.wave[tid >> 6] = run;
+  __syncthreads();
+  run -= sum;
+  for (int w = 0; w < tid >> 6; ++w) run += s.wave[w];
+  if constexpr (kListed) {
+    for (int w = 0; w < kWaves; ++w) total += s.wave[w];
+    set_target();
   }
+  if (target < run || target - run >= sum) return;           // one lane's range holds it
+  int i = i0 + tid * per;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    run += mine[j];
+    i += run <= target;
+  }
+  a.tokens[row] = i;
+  if (a.logprobs != nullptr) a.logprobs[row] = (float)(((double)l[i] - r.top) * r.inv_t - (log((double)total) - a.bits * kLn2));
 }
 
 }  // namespace
