@@ -7,13 +7,13 @@
 // of weights reaches its share, min-p at a weight.  So what is kept is `code >= cut && e^x >= min_p`, and the token is the first in
 // index order whose running sum of kept weights passes the random number's.
 //
-// Rows of up to kSampleListed tokens: a workgroup sorts the row's codes.  Longer ones in passes over the row, by many workgroups:
+// Rows of up to kSampleListed tokens: a workgroup holds the row's codes.  Longer ones in passes over the row, by many workgroups:
 //   top     the largest logit of every part of the row
 //   bins    count and weight of the row's tokens by weight (1,024 equal steps of the exponent down to weight 0), where a top-k or
 //           top-p may end inside the row.  The bins tell in which of them the two limits end.  Weights are left out where top-p is 1
 //           or the tokens of top-k are few (by_list): an exponential in fp64 costs more than all else in the pass
 //   parts   the weight of every part's tokens in the bins before those, and a list of the codes in them
-//   pick    a workgroup a row: the list, sorted, gives the cut; the parts' weights the part that holds the token, which is searched
+//   pick    a workgroup a row: the list gives the cut; the parts' weights the part that holds the token, which is searched
 // Where the list would be too long (thousands of tokens of nearly equal logits) the cut is found digit by digit instead (11, 11, 10
 // bits of the logit, twice 12 of the index): count or weight of the tokens that share the digits so far, by their next digit.
 #include "kvg_exp.h"
@@ -83,14 +83,19 @@ struct Digits {
   u64 weight[kBins];
   uint32_t count[kBins];
 };
+constexpr int kFew = 128;                 // codes that a wave sorts, two a lane
 struct Shared {
   double tab[64];
   u64 wave[kWaves];
   u64 found[2];
   union {
     Digits digits;
-    u64 list[kSampleListed];
+    struct {
+      u64 hi[kWaves], lo[kWaves], bins[kThreads], found, before;
+      uint32_t n;
+    } select;
   };
+  u64 few[2 * kFew];                  // unsorted, sorted
 };
 
 // The share p of a weight, rounded up: what a running sum has to reach.
@@ -191,7 +196,7 @@ __device__ __forceinline__ bool row_setup(const SampleArgs& a, int row, u64 top,
   r.cut = 0;
   // weights below half of 2^-bits are 0: no logit further below the top than (bits + 1) ln 2 t has one
   r.least = (float)(r.top - (a.bits + 2) * kLn2 * (double)t) ;
-  r.least = r.least - fabsf(r.least) * 0x1p-22f - 1e-37f;
+  r.least = fmaxf(r.least - fabsf(r.least) * 0x1p-22f - 1e-37f, -3.4028235e38f);
   r.bin_scale = kSampleBins / ((a.bits + 2) * kLn2);
   return true;
 }
@@ -462,102 +467,6 @@ __global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(const Sample
     if (at_row + i < kSampleListed) a.listed[(int64_t)row * kSampleListed + at_row + i] = listed[i];
 }
 
-// The larger (or smaller) of a code and the one that `d` places away.
-__device__ __forceinline__ u64 keep(u64 x, u64 y, bool larger) { return (x > y) == larger ? x : y; }
-
-// Sorts the n codes of a list, the largest first, `size` a power of two with zeros behind them, kPer consecutive ones a lane: pairs
-// within a lane or a wave meet in registers, others in the list.  (all lanes)
-template <int kPer>
-__device__ void sort_codes(u64* list, int n, int size) {
-  const int at = threadIdx.x * kPer;
-  u64 x[kPer];
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) x[j] = at + j < n ? list[at + j] : 0;
-  for (int run = 2; run <= size; run <<= 1)
-    for (int d = run >> 1; d > 0; d >>= 1) {
-      // whether this lane's lower code of a pair is the larger one, and whether it has the lower ones (d and run of kPer or more)
-      if (d >= 64 * kPer) {
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < kPer; ++j)
-          if (at < size) list[at + j] = x[j];
-        __syncthreads();
-        if (at < size) {
-#pragma unroll
-          for (int j = 0; j < kPer; ++j) x[j] = keep(x[j], list[(at + j) ^ d], ((at & d) == 0) == ((at & run) == 0));
-        }
-      } else if (d >= kPer) {
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) x[j] = keep(x[j], __shfl_xor(x[j], d / kPer), ((at & d) == 0) == ((at & run) == 0));
-      } else {
-#pragma unroll
-        for (int e = 1; e < kPer; e <<= 1)
-          if (d == e) {
-            u64 y[kPer];
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) y[j] = keep(x[j], x[j ^ e], ((j & e) == 0) == (((at + j) & run) == 0));
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) x[j] = y[j];
-          }
-      }
-    }
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < kPer; ++j)
-    if (at + j < n) list[at + j] = x[j];
-  __syncthreads();
-}
-// (all lanes; the list is written)
-__device__ void sort_list(u64* list, int n) {
-  int size = 64;
-  while (size < n) size <<= 1;
-  if (size <= kThreads)
-    sort_codes<1>(list, n, size);
-  else
-    sort_codes<kSampleListed / kThreads>(list, n, size);
-}
-
-// The first place of a sorted list, of n, at which `base` and the weights up to it reach `need`; n - 1 if none.  (all lanes)
-__device__ int reach(const Row& r, const u64* list, int n, u64 base, u64 need, Shared& s) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int per = (n + kThreads - 1) / kThreads, j0 = threadIdx.x * per;
-  u64 sum = 0;
-  for (int j = j0; j < min(n, j0 + per); ++j) sum += weight(r, logit_of((uint32_t)(list[j] >> kSampleIndexBits)), s.tab).n;
-  u64 upto = sum;
-  for (int m = 1; m < 64; m <<= 1) {
-    const u64 x = __shfl_up(upto, m);
-    upto += lane >= m ? x : 0;
-  }
-  __syncthreads();
-  if (lane == 63) s.wave[wave] = upto;
-  if (threadIdx.x == 0) s.found[0] = (u64)(n - 1);
-  __syncthreads();
-  u64 run = base + upto - sum;
-  for (int w = 0; w < wave; ++w) run += s.wave[w];
-  if (run < need)
-    for (int j = j0; j < min(n, j0 + per); ++j) {
-      run += weight(r, logit_of((uint32_t)(list[j] >> kSampleIndexBits)), s.tab).n;
-      if (run >= need) {
-        s.found[0] = (u64)j;
-        break;
-      }
-    }
-  __syncthreads();
-  return (int)s.found[0];
-}
-// The weight of the first n codes of a list.  (all lanes)
-__device__ u64 list_weight(const Row& r, const u64* list, int n, Shared& s) {
-  u64 sum = 0;
-  for (int j = threadIdx.x; j < n; j += kThreads) sum += weight(r, logit_of((uint32_t)(list[j] >> kSampleIndexBits)), s.tab).n;
-  sum = add_lanes(sum);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s.wave[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  u64 total = 0;
-  for (int w = 0; w < kWaves; ++w) total += s.wave[w];
-  return total;
-}
-
 // Up to and with each lane's, in order.
 __device__ __forceinline__ u64 scan_lanes(u64 x) {
 #pragma unroll
@@ -568,17 +477,129 @@ __device__ __forceinline__ u64 scan_lanes(u64 x) {
   return x;
 }
 
-// Up to 64 listed codes, one a lane: the largest first.
-__device__ __forceinline__ u64 sort_lanes(u64 c, int n) {
-  const int lane = threadIdx.x & 63;
-  int rank = 0;
-  for (int j = 0; j < n; ++j) {                              // n is the wave's
-    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)c, j), hi = __builtin_amdgcn_readlane((int)(uint32_t)(c >> 32), j);
-    rank += ((u64)hi << 32 | lo) > c;
-  }
-  const int to = 4 * (lane < n ? rank : lane);
-  const uint32_t lo = __builtin_amdgcn_ds_permute(to, (int)(uint32_t)c), hi = __builtin_amdgcn_ds_permute(to, (int)(uint32_t)(c >> 32));
+__device__ __forceinline__ u64 code_weight(const Row& r, u64 c, const double* tab) {
+  return weight(r, logit_of((uint32_t)(c >> kSampleIndexBits)), tab).n;
+}
+// Up to kFew codes in the first wave, without a barrier: the largest first, lane i has the ones at 2 i and 2 i + 1 (0: none).
+struct Few {
+  u64 a, b;
+  __device__ __forceinline__ u64 at(int i) const { return __shfl(i & 1 ? b : a, i >> 1); }
+};
+__device__ __forceinline__ u64 from_lane(u64 x, int j) {
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, j), hi = __builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), j);
   return (u64)hi << 32 | lo;
+}
+// a, b: the lane's, the codes at `lane` and `lane + 64` of n (the wave's)
+__device__ __forceinline__ Few sort_few(u64 a, u64 b, int n, u64* sorted) {
+  const int lane = threadIdx.x & 63;
+  int at_a = 0, at_b = 0;
+  for (int j = 0; j < min(n, 64); ++j) {
+    const u64 c = from_lane(a, j);
+    at_a += c > a;
+    at_b += c > b;
+  }
+  for (int j = 0; j < n - 64; ++j) {
+    const u64 c = from_lane(b, j);
+    at_a += c > a;
+    at_b += c > b;
+  }
+  if (lane < n) sorted[at_a] = a;
+  if (lane + 64 < n) sorted[at_b] = b;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  return {2 * lane < n ? sorted[2 * lane] : 0, 2 * lane + 1 < n ? sorted[2 * lane + 1] : 0};
+}
+// The first place at which the weights wa, wb up to it reach `need`; n - 1 if none.
+__device__ __forceinline__ int reach_few(u64 wa, u64 wb, u64 need, int n) {
+  const u64 upto = scan_lanes(wa + wb);
+  const uint64_t past = __builtin_amdgcn_ballot_w64(upto >= need);
+  if (past == 0) return n - 1;
+  const int at = __builtin_ctzll(past);
+  return min(2 * at + (__shfl(upto - wb, at) < need), n - 1);
+}
+
+// The sum over the workgroup.  (all lanes)
+__device__ u64 sum_block(u64 x, Shared& s) {
+  x = add_lanes(x);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s.wave[threadIdx.x >> 6] = x;
+  __syncthreads();
+  u64 total = 0;
+  for (int w = 0; w < kWaves; ++w) total += s.wave[w];
+  return total;
+}
+
+// Listed codes of a lane (0: none).
+constexpr int kHeld = kSampleListed / kThreads;
+// The code at which the count (or, by_weight, the weight) of the codes, from the largest on, reaches `need`; the least one if it does not.
+// The codes are put into bins by their logit, or where all are equal by index, linearly between the largest and the least, and all but
+// those of the bin where that happens are dropped, until kFew are left.  (all lanes; finite logits; the next call may follow at once)
+__device__ u64 select(const Row& r, const u64 (&codes)[kHeld], bool by_weight, u64 need, Shared& s) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto& t = s.select;
+  u64 c[kHeld];
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) c[j] = codes[j];
+  while (true) {
+    u64 hi = 0, low = 0;                                     // low: of the inverted codes, as the least is sought
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      hi = c[j] > hi ? c[j] : hi;
+      low = c[j] != 0 && ~c[j] > low ? ~c[j] : low;
+    }
+    hi = max_lanes(hi);
+    low = max_lanes(low);
+    __syncthreads();
+    if (lane == 0) {
+      t.hi[wave] = hi;
+      t.lo[wave] = low;
+    }
+    t.bins[tid] = 0;
+    if (tid == 0) t.n = 0;
+    __syncthreads();
+    hi = max_lanes(lane < kWaves ? t.hi[lane] : 0);
+    const u64 lo = ~max_lanes(lane < kWaves ? t.lo[lane] : 0);
+    const bool equal = hi >> kSampleIndexBits == lo >> kSampleIndexBits;
+    auto value = [&](u64 x) -> double { return equal ? (double)(x & kIndexMask) : (double)logit_of((uint32_t)(x >> kSampleIndexBits)); };
+    const double first = value(hi), range = first - value(lo), scale = range > 0.0 ? (kThreads - 1) / range : 0.0;
+    auto bin = [&](u64 x) -> int { return min((int)((first - value(x)) * scale), kThreads - 1); };
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+      if (c[j] != 0) atomicAdd(&t.bins[bin(c[j])], by_weight ? code_weight(r, c[j], s.tab) : 1);
+    __syncthreads();
+    const u64 mine = t.bins[tid];
+    u64 upto = scan_lanes(mine);
+    if (lane == 63) s.wave[wave] = upto;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) upto += s.wave[w];
+    if (upto - mine < need && (upto >= need || tid == kThreads - 1)) {
+      t.found = (u64)tid;
+      t.before = upto - mine;
+    }
+    __syncthreads();
+    need -= t.before;
+    const int found = (int)t.found;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+      if (c[j] != 0) {
+        if (bin(c[j]) != found) {
+          c[j] = 0;
+        } else {
+          const uint32_t at = atomicAdd(&t.n, 1u);
+          if (at < kFew) s.few[at] = c[j];
+        }
+      }
+    __syncthreads();
+    if (t.n <= kFew) break;
+  }
+  if (tid < 64) {
+    const int n = __builtin_amdgcn_readfirstlane((int)t.n);
+    const Few x = sort_few(lane < n ? s.few[lane] : 0, lane + 64 < n ? s.few[lane + 64] : 0, n, s.few + kFew);
+    const int at = by_weight ? reach_few(2 * lane < n ? code_weight(r, x.a, s.tab) : 0, 2 * lane + 1 < n ? code_weight(r, x.b, s.tab) : 0, need, n)
+                             : (int)min(need, (u64)n) - 1;
+    t.found = x.at(at);
+  }
+  __syncthreads();
+  return t.found;
 }
 
 // kListed: rows of up to kSampleListed tokens, all of them listed.
@@ -590,11 +611,11 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const float* l = a.logits + (int64_t)row * a.row_stride;
   if (tid < 64) s.tab[tid] = exp2(tid / 64.0);
-  u64 top = 0, early = 0;                                    // early: the first listed codes, every wave alike
+  u64 top = 0, early[2] = {0, 0};                            // early: the first listed codes
   uint32_t n_listed = 0;
   if constexpr (kListed) {
     for (int i = tid; i < a.V; i += kThreads) {
-      const u64 c = s.list[i] = token_code(l[i], i);
+      const u64 c = token_code(l[i], i);
       top = c > top ? c : top;
     }
     top = max_lanes(top);
@@ -604,7 +625,8 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
     __syncthreads();
   } else {
     n_listed = __builtin_amdgcn_readfirstlane((int)a.n_listed[row]);
-    early = a.listed[(int64_t)row * kSampleListed + lane];
+    early[0] = a.listed[(int64_t)row * kSampleListed + lane];
+    early[1] = a.listed[(int64_t)row * kSampleListed + 64 + lane];
     for (int i = tid; i < a.n_parts; i += kThreads) parts[i] = a.sums[(int64_t)row * a.n_parts + i];
     top = row_top(a, row);
   }
@@ -618,11 +640,18 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
   bool searched = false;                                     // by parts of the row
   if constexpr (kListed) {
     if (limit) {
-      sort_list(s.list, a.V);
-      int n = k > 0 && k < a.V ? k : a.V;
-      if (p < 1.0f) n = reach(r, s.list, n, 0, share_of(p, list_weight(r, s.list, n, s)), s) + 1;
-      r.cut = s.list[n - 1];
-      __syncthreads();
+      u64 c[kHeld], sum = 0;
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) {
+        const int i = tid + j * kThreads;
+        c[j] = i < a.V && l[i] >= r.least ? token_code(l[i], i) : 0;
+      }
+      if (k > 0 && k < a.V) r.cut = select(r, c, false, (u64)k, s);
+      if (p < 1.0f) {
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) sum += c[j] != 0 && c[j] >= r.cut ? code_weight(r, c[j], s.tab) : 0;
+        r.cut = select(r, c, true, share_of(p, sum_block(sum, s)), s);
+      }
     }
   } else {
     Ends ends = {kSampleBins, -1, kSampleBins, 0, 0, 0, 0};
@@ -636,42 +665,56 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
         r.cut = find_cut(a, r, l, true, share_of(p, part_weights(whole, l, 0, a.V, (a.V + kWaves - 1) / kWaves, s)), s);
       }
     } else if (ends.first < kSampleBins) {
-      // n: listed tokens of top-k; `from` on, their weight is added to `base`, and gives what top-p has a share of
-      const bool by_k = ends.k_bin < kSampleBins, whole = by_list(a, row);
+      // n: listed tokens of top-k.  What top-p has a share of: `base` and, where top-k or by_list say, the weight of those of them that
+      // no bin's weight holds
+      const bool by_k = ends.k_bin < kSampleBins, whole = by_list(a, row), add = by_k || whole;
       int n = by_k ? (int)(ends.listed_before_k + ends.k_need) : (int)n_listed;
-      const int from = by_k && !whole ? (int)ends.listed_before_k : 0;
       u64 base = by_k ? ends.before_k : 0;
-      if (!by_k && !whole)
+      if (!add)
         for (int i = 0; i < kWaves; ++i) base += ends_shared.weight[i];
-      const bool add = by_k || whole;
       auto to_part = [&](u64 c) {                            // a listed token that is kept, to its part
         const Weight w = weight(r, logit_of((uint32_t)(c >> kSampleIndexBits)), s.tab);
         if (w.e >= r.min_p) atomicAdd(&parts[token_of(c) / a.part_size], w.n);
       };
-      if (n_listed <= 64) {                                  // every wave alike, without a barrier
-        const u64 c = sort_lanes(lane < (int)n_listed ? early : 0, (int)n_listed);
+      if (n_listed <= kFew && tid >= 64) {
+      } else if (n_listed <= kFew) {
+        const int all = (int)n_listed, i = 2 * lane;
+        const Few x = sort_few(lane < all ? early[0] : 0, lane + 64 < all ? early[1] : 0, all, s.few);
         if (p < 1.0f) {
-          const u64 upto = scan_lanes(lane < n ? weight(r, logit_of((uint32_t)(c >> kSampleIndexBits)), s.tab).n : 0);
-          const u64 before = from > 0 ? __shfl(upto, from - 1) : 0;
-          const u64 need = share_of(p, base + (add ? __shfl(upto, n - 1) - before : 0));
-          const uint64_t past = __builtin_amdgcn_ballot_w64(lane < n && ends.before_first + upto >= need);
-          if (past != 0) n = __builtin_ctzll(past) + 1;
+          u64 wa = i < n ? code_weight(r, x.a, s.tab) : 0, wb = i + 1 < n ? code_weight(r, x.b, s.tab) : 0;
+          const int from = by_k && !whole ? (int)ends.listed_before_k : 0;
+          if (add) base += add_lanes((i >= from ? wa : 0) + (i + 1 >= from ? wb : 0));
+          n = reach_few(wa, wb, share_of(p, base) - ends.before_first, n) + 1;
         }
-        r.cut = __shfl(c, n - 1);
-        if (tid < n) to_part(c);
+        r.cut = x.at(n - 1);
+        if (i < n) to_part(x.a);
+        if (i + 1 < n) to_part(x.b);
+        s.found[0] = r.cut;
       } else {
-        for (int i = tid; i < (int)n_listed; i += kThreads) s.list[i] = a.listed[(int64_t)row * kSampleListed + i];
-        __syncthreads();
-        sort_list(s.list, (int)n_listed);
-        if (p < 1.0f) {
-          if (add) base += list_weight(r, s.list + from, n - from, s);
-          n = reach(r, s.list, n, ends.before_first, share_of(p, base), s) + 1;
+        u64 c[kHeld], sum = 0;
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+          const int i = tid + j * kThreads;
+          c[j] = i < (int)n_listed ? a.listed[(int64_t)row * kSampleListed + i] : 0;
         }
-        r.cut = s.list[n - 1];
-        for (int i = tid; i < n; i += kThreads) to_part(s.list[i]);
+        if (by_k) r.cut = select(r, c, false, (u64)n, s);
+        if (p < 1.0f) {
+          if (add) {
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j)
+              if (c[j] != 0 && c[j] >= r.cut && (whole || bin_of(r, logit_of((uint32_t)(c[j] >> kSampleIndexBits))) == ends.k_bin))
+                sum += code_weight(r, c[j], s.tab);
+            base += sum_block(sum, s);
+          }
+          r.cut = select(r, c, true, share_of(p, base) - ends.before_first, s);
+        }
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+          if (c[j] != 0 && c[j] >= r.cut) to_part(c[j]);
       }
     }
     __syncthreads();
+    if (limit && n_listed <= kFew && ends.first < kSampleBins) r.cut = s.found[0];
   }
   // the tokens [i0, i1) hold the one that is picked, `target` of their kept weight before it
   int i0 = 0, i1 = a.V;
