@@ -33,14 +33,17 @@ struct SampleArgs {
 
 // Bins of a row's tokens by their weight, the heaviest first.
 constexpr int kSampleBins = 1024;
-// Codes that a workgroup sorts.
+// Codes that a workgroup holds.
 constexpr int kSampleListed = 4096;
 
-// Parts of a row: enough to spread few rows over the chip, multiples of 1,024 tokens.
+// Parts of a row, multiples of 1,024 tokens: few rows need many to spread over the chip, of more each part's workgroup should have
+// more than its start to do.  Rows of 262,144 tokens with top-k, top-p and min-p, us, 128 parts / 64 / 32 / 8: 1 row 28.6 / 28.5, 16 rows 46 / 41 /
+// 42, 64 rows 97 / 77 / 73, 256 rows 292 / 178 / 177 / 187.  Of 32,000 tokens, parts of 1,024 / 2,048 / 4,096 / 8,192: 1 row 25.9 at all, 16
+// rows 32 / 31 / 31 / 36, 64 rows 46 / 37 / 35 / 39, 256 rows 87 / 62 / 52 / 50.
 constexpr int kSampleParts = 128;
 inline int sample_part_size(int64_t rows, int64_t V) {
-  const int64_t want = rows < 16 ? kSampleParts : rows < 1024 ? 2048 / rows : 2;
-  return (int)(((V + want - 1) / want + 1023) / 1024 * 1024);
+  const int64_t want = rows < 16 ? kSampleParts : rows < 32 ? 64 : 32, least = rows < 16 ? 1024 : 4096;
+  return (int)(((V + want - 1) / want + least - 1) / least * least);
 }
 
 hipError_t launch_sample(const SampleArgs& a, hipStream_t stream);
