@@ -17,21 +17,46 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// eight values times inv, rounded, as bytes; |x * inv| <= 127 but for the last bits
+// Eight values times inv, rounded to integers, as bytes.  |x inv| <= 127 but for a few last bits, so 1.5 2^23 added to it rounds it to
+// the nearest even and leaves the integer in the low byte.
 __device__ __forceinline__ u32x2 to_int8(const float (&x)[8], float inv) {
-  uint32_t w[2] = {0, 0};
+#pragma clang fp contract(off)
+  constexpr float kRound = 12582912.0f;
+  uint32_t n[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) n[e] = __float_as_uint(x[e] * inv + kRound);
+  auto four = [&](int e) -> uint32_t {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(n[e + 3], n[e + 2], 0x0C0C0400u), __builtin_amdgcn_perm(n[e + 1], n[e], 0x0C0C0400u), 0x05040100u);
+  };
+  return (u32x2){four(0), four(4)};
+}
+
+// A page's cosines and sines: a lane's eight pairs lie 80 bytes from its neighbour's, so that a wave's 16-byte reads meet all banks
+// alike (64 bytes apart, half the reads' time was conflicts).
+constexpr int turn_at(int pair) { return pair + pair / 8 * 2; }
+
+// y: the values of this lane's partners (half pairing).  Where all of a head turns they are half a head's lanes away.
+template <int D>
+__device__ __forceinline__ void partners(const Place& p, bool whole, int e0, const float (&x)[8], float (&y)[8]) {
+  if (D == 64 || !whole) {
+    from_partner<8>(p, e0, x, y);
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float n = fminf(fmaxf(__builtin_rintf(x[e] * inv), -kInt8Max), kInt8Max);
-    w[e / 4] |= ((uint32_t)(int)n & 0xFFu) << (8 * (e % 4));
+    if constexpr (D == 128) {
+      y[e] = __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x[e]), 0x128, 0xF, 0xF, true));      // rows of 16 by 8
+    } else {
+      const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[e]), __float_as_uint(x[e]), false, false);
+      y[e] = __uint_as_float(threadIdx.x & 16 ? both[0] : both[1]);
+    }
   }
-  return (u32x2){w[0], w[1]};
 }
 
 template <int D, typename Axes>
 __global__ __launch_bounds__(kThreads) void int8_append_kernel(const NormAppendArgs a, const Int8Scales scales, const Axes axes) {
   constexpr int VECS = D / 8, RPP = 64 / VECS, NP = kPage / RPP;      // lanes of a row, rows at a time, times
-  __shared__ float2 cs[kPage][D / 2];
+  __shared__ __attribute__((aligned(16))) float2 cs[kPage][turn_at(D / 2)];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int e0 = lane % VECS * 8, r0 = lane / VECS;
   const Place p = place(a.rot, e0);
@@ -51,7 +76,7 @@ __global__ __launch_bounds__(kThreads) void int8_append_kernel(const NormAppendA
   const int half = a.rot.dim / 2;
   for (int i = threadIdx.x; i < n * half; i += kThreads) {
     const int r = i / half, j = i % half;
-    cs[r][j] = turn(a.rot, pair_position(axes, pos0 + r, tok0 + r, a.seqs.n_tokens, j), j);
+    cs[r][turn_at(j)] = turn(a.rot, pair_position(axes, pos0 + r, tok0 + r, a.seqs.n_tokens, j), j);
   }
   __syncthreads();
 
@@ -108,8 +133,8 @@ __global__ __launch_bounds__(kThreads) void int8_append_kernel(const NormAppendA
         }
         if (is_q || is_k) {
           float y[8];
-          if (a.rot.pairing == 0) from_partner<8>(p, e0, x[i], y);
-          rotate_values(p, a.rot.pairing, cs[min(i * RPP + r0, n - 1)], x[i], y);
+          if (a.rot.pairing == 0) partners<D>(p, a.rot.dim == D, e0, x[i], y);
+          rotate_values(p, a.rot.pairing, cs[min(i * RPP + r0, n - 1)] + (turn_at(p.pair) - p.pair), x[i], y);
         }
         if (is_q) {
           const int r = i * RPP + r0;
