@@ -180,3 +180,46 @@ def test_frequencies(kvg):
     tokens, _ = run(kvg, logits.expand(n, 30).contiguous(), [1.0] * n, u)
     share = torch.softmax(logits[0].double(), 0).cpu().numpy()
     assert np.abs(np.bincount(tokens, minlength=30) / n - share).max() <= 2.0 / n
+
+
+@pytest.mark.parametrize("V", [4000, 50021])
+def test_limits_among_many_close_logits(kvg, V):
+    """Hundreds to thousands of tokens of nearly or exactly equal logits where a limit ends, side by side in a part of the row or
+    all over it, fewer and more of them than are listed; a few far above them or none."""
+    rng = np.random.default_rng(V)
+    rows = []
+    for spread in (0.0, 1e-6, 0.01, 0.3, 3.0):
+        for n in (150, 700, 3000, V):
+            for together in (True, False):
+                x = rng.uniform(-40.0, -30.0, V)
+                at = np.arange(500, 500 + n) % V if together else rng.permutation(V)[:n]
+                x[at] = 2.0 + spread * rng.random(n)
+                x[rng.integers(0, V, 3)] = [7.0, 6.5, 6.0]
+                rows.append(x)
+    R = len(rows)
+    logits = torch.from_numpy(np.stack(rows).astype(np.float32)).cuda()
+    pick = lambda x: np.array([x[i % len(x)] for i in range(R)])  # noqa: E731
+    u, temperature = rng.random(R), pick([1.0, 0.7, 1.3])
+    for limits in (dict(top_k=pick([40, 100, 600, 900, 2000])), dict(top_p=pick([0.5, 0.9, 0.1, 0.99])),
+                   dict(top_k=pick([40, 100, 600, 900, 1500]), top_p=pick([0.5, 0.9, 0.99])),
+                   dict(top_k=pick([1024, 1025, 3000]), top_p=pick([0.3, 0.8]), min_p=pick([0.0, 0.001]))):
+        tokens, logprobs = run(kvg, logits, temperature, u, **limits)
+        compare(logits, temperature, u, tokens, logprobs, **limits)
+
+
+def test_logits_far_apart(kvg):
+    """Finite logits at the ends of fp32's range and temperatures at its ends."""
+    V = 3000
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((6, V)).astype(np.float32)
+    x[0, 5], x[0, 6] = 3.4e38, -3.4e38
+    x[1] *= np.float32(1e-38)
+    x[2, 100:] = -np.inf
+    x[3] *= np.float32(1e37)
+    temperature = [1.0, 1e-38, 1.0, 1e38, 1e-30, 3e38]
+    u = rng.random(6)
+    logits = torch.from_numpy(x).cuda()
+    for limits in (dict(), dict(top_k=[50] * 6), dict(top_p=[0.9] * 6), dict(top_k=[200] * 6, top_p=[0.7] * 6, min_p=[0.01] * 6)):
+        limits = {k: np.array(v) for k, v in limits.items()}
+        tokens, logprobs = run(kvg, logits, temperature, u, **limits)
+        compare(logits, temperature, u, tokens, logprobs, **limits)
