@@ -24,6 +24,8 @@ inline int64_t int8_append_units(const PackedSeqs& s) {
   return most < s.n_tokens ? most : s.n_tokens;
 }
 
+// dimensions of the values that a workgroup of a split tile launch sums
+constexpr int int8_split_values(int D) { return D == 256 ? 128 : D; }
 // attention: PackedAttnArgs with int8 pools (launch_packed_tiles, launch_packed_few for int8 caches)
 hipError_t launch_int8_tiles(const PackedAttnArgs& a, const Int8Scales& s, hipStream_t stream);
 hipError_t launch_int8_few(const PackedAttnArgs& a, const Int8Scales& s, hipStream_t stream);

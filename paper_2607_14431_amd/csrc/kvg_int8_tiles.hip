@@ -27,15 +27,18 @@ namespace {
 constexpr int kTileKeys = 64;
 constexpr int kSegTiles = kPackedSeg / kTileKeys, kSegPages = kPackedSeg / kPage;
 constexpr int kWaves = 4;
-// kSplitKeys: a workgroup takes one segment and leaves its partial.
-template <int D, bool kSplitKeys>
-__global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kernel(const PackedAttnArgs a, const Int8Scales scales) {
+// kSplitKeys: a workgroup takes one segment and leaves its partial.  DV: dimensions of the values that a workgroup sums, all of them or
+// half (the scores are then computed twice).  Waves a SIMD are what the registers give; head_dim 64 is held to three, without which the
+// compiler takes one register more than they have: 16 prompts of up to 4,096 tokens, 4 heads on 2, 116 us, with two waves 129.
+template <int D, int DV, bool kSplitKeys>
+__global__ __launch_bounds__(64 * kWaves, DV == 256 ? 1 : D == 64 ? (kSplitKeys ? 4 : 3) : 2) void int8_tiles_kernel(const PackedAttnArgs a, const Int8Scales scales) {
   constexpr int NS = D / 32;               // score steps over head_dim
-  constexpr int ND = D / 32;               // 32-wide blocks of head_dim
+  constexpr int ND = DV / 32;              // 32-wide blocks of the values' dimensions
+  constexpr int kParts = D / DV;
   constexpr int BM = kTilePairs;
   static_assert(BM == 32 * kWaves, "a block of 32 pairs per wave");
   using KR = KRows<D>;
-  using VR = VRows<2 * D>;
+  using VR = VRows<2 * DV>;
   // a wave brings one page of a tile; the V stages first, where an LDS instruction's immediate offset reaches
   __shared__ __attribute__((aligned(1024))) char sA_V0[kWaves * VR::kPageBytes];
   __shared__ __attribute__((aligned(1024))) char sA_V1[kWaves * VR::kPageBytes];
@@ -50,6 +53,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
 
   // ---- (tile, layer, segment, KV head), the KV head fastest; late tiles, which have the most keys, first (as packed_tiles_kernel)
   uint32_t id = blockIdx.x;
+  const int part = kParts == 1 ? 0 : (int)(id % kParts);
+  id /= kParts;
   const int g = (int)(id % (uint32_t)a.Hkv);
   id /= (uint32_t)a.Hkv;
   int seg = 0;
@@ -115,20 +120,20 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
     load_page<KR, 0>(kpool + slab_of(kt), rows_of(kt), dk, source);
   };
   // V: 16 bytes of a row are a lane's.  Its row and place of load j are such that the lanes' stores of widened values lie side by side.
-  constexpr int kVLoads = D / 64;
+  constexpr int kVLoads = DV / 64;
   constexpr int kLines = VR::kRows;                      // rows whose 16-byte chunks lie side by side
-  const int v_row = lane % kLines + lane / 32 * (32 / (D / 16)), v_col = lane % 32 / kLines;
-  const int v_source = v_row * D + v_col * 16;
-  static_assert(32 / (D / 16) == kLines, "half a wave takes kLines rows");
+  const int v_row = lane % kLines + lane / 32 * (32 / (DV / 16)), v_col = lane % 32 / kLines;
+  const int v_source = v_row * D + part * DV + v_col * 16;
+  static_assert(32 / (DV / 16) == kLines, "half a wave takes kLines rows");
   const int v_store = wave * VR::kPageBytes + VR::at(v_row, 2 * v_col);
   constexpr int kNextChunk = VR::at(0, 1), kNextLoad = 2 * VR::kLoad;
-  static_assert(1024 / D == 2 * kLines, "a load takes 2 kLines rows");
+  static_assert(1024 / DV == 2 * kLines, "a load takes 2 kLines rows");
   uint4 v_raw[kVLoads];
   auto issue_v = [&](int kt) {
     const __amdgpu_buffer_rsrc_t rs =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(vpool + slab_of(kt)), 0, rows_of(kt) * D, kBufferWord3);
 #pragma unroll
-    for (int j = 0; j < kVLoads; ++j) v_raw[j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, v_source, 1024 * j, 0));
+    for (int j = 0; j < kVLoads; ++j) v_raw[j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, v_source, 2 * kLines * D * j, 0));
   };
   auto widen_v = [&](auto stage, int j) {
     char* to = (decltype(stage)::value ? sA_V1 : sA_V0) + v_store + j * kNextLoad;
@@ -157,7 +162,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
     if constexpr (!kSplitKeys) o_run[d] = splat(0.0f);
   }
 
-  const int k_lane = k_lane_base<D, false>(lane), v_lane = v_lane_base<2 * D, false>(lane);
+  const int k_lane = k_lane_base<D, false>(lane), v_lane = v_lane_base<2 * DV, false>(lane);
 
   using Stage0 = std::integral_constant<int, 0>;
   using Stage1 = std::integral_constant<int, 1>;
@@ -206,7 +211,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
     const lds_char* vbase = (const lds_char*)(lds_void*)(ST ? sA_V1 : sA_V0) + v_lane;
     const bool need_mask = key0 + kTileKeys - 1 > wave_first || key0 < mask_lo;
     auto kread = [&](int f) { return int8_k_fragment<D>(kbase + KR::at(32 * (f / NS), 0), f % NS); };          // f = block * NS + step
-    auto vread = [&](int t) { return v_fragment<2 * D, false>(vbase + VR::at(16 * (t / ND), 0), t % ND); };    // t = 16-key step * ND + d
+    auto vread = [&](int t) { return v_fragment<2 * DV, false>(vbase + VR::at(16 * (t / ND), 0), t % ND); };    // t = 16-key step * ND + d
     // -Inf where the row does not see the key
     auto mask = [&](f32x16& s, int kb) __attribute__((always_inline)) {
       if (need_mask) {
@@ -311,20 +316,20 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
     if (idle) return;
     end_segment();
     const int64_t block = part_block(a, a.part.n_seg, l, slot, g, kWaves, wave, seg);
-    float* op = a.part.acc + block * (32 * D) + lane * 4;
+    float* op = a.part.acc + block * (32 * D) + part * (32 * DV) + lane * 4;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4)
         *reinterpret_cast<float4*>(op + (d * 4 + r4) * 256) =
             make_float4(o[d][r4 * 4], o[d][r4 * 4 + 1], o[d][r4 * 4 + 2], o[d][r4 * 4 + 3]);
-    if (half == 0) *reinterpret_cast<float2*>(a.part.ml + (block * 32 + lrow) * 2) = make_float2(st.m, st.l);
+    if (half == 0 && part == 0) *reinterpret_cast<float2*>(a.part.ml + (block * 32 + lrow) * 2) = make_float2(st.m, st.l);
   } else {
     fold();
     if (!row_ok) return;
     const float inv = 1.0f / l_run;
     const int64_t tok = (int64_t)l * a.seqs.n_tokens + sq.row0 + row;
-    uint16_t* op = static_cast<uint16_t*>(a.out) + (tok * a.Hq + g * a.group + ((pair0 + lrow) & (a.group - 1))) * D;
+    uint16_t* op = static_cast<uint16_t*>(a.out) + (tok * a.Hq + g * a.group + ((pair0 + lrow) & (a.group - 1))) * D + part * DV;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -337,11 +342,15 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void int8_tiles_kern
 
 template <int D>
 hipError_t launch_d(const PackedAttnArgs& a, const Int8Scales& s, hipStream_t stream) {
-  const dim3 grid((unsigned)packed_tile_workgroups(a));
-  if (a.part.n_seg > 1)
-    int8_tiles_kernel<D, true><<<grid, 64 * kWaves, 0, stream>>>(a, s);
-  else
-    int8_tiles_kernel<D, false><<<grid, 64 * kWaves, 0, stream>>>(a, s);
+  const int64_t grid = packed_tile_workgroups(a);
+  // Where the running sums of the segments are not held, half of 256 dimensions lets two workgroups share a compute unit: 512 tokens over
+  // 4,096 99 us (with all of them 112), 4 x 35 over 32,768 164 (169).
+  if (a.part.n_seg > 1) {
+    constexpr int DV = int8_split_values(D);
+    int8_tiles_kernel<D, DV, true><<<(unsigned)(grid * (D / DV)), 64 * kWaves, 0, stream>>>(a, s);
+  } else {
+    int8_tiles_kernel<D, D, false><<<(unsigned)grid, 64 * kWaves, 0, stream>>>(a, s);
+  }
   return hipGetLastError();
 }
 

@@ -10,6 +10,7 @@
 
 #include "kvg.h"
 #include "kvg_host.h"
+#include "kvg_int8.h"
 #include "kvg_launch.h"
 #include "kvg_packed.h"
 
@@ -221,7 +222,7 @@ inline AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packe
   }
   const int64_t tile_grid = n_layers * r.n_tiles * c->n_kv_heads, fold_grid = (bm / 32) * (c->head_dim / 32);
   r.fits = fits_grid((int64_t)n_layers * r.few_seg * (r.few_rows > 0 ? s->batch : 0) * c->n_kv_heads, 256) &&
-           fits_grid(tile_grid * r.tile_seg, 256) &&
+           fits_grid(tile_grid * r.tile_seg * (c->dtype == KVG_INT8 ? c->head_dim / kvg::int8_split_values((int)c->head_dim) : 1), 256) &&
            fits_grid(n_layers * r.few_rows * c->n_q_heads + (r.tile_seg > 1 ? tile_grid * fold_grid : 0), 256);
   if (!r.fits) return r;
   auto bytes = [&](int64_t row_heads, int32_t n_seg, size_t values) {
