@@ -132,8 +132,8 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
     issue(KR{}, kpool, s_k + slot * kKBytes, u + kDepth);
     const int kb = key0 + 32 * wave;
     auto lv_at = [&](int key) -> float { return lane_value(page.lv, (key / kPage) & 31); };
-    const float kq0 = key_factor(q_scale, lane_value(page.k, (kb / kPage) & 31));
-    const float kq1 = key_factor(q_scale, lane_value(page.k, (kb / kPage + 1) & 31));
+    float kq0 = key_factor(q_scale, lane_value(page.k, (kb / kPage) & 31));
+    float kq1 = key_factor(q_scale, lane_value(page.k, (kb / kPage + 1) & 31));
     f32x16 s;
     float mx[2] = {-INFINITY, -INFINITY};
     const bool masked = kb + 31 > first_n || kb < mask_lo;
@@ -167,6 +167,10 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
       if (w == wave) {
         p0 = page_weights(st, lv0);
         p1 = page_weights(st, lv1);
+        if (__builtin_amdgcn_ballot_w64(is_far(st)) != 0) {
+          far_page(s, 0, kq0, p0, st, lv0);
+          far_page(s, 8, kq1, p1, st, lv1);
+        }
       }
     }
     float sum[2] = {0.0f, 0.0f};

@@ -145,8 +145,9 @@ struct Int8State {
 __device__ __forceinline__ Int8State empty_state(float l0) { return {-INFINITY, -INFINITY, l0, 0.0f, 0.0f}; }
 
 // The steps of a block of 32 keys (two pages).  A lane's scores of a page are S kq: S an integer (as a float; -Inf for a key that
-// the row does not see), kq the query's step times the keys' scale, in log2 units (not 0, by which -Inf would be NaN).
-__device__ __forceinline__ float key_factor(float q_scale, float k) { return fmaxf(q_scale * k, 0x1p-126f); }
+// the row does not see), kq the query's step times the keys' scale, in log2 units (not 0, by which -Inf would be NaN, and not above
+// 2^96, by which |S| < 2^30 would leave fp32).
+__device__ __forceinline__ float key_factor(float q_scale, float k) { return __builtin_amdgcn_fmed3f(q_scale * k, 0x1p-126f, 0x1p96f); }
 // What a lane's largest scores of the pages (both halves of the wave joined) do to the state: factors of the sum of p and of the
 // sums of values, powers of two (or 0).
 struct Int8Raise {
@@ -170,6 +171,22 @@ struct Int8Page {
 __device__ __forceinline__ Int8Page page_weights(const Int8State& s, float lv) {
   const float f = fmaxf(lv + s.x, -kLightest);
   return {f - s.m_ref, __builtin_amdgcn_exp2f(-f)};
+}
+// Rows whose reference is so far out that a score's rounding is past a few units: the exact product S kq of fma could lie well above or
+// below the rounded one that the reference was raised to, and every weight be Inf or 0.  Their scores are rounded, and taken less the
+// reference, which is exact near it; `first`: of a page's eight in s.  (the other rows keep theirs)
+constexpr float kFar = 0x1p20f;
+__device__ __forceinline__ bool is_far(const Int8State& st) { return fabsf(st.m_ref) >= kFar; }
+__device__ __forceinline__ void far_page(f32x16& s, int first, float& kq, Int8Page& p, const Int8State& st, float lv) {
+#pragma clang fp contract(off)
+  const bool far = is_far(st);
+#pragma unroll
+  for (int r = first; r < first + 8; ++r) {
+    const float rounded = s[r] * kq;
+    s[r] = far ? rounded - st.m_ref : s[r];
+  }
+  kq = far ? 1.0f : kq;
+  p.c = far ? fmaxf(lv + st.x, -kLightest) : p.c;
 }
 __device__ __forceinline__ float weight_of(float S, float kq, float c) { return __builtin_amdgcn_exp2f(fmaf(S, kq, c)); }
 __device__ __forceinline__ uint32_t round_pair(float a, float b) {

@@ -183,6 +183,7 @@ __global__ __launch_bounds__(64 * kWaves, DV == 256 ? 1 : D == 64 ? (kSplitKeys 
   issue_v(kt_begin + 1);
 
   bool fresh = true;                      // no block of the segment yet
+  bool any_far = false;                   // a row of the wave is_far
   auto tile = [&](auto stage, int kt) __attribute__((always_inline)) {
     constexpr int ST = decltype(stage)::value;
     using Next = std::integral_constant<int, 1 - ST>;
@@ -230,6 +231,7 @@ __global__ __launch_bounds__(64 * kWaves, DV == 256 ? 1 : D == 64 ? (kSplitKeys 
       const float t0 = fmaxf(m0.x, m0.y) * kq0, t1 = fmaxf(m1.x, m1.y) * kq1;
       if (__builtin_amdgcn_ballot_w64(is_raised(st, t0, t1, lv0, lv1)) != 0) {       // seldom: the references are coarse
         const Int8Raise up = raise_block(st, t0, t1, lv0, lv1);
+        any_far = __builtin_amdgcn_ballot_w64(is_far(st)) != 0;
         st.l *= up.alpha_l;
         if (!fresh) {
 #pragma unroll
@@ -240,7 +242,7 @@ __global__ __launch_bounds__(64 * kWaves, DV == 256 ? 1 : D == 64 ? (kSplitKeys 
     };
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      const float kq0 = key_factor(q_scale, lane_value(sc.k, page0 + 2 * kb)), kq1 = key_factor(q_scale, lane_value(sc.k, page0 + 2 * kb + 1));
+      float kq0 = key_factor(q_scale, lane_value(sc.k, page0 + 2 * kb)), kq1 = key_factor(q_scale, lane_value(sc.k, page0 + 2 * kb + 1));
       const float lv0 = lane_value(sc.lv, page0 + 2 * kb), lv1 = lane_value(sc.lv, page0 + 2 * kb + 1);
       uint4 kf[NS];
 #pragma unroll
@@ -261,7 +263,11 @@ __global__ __launch_bounds__(64 * kWaves, DV == 256 ? 1 : D == 64 ? (kSplitKeys 
         mx1 = fmaxf(mx1, s[8 + r]);
       }
       references(mx0, mx1, kq0, kq1, lv0, lv1);
-      const Int8Page p0 = page_weights(st, lv0), p1 = page_weights(st, lv1);
+      Int8Page p0 = page_weights(st, lv0), p1 = page_weights(st, lv1);
+      if (any_far) {
+        far_page(s, 0, kq0, p0, st, lv0);
+        far_page(s, 8, kq1, p1, st, lv1);
+      }
       float sum0 = 0.0f, sum1 = 0.0f;
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
@@ -300,6 +306,7 @@ __global__ __launch_bounds__(64 * kWaves, DV == 256 ? 1 : D == 64 ? (kSplitKeys 
 #pragma unroll
       for (int d = 0; d < ND; ++d) o[d] = splat(0.0f);
       fresh = true;
+      any_far = false;
     }
   };
   auto step = [&](auto stage, int kt) __attribute__((always_inline)) {

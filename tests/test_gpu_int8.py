@@ -108,6 +108,26 @@ def test_extreme_queries(kvg):  # noqa: F811
     assert torch.equal(bits(out), bits(want))
 
 
+@pytest.mark.parametrize("heads,lens,ctxs", [((4, 2, 64), [50], [0]), ((8, 4, 256), [3], [30]), ((4, 4, 128), [200], [600])])
+def test_scores_past_fp32(kvg, heads, lens, ctxs):  # noqa: F811
+    """Scores that leave fp32: the key with the largest takes the row, or the keys where they are equal."""
+    b = Int8Batch(lens, ctxs, heads, seed=12)
+    b.cache.k_scale[0, int(b.table[0, 0])] = 1e35
+    b.cache.k_scale[0, int(b.table[0, 1])] = 0.0
+    q = b.rows(heads[0], 1e25)
+    out = host(b.attend(q, 0.1)[0])
+    kn, ks, vn, vs = b.cached(0, 0)
+    group = heads[0] // heads[1]
+    for t in range(lens[0]):
+        n = ctxs[0] + t + 1
+        for h in range(heads[0]):
+            g = h // group
+            s = kn[:n, g] @ host(q[0, t, h]) * ks[:n, g]
+            top = s >= s.max() - 1e-9 * abs(s.max())
+            want = (vn[:n, g] * vs[:n, g, None])[top].mean(axis=0)
+            assert np.all(np.abs(out[t, h] - want) <= 2.0 ** -7 * np.abs(vn[:n, g] * vs[:n, g, None])[top].max(axis=0) + 1e-30), (t, h)
+
+
 @pytest.mark.parametrize("heads,lens,ctxs", [((4, 2, 64), [50, 1], [0, 300]), ((8, 4, 256), [200], [0]), ((4, 4, 128), [5, 7], [700, 0])])
 @pytest.mark.parametrize("which", ["k_scale", "v_scale"])
 def test_scales_that_are_not_finite(kvg, heads, lens, ctxs, which):  # noqa: F811
