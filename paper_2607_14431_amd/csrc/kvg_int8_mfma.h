@@ -131,18 +131,23 @@ __device__ __forceinline__ float lane_value(float x, int lane) {
 
 constexpr float kNaN = __builtin_nanf("");
 
-// Softmax state of a segment: references (log2 units, multiples of kStep) of the weights p = 2^(s - m) and of p sv, the sum of p (l0 at
-// first: 0, or NaN for a query that is not finite), and what follows from the references: m, or 0 before the first key, and the
-// exponent x that takes p sv to the range of fp16.
+// Softmax state of a segment: the reference m of the weights p = 2^(s - m) (log2 units, a multiple of kStep), the sum of p (l0 at first: 0,
+// or NaN for a query that is not finite), m_ref: m, or 0 before the first key, the exponent x that takes p sv to the range of fp16, and
+// mt, what s + log2 sv has to pass for another x (-Inf: no value yet).  The reference of p sv is the integer r = kWeightTop - x.
 //
-// Weights are p sv 2^x = 2^(S kq + c), the largest of a row below 2^kWeightTop, rounded to fp16: off by half a step (2^-11 of it) at
-// most, less than the result's own rounding to bf16.  p is the weight times `back`.  Values that weigh less than 2^-kLightest of
-// the row's largest may as well weigh that: it stays far below an fp16 step, and the sum of p keeps its bits.
-constexpr float kWeightTop = 15.0f, kLightest = 60.0f;
+// Weights are p sv 2^x = 2^(S kq + c), all below 2^kWeightTop and rounded to fp16: off by half a step (2^-11 of it) at
+// most, less than the result's own rounding to bf16.  r goes kRoom above what raises it, so that later blocks seldom raise it again (all
+// of a wave's sums are multiplied where one of its rows does; with 4 in place of 8, 7% more vector instructions): the largest weight is above 2^6, and
+// those below 2^-20 of it lose bits.  p is the weight times `back`.  Values that weigh less than 2^-kLightest of the row's largest
+// may as well weigh that: it stays far below an fp16 step, and the sum of p keeps its bits.
+constexpr float kWeightTop = 15.0f, kRoom = 8.0f, kLightest = 60.0f;
+// Rows whose m is past this are far out: see far_page.
+constexpr float kFar = 0x1p20f;
 struct Int8State {
   float m, mt, l, m_ref, x;
 };
 __device__ __forceinline__ Int8State empty_state(float l0) { return {-INFINITY, -INFINITY, l0, 0.0f, 0.0f}; }
+__device__ __forceinline__ bool is_far(const Int8State& st) { return fabsf(st.m_ref) >= kFar; }
 
 // The steps of a block of 32 keys (two pages).  A lane's scores of a page are S kq: S an integer (as a float; -Inf for a key that
 // the row does not see), kq the query's step times the keys' scale, in log2 units (not 0, by which -Inf would be NaN, and not above
@@ -159,10 +164,17 @@ __device__ __forceinline__ bool is_raised(const Int8State& s, float mx0, float m
 __device__ __forceinline__ Int8Raise raise_block(Int8State& s, float mx0, float mx1, float lv0, float lv1) {
   Int8Raise b;
   bool up;
+  const float m = s.m;
   b.alpha_l = raise_reference(s.m, fmaxf(mx0, mx1), up);
-  b.alpha_o = raise_reference(s.mt, fmaxf(mx0 + lv0, mx1 + lv1), up);
   s.m_ref = s.m == -INFINITY ? 0.0f : s.m;
-  s.x = s.mt == -INFINITY ? 0.0f : s.m_ref - s.mt + kWeightTop;
+  const float was = s.mt == -INFINITY ? -INFINITY : kWeightTop - s.x + (m - s.m);      // r beside the new m
+  const float y = fmaxf((mx0 - s.m_ref) + lv0, (mx1 - s.m_ref) + lv1), to = __builtin_ceilf(y) + kRoom;
+  up = y > was;
+  b.alpha_o = up ? __builtin_amdgcn_exp2f(was - to) : 1.0f;
+  const float r = up ? to : was;
+  s.x = r == -INFINITY ? 0.0f : kWeightTop - r;
+  // far out, the sum s + log2 sv has no bits to compare: every block comes here
+  s.mt = r == -INFINITY ? r : is_far(s) ? -0x1p127f : r + s.m_ref;
   return b;
 }
 struct Int8Page {
@@ -175,8 +187,6 @@ __device__ __forceinline__ Int8Page page_weights(const Int8State& s, float lv) {
 // Rows whose reference is so far out that a score's rounding is past a few units: the exact product S kq of fma could lie well above or
 // below the rounded one that the reference was raised to, and every weight be Inf or 0.  Their scores are rounded, and taken less the
 // reference, which is exact near it; `first`: of a page's eight in s.  (the other rows keep theirs)
-constexpr float kFar = 0x1p20f;
-__device__ __forceinline__ bool is_far(const Int8State& st) { return fabsf(st.m_ref) >= kFar; }
 __device__ __forceinline__ void far_page(f32x16& s, int first, float& kq, Int8Page& p, const Int8State& st, float lv) {
 #pragma clang fp contract(off)
   const bool far = is_far(st);
@@ -202,8 +212,8 @@ __device__ __forceinline__ float block_sum(float sum0, float sum1, float back0, 
   const float2 both = halves32(fmaf(sum0, back0, sum1 * back1));
   return both.x + both.y;
 }
-// End of a segment: the exponent that takes its sums of values to the reference of p (far below fp32 where every scale was 0).
-__device__ __forceinline__ int end_exponent(const Int8State& s) { return s.mt == -INFINITY ? -1000 : (int)(s.mt - s.m - kWeightTop); }
+// End of a segment: the exponent that takes its sums of values to p sv (far below fp32 where every scale was 0).
+__device__ __forceinline__ int end_exponent(const Int8State& s) { return s.mt == -INFINITY ? -1000 : (int)fmaxf(-s.x, -1000.0f); }
 
 }  // namespace
 

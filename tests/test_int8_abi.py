@@ -180,3 +180,15 @@ def test_oracle_page():
     q = np.ones((1, 2, 4))
     want, tol = oracle.attend(q, np.array([0]), np.ones((1, 1, 4)), np.ones((1, 1)), np.full((1, 1, 4), 8.0), np.full((1, 1), 0.25), 0.5)
     assert np.allclose(want, 2.0) and np.all(tol < 2 * (2.0 ** -8 + 2.0 ** -10))
+
+
+def test_oracle_attention():
+    """The oracle's attention over integers and scales is the bf16 caches' over the values they stand for."""
+    from oracle.packed import attend_bounds
+    rng = np.random.default_rng(4)
+    kn, vn = (rng.integers(-127, 128, (50, 2, 8)).astype(np.float64) for _ in range(2))
+    ks, vs = (np.repeat(rng.random((4, 2)), 16, axis=0)[:50] for _ in range(2))
+    q, index = rng.normal(size=(3, 4, 8)), np.array([0, 17, 49])
+    for window in (0, 20):
+        want = attend_bounds(q, index, kn * ks[..., None], vn * vs[..., None], 0.01, window)[0]
+        assert np.allclose(oracle.attend(q, index, kn, ks, vn, vs, 0.01, window)[0], want, rtol=0, atol=1e-12 * np.abs(want).max())
