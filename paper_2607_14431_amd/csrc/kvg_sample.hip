@@ -320,26 +320,46 @@ struct Ends {
   u64 before_first, before_k; // weight of the bins before
 };
 struct EndsShared {
-  u64 weight[16], count[16];  // of the waves' bins
+  u64 weight[16];             // of the waves' bins
+  uint32_t count[16];
   u64 upto_k;                 // weight up to top-k's bin, with it
   Ends ends;
 };
-// (all lanes of a workgroup of kSampleBins lanes or fewer; bins in order, kSampleBins / threads a lane)
+// A lane's bins, in order; requested before what the row's parameters wait for.
 template <int kT>
-__device__ void find_ends(const SampleArgs& a, int row, Ends& out, EndsShared& s) {
+struct LaneBins {
+  static constexpr int kPer = kSampleBins / kT;
+  u64 w[kPer];
+  uint32_t c[kPer];
+  __device__ __forceinline__ void load(const SampleArgs& a, int row) {
+    const int64_t at = (int64_t)row * kSampleBins + threadIdx.x * kPer;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      w[i] = a.bin_weights[at + i];
+      c[i] = a.bin_counts[at + i];
+    }
+  }
+};
+// (all lanes of a workgroup of kSampleBins lanes or fewer)
+template <int kT>
+__device__ void find_ends(const SampleArgs& a, int row, const LaneBins<kT>& bins, Ends& out, EndsShared& s) {
   constexpr int kPer = kSampleBins / kT;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b0 = threadIdx.x * kPer;
-  u64 w[kPer], c[kPer], sw = 0, sc = 0;
+  const u64(&w)[kPer] = bins.w;
+  const uint32_t(&c)[kPer] = bins.c;
+  u64 sw = 0;
+  uint32_t sc = 0;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    w[i] = a.bin_weights[(int64_t)row * kSampleBins + b0 + i];
-    c[i] = a.bin_counts[(int64_t)row * kSampleBins + b0 + i];
     sw += w[i];
     sc += c[i];
   }
-  u64 uw = sw, uc = sc;                                      // up to and with this lane's
+  u64 uw = sw;                                               // up to and with this lane's
+  uint32_t uc = sc;
+#pragma unroll
   for (int m = 1; m < 64; m <<= 1) {
-    const u64 x = __shfl_up(uw, m), y = __shfl_up(uc, m);
+    const u64 x = __shfl_up(uw, m);
+    const uint32_t y = __shfl_up(uc, m);
     uw += lane >= m ? x : 0;
     uc += lane >= m ? y : 0;
   }
@@ -349,7 +369,8 @@ __device__ void find_ends(const SampleArgs& a, int row, Ends& out, EndsShared& s
   }
   if (threadIdx.x == 0) s.ends = {0, -1, kSampleBins, 0, 0, 0, 0};
   __syncthreads();
-  u64 total_w = 0, total_c = 0;
+  u64 total_w = 0;
+  uint32_t total_c = 0;
   for (int i = 0; i < kT / 64; ++i) {
     if (i < wave) {
       uw += s.weight[i];
@@ -362,14 +383,15 @@ __device__ void find_ends(const SampleArgs& a, int row, Ends& out, EndsShared& s
   uc -= sc;
   const int k = a.top_k != nullptr ? a.top_k[row] : 0;
   const float p = a.top_p != nullptr ? a.top_p[row] : 1.0f;
-  const bool by_k = k > 0 && (u64)k < total_c;
+  const bool by_k = k > 0 && (uint32_t)k < total_c;
   if (by_k) {
-    u64 x = uw, y = uc;
+    u64 x = uw;
+    uint32_t y = uc;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      if (y < (u64)k && y + c[i] >= (u64)k) {
+      if (y < (uint32_t)k && y + c[i] >= (uint32_t)k) {
         s.ends.k_bin = b0 + i;
-        s.ends.k_need = (uint32_t)((u64)k - y);
+        s.ends.k_need = (uint32_t)k - y;
         s.ends.before_k = x;
         s.upto_k = x + w[i];
       }
@@ -404,11 +426,12 @@ __device__ void find_ends(const SampleArgs& a, int row, Ends& out, EndsShared& s
   }
   __syncthreads();
   if (s.ends.k_bin < kSampleBins) {                          // listed codes in front of top-k's bin
-    u64 n = 0;
+    uint32_t n = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) n += b0 + i >= s.ends.first && b0 + i <= s.ends.last && b0 + i < s.ends.k_bin ? c[i] : 0;
-    n = add_lanes(n);
-    if (lane == 0 && n != 0) atomicAdd(&s.ends.listed_before_k, (uint32_t)n);
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) n += __shfl_xor(n, m);
+    if (lane == 0 && n != 0) atomicAdd(&s.ends.listed_before_k, n);
   }
   __syncthreads();
   out = s.ends;
@@ -423,11 +446,13 @@ __global__ __launch_bounds__(kPartThreads) void sample_parts_kernel(const Sample
   __shared__ uint32_t n_here, at_row;
   const int row = blockIdx.y, part = blockIdx.x;
   if (threadIdx.x == 0) n_here = 0;
+  LaneBins<kPartThreads> bins;
+  bins.load(a, row);
   Row r;
   if (!row_setup(a, row, row_top(a, row), false, r)) return;
   if (threadIdx.x < 64) tab[threadIdx.x] = exp2(threadIdx.x / 64.0);
   Ends ends = {kSampleBins, -1, kSampleBins, 0, 0, 0, 0};
-  if (limited(a, row)) find_ends<kPartThreads>(a, row, ends, ends_shared);
+  if (limited(a, row)) find_ends<kPartThreads>(a, row, bins, ends, ends_shared);
   __syncthreads();
   const bool all = ends.first == kSampleBins;
   // logits below `low` are in later bins, or below min-p where that is the only limit; the rounding of these lines is below its slack
@@ -618,6 +643,7 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
   if (tid < 64) s.tab[tid] = exp2(tid / 64.0);
   u64 top = 0, early[2] = {0, 0};                            // early: the first listed codes
   uint32_t n_listed = 0;
+  LaneBins<kThreads> bins;
   if constexpr (kListed) {
     for (int i = tid; i < a.V; i += kThreads) {
       const u64 c = token_code(l[i], i);
@@ -629,6 +655,7 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
     for (int w = 0; w < kWaves; ++w) top = s.wave[w] > top ? s.wave[w] : top;
     __syncthreads();
   } else {
+    bins.load(a, row);
     n_listed = __builtin_amdgcn_readfirstlane((int)a.n_listed[row]);
     early[0] = a.listed[(int64_t)row * kSampleListed + lane];
     early[1] = a.listed[(int64_t)row * kSampleListed + 64 + lane];
@@ -660,7 +687,7 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
     }
   } else {
     Ends ends = {kSampleBins, -1, kSampleBins, 0, 0, 0, 0};
-    if (limit) find_ends<kThreads>(a, row, ends, ends_shared);
+    if (limit) find_ends<kThreads>(a, row, bins, ends, ends_shared);
     searched = !limit || n_listed <= kSampleListed;
     if (!searched) {
       if (k > 0 && k < a.V) r.cut = find_cut(a, r, l, false, (u64)k, s);
