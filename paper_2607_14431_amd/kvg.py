@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
+import struct
 
 import torch
 
@@ -465,6 +466,9 @@ def kvg_artifact_header_init_rotary(cache: Cache, n_tokens: int, own_pos: int, r
     return hdr
 
 
+_AXES = struct.Struct("@P8i")       # kvg_axes
+
+
 @dataclasses.dataclass
 class Axes:
     """Positions with several axes: int64 [n_axes][n_tokens] (device); pairs of a head's rotated components for each axis,
@@ -480,7 +484,9 @@ class Axes:
             raise ValueError(f"pairs: of 1 to {KVG_MAX_AXES} axes")
         if not (pos.dtype is torch.int64 and pos.is_contiguous() and pos.shape == (n, n_tokens)):
             raise ValueError("positions: int64 [n_axes][n_tokens], contiguous")
-        return kvg_axes(pos.data_ptr(), n, self.order, int(self.own_frequencies), 0, (ctypes.c_int32 * 4)(*self.pairs))
+        # packed in one step: a ctypes array and nine fields took half of a small call's marshalling
+        return kvg_axes.from_buffer_copy(_AXES.pack(pos.data_ptr(), n, self.order, int(self.own_frequencies), 0, *self.pairs,
+                                                    *(0,) * (KVG_MAX_AXES - n)))
 
 
 def _rotate_strides(where: str, x: torch.Tensor, y: torch.Tensor):
