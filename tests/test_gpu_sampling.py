@@ -223,3 +223,37 @@ def test_logits_far_apart(kvg):
         limits = {k: np.array(v) for k, v in limits.items()}
         tokens, logprobs = run(kvg, logits, temperature, u, **limits)
         compare(logits, temperature, u, tokens, logprobs, **limits)
+
+
+def test_a_long_vocabulary(kvg):
+    """Parts of more tokens than a workgroup takes at the end.  With 41 bits after the point, 2 off is 1.1e-6 of the likeliest token's
+    weight, and the broad base (logits N(0, 2), 16 and more below the likeliest) weighs e^-16 = 1e-7 a token at temperature 1: a row
+    whose number or limit falls into its base cannot be compared.  Its base is 2e6 E[e^x] e^-18 = 2e6 e^2 e^-18 = 0.2 beside a
+    few units of likely tokens, so a top-p of 0.999 ends there always and a number falls there now and then: two rows of four."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    R, V = 4, 2_000_003
+    logits = logits_like(gen, R, V, 2.0)
+    rng = np.random.default_rng(2)
+    for limits in (dict(), dict(top_k=np.array([50, 1000, 5000, V])), dict(top_p=np.array([0.9, 0.3, 0.999, 0.01])),
+                   dict(top_k=np.array([64, 900, 4000, 0]), top_p=np.array([0.9, 0.95, 0.5, 0.99]), min_p=np.array([0.0, 0.01, 0.0, 0.001]))):
+        u = rng.random(R)
+        tokens, logprobs = run(kvg, logits, [1.0, 0.8, 1.2, 0.6], u, **limits)
+        compare(logits, [1.0, 0.8, 1.2, 0.6], u, tokens, logprobs, **limits, most_close=2)
+
+
+def test_more_equal_logits_than_are_listed(kvg):
+    """The end of a limit among 5,000 and more tokens of one logit, by index, and among their neighbours."""
+    V = 70000
+    rng = np.random.default_rng(3)
+    x = np.full((6, V), -20.0, dtype=np.float32)
+    for r in range(6):
+        x[r, rng.permutation(V)[:5000 + 9000 * r]] = 1.5
+        x[r, rng.integers(0, V, 20)] = 3.0
+        x[r, rng.integers(0, V, 20)] = np.float32(1.5) + np.float32(2.0 ** -20)
+    u = rng.random(6)
+    logits = torch.from_numpy(x).cuda()
+    for limits in (dict(top_k=[100, 3000, 5020, 6000, 20000, 40]), dict(top_p=[0.5, 0.1, 0.9, 0.99, 0.3, 0.7]),
+                   dict(top_k=[900, 1000, 4000, 9000, 30000, 1024], top_p=[0.5, 0.9, 0.5, 0.1, 0.9, 0.3])):
+        limits = {k: np.array(v) for k, v in limits.items()}
+        tokens, logprobs = run(kvg, logits, [1.0] * 6, u, **limits)
+        compare(logits, [1.0] * 6, u, tokens, logprobs, **limits, always=range(6))
