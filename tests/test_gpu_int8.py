@@ -48,12 +48,17 @@ def test_long_prompts(kvg, heads):  # noqa: F811
         check(b, q, b.attend(q, 1.0 / math.sqrt(heads[2])), 1.0 / math.sqrt(heads[2]), rows)
 
 
-@pytest.mark.parametrize("heads", [(4, 2, 64), (16, 8, 256)])
-def test_a_rows_bytes_are_its_own(kvg, heads):  # noqa: F811
-    """The same cache read in one call, in chunks, token by token and alone: the same bytes.  Scales differ a thousandfold."""
+@pytest.mark.parametrize("heads,far", [((4, 2, 64), False), ((16, 8, 256), False), ((4, 2, 128), False), ((4, 2, 128), True), ((8, 4, 256), True)])
+def test_a_rows_bytes_are_its_own(kvg, heads, far):  # noqa: F811
+    """The same cache read in one call, in chunks, token by token and alone: the same bytes.  Scales differ a thousandfold; `far`: every
+    other row's scores are past 2^20, and value scales far from 1."""
     n = 700
     b = Int8Batch([n, 30], [0, 1100], heads, seed=4, spread=3.0)
     q, scale = b.rows(heads[0], 2.0), 0.1
+    if far:
+        q[:, ::2] *= 2.0 ** 22
+        b.cache.v_scale.mul_(2.0 ** 20)
+        assert bool(b.attend(q, scale)[:, :n].isfinite().all())
     whole = b.attend(q, scale)
     for cuts in ([1, 64, 65, 300, 270], [n - 1, 1], [35] * 20):
         at = 0
