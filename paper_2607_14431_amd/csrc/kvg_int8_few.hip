@@ -147,8 +147,8 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
       mx[r / 8] = fmaxf(mx[r / 8], s[r]);
     }
     {
-      const float2 m0 = halves32(mx[0]), m1 = halves32(mx[1]);
-      s_mx[wave][lrow] = make_float2(fmaxf(m0.x, m0.y) * kq0, fmaxf(m1.x, m1.y) * kq1);      // both halves of the wave, the same values
+      const float2 m = max_halves(mx[0], mx[1]);
+      s_mx[wave][lrow] = make_float2(m.x * kq0, m.y * kq1);      // both halves of the wave, the same values
     }
     __syncthreads();
     // ---- the references of the unit's blocks in order (every wave alike), this wave's weights

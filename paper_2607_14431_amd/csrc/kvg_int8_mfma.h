@@ -149,6 +149,14 @@ struct Int8State {
 __device__ __forceinline__ Int8State empty_state(float l0) { return {-INFINITY, -INFINITY, l0, 0.0f, 0.0f}; }
 __device__ __forceinline__ bool is_far(const Int8State& st) { return fabsf(st.m_ref) >= kFar; }
 
+// The larger of both halves of the wave, of x and of y.
+__device__ __forceinline__ float2 max_halves(float x, float y) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);      // lower halves, upper ones
+  const float m = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));                                       // of x below, of y above
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+  return make_float2(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // The steps of a block of 32 keys (two pages).  A lane's scores of a page are S kq: S an integer (as a float; -Inf for a key that
 // the row does not see), kq the query's step times the keys' scale, in log2 units (not 0, by which -Inf would be NaN, and not above
 // 2^96, by which |S| < 2^30 would leave fp32).

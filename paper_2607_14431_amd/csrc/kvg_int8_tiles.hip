@@ -227,8 +227,8 @@ __global__ __launch_bounds__(64 * kWaves, DV == 256 ? 1 : D == 64 ? (kSplitKeys 
     // the references of block kb from a lane's largest scores of its pages, O and the sum of p with them (O of a segment's first block
     // is still 0)
     auto references = [&](float mx0, float mx1, float kq0, float kq1, float lv0, float lv1) __attribute__((always_inline)) {
-      const float2 m0 = halves32(mx0), m1 = halves32(mx1);
-      const float t0 = fmaxf(m0.x, m0.y) * kq0, t1 = fmaxf(m1.x, m1.y) * kq1;
+      const float2 mx = max_halves(mx0, mx1);
+      const float t0 = mx.x * kq0, t1 = mx.y * kq1;
       if (__builtin_amdgcn_ballot_w64(is_raised(st, t0, t1, lv0, lv1)) != 0) {       // seldom: the references are coarse
         const Int8Raise up = raise_block(st, t0, t1, lv0, lv1);
         any_far = __builtin_amdgcn_ballot_w64(is_far(st)) != 0;
