@@ -176,7 +176,12 @@ inline bool split_tiles(bool f32, int64_t head_dim, int64_t workgroups, int64_t 
 // 64 20 / 17, 256 24 / 17, 512 27 / 23.  fp8, 256: 64 21 / 24, 128 23 / 25, 256 26 / 27, 512 35 / 49; 128: 64 17 / 18, 256 29 / 23;
 // 64: 16 19 / 16, 32 18 / 15.  One limit for all: at 512 it takes the slower side at head_dim 64.  int8, whose few kernel has all of
 // a segment on its way at once, 128: 16 15 / 16, 80 21 / 26, 160 20 / 26, 320 27 / 28; 64: 48 20 / 19, 144 22 / 19, 576 26 / 23.
-inline bool few_in_tiles(const kvg_cache* c, int64_t workgroups) {
+// `mixed`: there are longer sequences too (the figures above are of single tokens alone).  Their tiles' launch has room for the short
+// ones, until these have more to read than it.  int8, mixed calls, 256: 224 81 / 65, 448 94 / 72, 544 144 / 129, 1,008 114 / 123, 1,024
+// 66-78 / 66-85, 2,016 124 / 151; 128: 96 96 / 79, 288 129 / 110, 768 49-89 / 33-68, 1,512 134 / 124, 2,048 74 / 78; 64: 288 51 / 34, 1,008 56 / 43, 2,016
+// 77 / 67.
+inline bool few_in_tiles(const kvg_cache* c, int64_t workgroups, bool mixed) {
+  if (c->dtype == KVG_INT8 && mixed) return workgroups * c->head_dim <= 196608;
   return workgroups <= 256 && (c->dtype == KVG_BF16 || c->head_dim <= (c->dtype == KVG_INT8 ? 64 : 128));
 }
 
@@ -212,7 +217,7 @@ inline AttnPlan attn_plan(const kvg_cache* c, const kvg_seqs* s, const kvg_packe
   if (split_tiles(f32, c->head_dim, r.n_tiles * c->n_kv_heads * sum / longest, longest)) r.tile_seg = segs;
   // The lengths are the device's.  A single sequence that may be long goes in tiles whatever its length.
   if (!f32 && (len * group <= kvg::kFewPairs || s->batch > 1) &&
-      !(r.tile_seg > 1 && few_in_tiles(c, (int64_t)n_layers * segs * s->batch * c->n_kv_heads))) {
+      !(r.tile_seg > 1 && few_in_tiles(c, (int64_t)n_layers * segs * s->batch * c->n_kv_heads, len * group > kvg::kFewPairs))) {
     r.few_rows = std::min<int64_t>(p->n_tokens, s->batch * std::min<int64_t>(len, kvg::kFewPairs / group));
     r.few_seg = segs;
     if (len * group <= kvg::kFewPairs) {
