@@ -561,37 +561,25 @@ __device__ u64 sum_block(u64 x, Shared& s) {
 // Listed codes of a lane (0: none).
 constexpr int kHeld = kSampleListed / kThreads;
 // The code at which the count (or, by_weight, the weight) of the codes, from the largest on, reaches `need`; the least one if it does not.
-// The codes are put into bins by their logit, or where all are equal by index, linearly between the largest and the least, and all but
-// those of the bin where that happens are dropped, until kFew are left.  (all lanes; finite logits; the next call may follow at once)
-__device__ u64 select(const Row& r, const u64 (&codes)[kHeld], bool by_weight, u64 need, Shared& s) {
+// The codes are put into bins by their logit, linearly between `high` and `low`, and all but those of the bin where that happens are
+// dropped; so on between the largest and the least of the rest, by index where their logits are equal, until kFew are left.  (all
+// lanes; finite logits, of which none need lie at or between the ends; the next call may follow at once)
+__device__ u64 select(const Row& r, const u64 (&codes)[kHeld], bool by_weight, u64 need, double high, double low, Shared& s) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   auto& t = s.select;
   u64 c[kHeld];
 #pragma unroll
   for (int j = 0; j < kHeld; ++j) c[j] = codes[j];
+  bool equal = false;
+  double first = high, range = high - low;
   while (true) {
-    u64 hi = 0, low = 0;                                     // low: of the inverted codes, as the least is sought
-#pragma unroll
-    for (int j = 0; j < kHeld; ++j) {
-      hi = c[j] > hi ? c[j] : hi;
-      low = c[j] != 0 && ~c[j] > low ? ~c[j] : low;
-    }
-    hi = max_lanes(hi);
-    low = max_lanes(low);
     __syncthreads();
-    if (lane == 0) {
-      t.hi[wave] = hi;
-      t.lo[wave] = low;
-    }
     t.bins[tid] = 0;
     if (tid == 0) t.n = 0;
     __syncthreads();
-    hi = max_lanes(lane < kWaves ? t.hi[lane] : 0);
-    const u64 lo = ~max_lanes(lane < kWaves ? t.lo[lane] : 0);
-    const bool equal = hi >> kSampleIndexBits == lo >> kSampleIndexBits;
     auto value = [&](u64 x) -> double { return equal ? (double)(x & kIndexMask) : (double)logit_of((uint32_t)(x >> kSampleIndexBits)); };
-    const double first = value(hi), range = first - value(lo), scale = range > 0.0 ? (kThreads - 1) / range : 0.0;
-    auto bin = [&](u64 x) -> int { return min((int)((first - value(x)) * scale), kThreads - 1); };
+    const double scale = range > 0.0 ? (kThreads - 1) / range : 0.0;
+    auto bin = [&](u64 x) -> int { return (int)fmin(fmax((first - value(x)) * scale, 0.0), (double)(kThreads - 1)); };
 #pragma unroll
     for (int j = 0; j < kHeld; ++j)
       if (c[j] != 0) atomicAdd(&t.bins[bin(c[j])], by_weight ? code_weight(r, c[j], s.tab) : 1);
@@ -620,6 +608,24 @@ __device__ u64 select(const Row& r, const u64 (&codes)[kHeld], bool by_weight, u
       }
     __syncthreads();
     if (t.n <= kFew) break;
+    u64 most = 0, least = 0;                                 // least: of the inverted codes
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      most = c[j] > most ? c[j] : most;
+      least = c[j] != 0 && ~c[j] > least ? ~c[j] : least;
+    }
+    most = max_lanes(most);
+    least = max_lanes(least);
+    if (lane == 0) {
+      t.hi[wave] = most;
+      t.lo[wave] = least;
+    }
+    __syncthreads();
+    most = max_lanes(lane < kWaves ? t.hi[lane] : 0);
+    least = ~max_lanes(lane < kWaves ? t.lo[lane] : 0);
+    equal = most >> kSampleIndexBits == least >> kSampleIndexBits;
+    first = equal ? (double)(most & kIndexMask) : (double)logit_of((uint32_t)(most >> kSampleIndexBits));
+    range = first - (equal ? (double)(least & kIndexMask) : (double)logit_of((uint32_t)(least >> kSampleIndexBits)));
   }
   if (tid < 64) {
     const int n = __builtin_amdgcn_readfirstlane((int)t.n);
@@ -678,11 +684,11 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
         const int i = tid + j * kThreads;
         c[j] = i < a.V && l[i] >= r.least ? token_code(l[i], i) : 0;
       }
-      if (k > 0 && k < a.V) r.cut = select(r, c, false, (u64)k, s);
+      if (k > 0 && k < a.V) r.cut = select(r, c, false, (u64)k, r.top, r.least, s);
       if (p < 1.0f) {
 #pragma unroll
         for (int j = 0; j < kHeld; ++j) sum += c[j] != 0 && c[j] >= r.cut ? code_weight(r, c[j], s.tab) : 0;
-        r.cut = select(r, c, true, share_of(p, sum_block(sum, s)), s);
+        r.cut = select(r, c, true, share_of(p, sum_block(sum, s)), r.top, r.least, s);
       }
     }
   } else {
@@ -729,7 +735,9 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
           const int i = tid + j * kThreads;
           c[j] = i < (int)n_listed ? a.listed[(int64_t)row * kSampleListed + i] : 0;
         }
-        if (by_k) r.cut = select(r, c, false, (u64)n, s);
+        const double bin = 1.0 / (r.inv_t * r.bin_scale), high = r.top - ends.first * bin;
+        const double low = r.top - (max(ends.last, by_k ? ends.k_bin : 0) + 1) * bin;
+        if (by_k) r.cut = select(r, c, false, (u64)n, high, low, s);
         if (p < 1.0f) {
           if (add) {
 #pragma unroll
@@ -738,7 +746,7 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(const SampleArgs 
                 sum += code_weight(r, c[j], s.tab);
             base += sum_block(sum, s);
           }
-          r.cut = select(r, c, true, share_of(p, base) - ends.before_first, s);
+          r.cut = select(r, c, true, share_of(p, base) - ends.before_first, high, low, s);
         }
 #pragma unroll
         for (int j = 0; j < kHeld; ++j)
