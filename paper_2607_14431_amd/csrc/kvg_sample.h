@@ -37,9 +37,9 @@ constexpr int kSampleBins = 1024;
 constexpr int kSampleListed = 4096;
 
 // Parts of a row, multiples of 1,024 tokens: few rows need many to spread over the chip, of more each part's workgroup should have
-// more than its start to do.  Rows of 262,144 tokens with top-k, top-p and min-p, us, 128 parts / 64 / 32 / 8: 1 row 28.6 / 28.5, 16 rows 46 / 41 /
-// 42, 64 rows 97 / 77 / 73, 256 rows 292 / 178 / 177 / 187.  Of 32,000 tokens, parts of 1,024 / 2,048 / 4,096 / 8,192: 1 row 25.9 at all, 16
-// rows 32 / 31 / 31 / 36, 64 rows 46 / 37 / 35 / 39, 256 rows 87 / 62 / 52 / 50.
+// more than its start to do.  Rows of 262,144 tokens with top-k, top-p and min-p, us, 128 parts / 64 / 32 / 8: 1 row 28.3 / 27.7 / 32.4 / 52, 16 rows
+// 44 / 40 / 42 / 70, 64 rows 92 / 74 / 68 / 81, 256 rows 276 / 195 / 172 / 173.  Of 32,000 tokens, parts of 1,024 / 2,048 / 4,096 / 8,192: 1 row 25.0 /
+// 25.5 / 27.1 / 32.2, 16 rows 31 / 30 / 30 / 35, 64 rows 42 / 36 / 34 / 38, 256 rows 82 / 59 / 48 / 49.
 constexpr int kSampleParts = 128;
 inline int sample_part_size(int64_t rows, int64_t V) {
   const int64_t want = rows < 16 ? kSampleParts : rows < 32 ? 64 : 32, least = rows < 16 ? 1024 : 4096;

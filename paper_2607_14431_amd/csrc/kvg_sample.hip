@@ -16,8 +16,8 @@
 //   pick    a workgroup a row: the list gives the cut; the parts' weights the part that holds the token, which is searched
 // Bound: one row, four launches and the chains in them (262,144 tokens: 3 + 8 + 5 + 10 us; a workgroup that makes every pass took
 // 523).  64 rows, each with other limits: 13 us for the first read (5.2 TB/s), 22 for the bins (fp64 exponentials and LDS
-// additions of the rows with a top-p alone), 18 for the parts, 29 for the longest lists.  A bitonic sort of a list of 1,400 codes
-// took 20 us, select() takes 4.
+// additions of the rows with a top-p alone), 18 for the parts, 24 for the longest lists.  A bitonic sort of a list of 1,400 codes
+// took 20 us, select() about 5.
 //
 // Where the list would be too long (thousands of tokens of nearly equal logits) the cut is found digit by digit instead (11, 11, 10
 // bits of the logit, twice 12 of the index): count or weight of the tokens that share the digits so far, by their next digit.
