@@ -18,7 +18,7 @@ namespace {
 // s_waitcnt operand that waits for vmcnt <= n alone (gfx9 encoding: bits 3:0 and 15:14)
 constexpr int vm_wait(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
 constexpr int kLgkmWait = 0xC07F;      // lgkmcnt(0) alone
-constexpr int kStream = 2;             // buffer load policy: nontemporal (every row is read once)
+constexpr int kStream = 2;             // buffer load policy: nontemporal (every row is read once; 16 tokens over 33k keys 306 us, plain 324)
 
 // kWaves: waves of a workgroup, a block of 32 keys and D / kWaves dimensions each.  kDepth: units in LDS or on their way.
 template <int D, int kWaves, int kDepth>
@@ -260,7 +260,7 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
 
 // Up to this many workgroups, one a compute unit, a workgroup has waves for all of head_dim and, where LDS holds them, all keys of a
 // segment on their way at once: the time is one workgroup's, start to end.  More workgroups hide their waits from each other: two
-// waves each and one unit.  Small workgroups against large ones, each with the fold, us, at workgroups: head_dim 256: 80 30 / 25, 160
+// waves each and one unit (with four, those 16 tokens take 354 us).  Small workgroups against large ones, each with the fold, us, at workgroups: head_dim 256: 80 30 / 25, 160
 // 33 / 26, 240 33 / 27, 320 38 / 43, 1,280 53 / 84; 128: 16 17 / 15, 80 26 / 21, 160 25-26 / 20-22, 320 28-30 / 27, 640 30-32 /
 // 42-49, 1,280 35 / 63.  At head_dim 64 it is the same kernel (a deep one of 8 units: 48 20.0 / 20.4, 576 26 / 28).
 constexpr unsigned kFewGrid = 256;
