@@ -260,9 +260,9 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
 
 // Up to this many workgroups, one a compute unit, a workgroup has waves for all of head_dim and, where LDS holds them, all keys of a
 // segment on their way at once: the time is one workgroup's, start to end.  More workgroups hide their waits from each other: two
-// waves each and one unit (with four, those 16 tokens take 354 us).  Small workgroups against large ones, each with the fold, us, at workgroups: head_dim 256: 80 30 / 25, 160
-// 33 / 26, 240 33 / 27, 320 38 / 43, 1,280 53 / 84; 128: 16 17 / 15, 80 26 / 21, 160 25-26 / 20-22, 320 28-30 / 27, 640 30-32 /
-// 42-49, 1,280 35 / 63.  At head_dim 64 it is the same kernel (a deep one of 8 units: 48 20.0 / 20.4, 576 26 / 28).
+// waves each and one unit (16 tokens over 33k keys of head_dim 256: 306 us, with four waves 354).  Small workgroups against
+// large ones, each with the fold, us, at workgroups: head_dim 256: 80 30 / 25, 160 33 / 26, 240 33 / 27, 320 38 / 43, 1,280 53 / 84; 128: 16
+// 17 / 15, 80 26 / 21, 160 25-26 / 20-22, 320 28-30 / 27, 640 30-32 / 42-49, 1,280 35 / 63.  At head_dim 64 it is the same kernel (a deep one of 8 units: 48 20.0 / 20.4, 576 26 / 28).
 constexpr unsigned kFewGrid = 256;
 template <int D>
 hipError_t launch_few_d(const PackedAttnArgs& a, const Int8Scales& s, hipStream_t stream) {
