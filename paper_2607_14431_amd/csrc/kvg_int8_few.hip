@@ -148,7 +148,7 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
     }
     {
       const float2 m = max_halves(mx[0], mx[1]);
-      s_mx[wave][lrow] = make_float2(m.x * kq0, m.y * kq1);      // both halves of the wave, the same values
+      s_mx[wave][lrow] = make_float2(largest_score(m.x, kq0), largest_score(m.y, kq1));      // both halves of the wave, the same values
     }
     __syncthreads();
     // ---- the references of the unit's blocks in order (every wave alike), this wave's weights
@@ -162,8 +162,9 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
     for (int w = 0; w < kWaves; ++w) {
       const float2 x = most[w];
       const float lv0 = lv_at(key0 + 32 * w), lv1 = lv_at(key0 + 32 * w + kPage);
-      raised[w] = __builtin_amdgcn_ballot_w64(is_raised(st, x.x, x.y, lv0, lv1)) != 0;
-      if (raised[w]) raise[w] = raise_block(st, x.x, x.y, lv0, lv1);
+      const bool mine = is_raised(st, x.x, x.y, lv0, lv1);
+      raised[w] = __builtin_amdgcn_ballot_w64(mine) != 0;
+      if (raised[w]) raise[w] = raise_block(st, mine, x.x, x.y, lv0, lv1);
       if (w == wave) {
         p0 = page_weights(st, lv0);
         p1 = page_weights(st, lv1);

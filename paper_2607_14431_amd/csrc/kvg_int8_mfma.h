@@ -161,29 +161,43 @@ __device__ __forceinline__ float2 max_halves(float x, float y) {
 // the row does not see), kq the query's step times the keys' scale, in log2 units (not 0, by which -Inf would be NaN, and not above
 // 2^96, by which |S| < 2^30 would leave fp32).
 __device__ __forceinline__ float key_factor(float q_scale, float k) { return __builtin_amdgcn_fmed3f(q_scale * k, 0x1p-126f, 0x1p96f); }
-// What a lane's largest scores of the pages (both halves of the wave joined) do to the state: factors of the sum of p and of the
-// sums of values, powers of two (or 0).
+// A lane's largest score of a page, rounded to fp32: what the references are raised by, in every kernel.
+__device__ __forceinline__ float largest_score(float S, float kq) {
+#pragma clang fp contract(off)
+  return S * kq;
+}
+// Whether a lane's largest scores of the pages (both halves of the wave joined) raise its references.  The one test of that: a wave
+// takes its rows to raise_block() together, but the rows whose own test fails keep their state, so that a row's bytes are
+// those it has alone.  (No fma here: sums of rounded products are the same in every kernel.)
+__device__ __forceinline__ bool is_raised(const Int8State& s, float mx0, float mx1, float lv0, float lv1) {
+#pragma clang fp contract(off)
+  return fmaxf(mx0, mx1) > s.m || fmaxf(mx0 + lv0, mx1 + lv1) > s.mt;
+}
+// What they do to the state where `raised` (is_raised): factors of the sum of p and of the sums of values, powers of two (or 0), and
+// 1 elsewhere.  mx + lv rounds by up to 2^-4 (below kFar), so weights of a row that is not raised stay below 2^(kWeightTop + 1/16).
 struct Int8Raise {
   float alpha_l, alpha_o;
 };
-__device__ __forceinline__ bool is_raised(const Int8State& s, float mx0, float mx1, float lv0, float lv1) {
-  return fmaxf(mx0, mx1) > s.m || fmaxf(mx0 + lv0, mx1 + lv1) > s.mt;
-}
-__device__ __forceinline__ Int8Raise raise_block(Int8State& s, float mx0, float mx1, float lv0, float lv1) {
+__device__ __forceinline__ Int8Raise raise_block(Int8State& s, bool raised, float mx0, float mx1, float lv0, float lv1) {
+#pragma clang fp contract(off)
+  Int8State to = s;
   Int8Raise b;
   bool up;
-  const float m = s.m;
-  b.alpha_l = raise_reference(s.m, fmaxf(mx0, mx1), up);
-  s.m_ref = s.m == -INFINITY ? 0.0f : s.m;
-  const float was = s.mt == -INFINITY ? -INFINITY : kWeightTop - s.x + (m - s.m);      // r beside the new m
-  const float y = fmaxf((mx0 - s.m_ref) + lv0, (mx1 - s.m_ref) + lv1), to = __builtin_ceilf(y) + kRoom;
+  b.alpha_l = raise_reference(to.m, fmaxf(mx0, mx1), up);
+  to.m_ref = to.m == -INFINITY ? 0.0f : to.m;
+  const float was = s.mt == -INFINITY ? -INFINITY : kWeightTop - s.x + (s.m - to.m);      // r beside the new m
+  const float y = fmaxf((mx0 - to.m_ref) + lv0, (mx1 - to.m_ref) + lv1), at = __builtin_ceilf(y) + kRoom;
   up = y > was;
-  b.alpha_o = up ? __builtin_amdgcn_exp2f(was - to) : 1.0f;
-  const float r = up ? to : was;
-  s.x = r == -INFINITY ? 0.0f : kWeightTop - r;
+  b.alpha_o = up ? __builtin_amdgcn_exp2f(was - at) : 1.0f;
+  const float r = up ? at : was;
+  to.x = r == -INFINITY ? 0.0f : kWeightTop - r;
   // far out, the sum s + log2 sv has no bits to compare: every block comes here
-  s.mt = r == -INFINITY ? r : is_far(s) ? -0x1p127f : r + s.m_ref;
-  return b;
+  to.mt = r == -INFINITY ? r : is_far(to) ? -0x1p127f : r + to.m_ref;
+  s.m = raised ? to.m : s.m;
+  s.mt = raised ? to.mt : s.mt;
+  s.m_ref = raised ? to.m_ref : s.m_ref;
+  s.x = raised ? to.x : s.x;
+  return {raised ? b.alpha_l : 1.0f, raised ? b.alpha_o : 1.0f};
 }
 struct Int8Page {
   float c, back;

@@ -228,9 +228,10 @@ __global__ __launch_bounds__(64 * kWaves, DV == 256 ? 1 : D == 64 ? (kSplitKeys 
     // is still 0)
     auto references = [&](float mx0, float mx1, float kq0, float kq1, float lv0, float lv1) __attribute__((always_inline)) {
       const float2 mx = max_halves(mx0, mx1);
-      const float t0 = mx.x * kq0, t1 = mx.y * kq1;
-      if (__builtin_amdgcn_ballot_w64(is_raised(st, t0, t1, lv0, lv1)) != 0) {       // seldom: the references are coarse
-        const Int8Raise up = raise_block(st, t0, t1, lv0, lv1);
+      const float t0 = largest_score(mx.x, kq0), t1 = largest_score(mx.y, kq1);
+      const bool raised = is_raised(st, t0, t1, lv0, lv1);
+      if (__builtin_amdgcn_ballot_w64(raised) != 0) {                                // seldom: the references are coarse
+        const Int8Raise up = raise_block(st, raised, t0, t1, lv0, lv1);
         any_far = __builtin_amdgcn_ballot_w64(is_far(st)) != 0;
         st.l *= up.alpha_l;
         if (!fresh) {
