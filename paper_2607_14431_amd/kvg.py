@@ -308,6 +308,20 @@ def _payload_ptr(payload):
     return payload.data_ptr()
 
 
+def _payload_ok(payload, nbytes: int, what: str):
+    """Checks of a payload that kernels read or write: `nbytes` of dense bytes, in device or pinned host memory (what is not a torch tensor
+    gives its own device address).  The tensor, if it is a device's."""
+    if payload.nbytes < nbytes:
+        raise ValueError(f"payload: {what}")
+    if isinstance(payload, torch.Tensor):
+        if not payload.is_contiguous():
+            raise ValueError("payload: contiguous")
+        if not payload.is_cuda and not payload.is_pinned():
+            raise ValueError(f"payload: on the device or in pinned host memory, got {payload.device}")
+        return payload if payload.is_cuda else None
+    return None
+
+
 def kvg_artifact_seal(hdr: kvg_artifact_hdr, payload, ws: torch.Tensor, stream=None):
     _check(_lib.kvg_artifact_seal(ctypes.byref(hdr), _payload_ptr(payload), _ptr(ws), ws.nbytes, _stream(stream)),
            "kvg_artifact_seal")
@@ -337,16 +351,14 @@ def kvg_append(cache: Cache, seqs: Seqs, rp: kvg_rope, layer0: int, n_layers: in
 
 def kvg_deposit(cache: Cache, block_table_row: torch.Tensor, first_token: int, n_tokens: int,
                 payload: torch.Tensor, stream=None):
-    if payload.nbytes < kvg_payload_bytes(cache, n_tokens):
-        raise ValueError("payload: kvg_payload_bytes(cache, n_tokens) bytes")
+    _payload_ok(payload, kvg_payload_bytes(cache, n_tokens), "kvg_payload_bytes(cache, n_tokens) bytes")
     _check(_lib.kvg_deposit(ctypes.byref(cache.struct()), _ptr(block_table_row), block_table_row.numel(),
                             first_token, n_tokens, _ptr(payload), _stream(stream)), "kvg_deposit")
 
 
 def kvg_graft(cache: Cache, hdr: kvg_artifact_hdr, payload: torch.Tensor, block_table_row: torch.Tensor,
               first_token: int, target_pos: int, flags: int = 0, stream=None):
-    if payload.nbytes < hdr.payload_bytes:
-        raise ValueError("payload: the header's payload_bytes")
+    _payload_ok(payload, hdr.payload_bytes, "the header's payload_bytes")
     _check(_lib.kvg_graft(ctypes.byref(cache.struct()), ctypes.byref(hdr), _ptr(payload), _ptr(block_table_row),
                           block_table_row.numel(), first_token, target_pos, flags, _stream(stream)), "kvg_graft")
 
@@ -707,9 +719,8 @@ def kvg_int8_deposit(cache: Int8Cache, block_table_row: torch.Tensor, first_toke
                      stream=None):
     """kvg_deposit of an int8 block: its integers, then its scales."""
     _block_table(block_table_row)
-    if not payload.is_contiguous() or payload.nbytes < kvg_int8_payload_bytes(cache, n_tokens):
-        raise ValueError("payload: kvg_int8_payload_bytes(cache, n_tokens) bytes, contiguous")
-    _on_current_device(*cache.tensors(), block_table_row)
+    on_device = _payload_ok(payload, kvg_int8_payload_bytes(cache, n_tokens), "kvg_int8_payload_bytes(cache, n_tokens) bytes")
+    _on_current_device(*cache.tensors(), block_table_row, on_device)
     _check(_lib.kvg_int8_deposit(ctypes.byref(cache.struct()), _ptr(block_table_row), block_table_row.numel(), first_token,
                                  n_tokens, _ptr(payload), _stream(stream)), "kvg_int8_deposit")
 
@@ -718,9 +729,8 @@ def kvg_int8_graft(cache: Int8Cache, hdr: kvg_artifact_hdr, payload, block_table
                    target_pos: int, stream=None):
     """kvg_graft of an int8 block, at its own position."""
     _block_table(block_table_row)
-    if payload.nbytes < hdr.payload_bytes:
-        raise ValueError("payload: the header's payload_bytes")
-    _on_current_device(*cache.tensors(), block_table_row)
+    on_device = _payload_ok(payload, hdr.payload_bytes, "the header's payload_bytes")
+    _on_current_device(*cache.tensors(), block_table_row, on_device)
     _check(_lib.kvg_int8_graft(ctypes.byref(cache.struct()), ctypes.byref(hdr), _payload_ptr(payload), _ptr(block_table_row),
                                block_table_row.numel(), first_token, target_pos, _stream(stream)), "kvg_int8_graft")
 
