@@ -82,7 +82,8 @@ typedef enum { KVG_F32 = 0, KVG_BF16 = 1, KVG_FP8_E4M3 = 2 } kvg_dtype;
 /* Rotary pairing of the D components: HALF pairs i with i + D/2, INTERLEAVED pairs
  * 2i with 2i + 1.  theta_i = base^(-2i/D), i in [0, D/2). */
 typedef enum { KVG_ROPE_HALF = 0, KVG_ROPE_INTERLEAVED = 1 } kvg_rope_pairing;
-/* rope_pairing of a block whose keys no kvg_rope has rotated (kvg_artifact_header_init_rotary): it cannot be relocated */
+/* rope_pairing of a block whose keys no kvg_rope has rotated (kvg_artifact_header_init_rotary, kvg_artifact_header_init_axes):
+ * it cannot be relocated */
 #define KVG_ROPE_OTHER 2
 
 typedef struct {
@@ -343,7 +344,8 @@ int kvg_decode_attn_noalloc(const kvg_cache* cache, const kvg_seqs* seqs, const 
  * kvg_norm_append writes the new tokens' keys and values to the cache and their queries, normed
  * and rotated, to q_out; kvg_packed_attn attends over the cache from them.  The blocks deposited
  * from such a cache graft like any other at their own position (a byte move); their headers come from
- * kvg_artifact_header_init_rotary, which leaves open to relocation those that it can be right for. */
+ * kvg_artifact_header_init_rotary, which leaves open to relocation those that it can be right for (positions with several axes:
+ * kvg_artifact_header_init_axes). */
 
 /* How a rotary's frequencies follow from theta_i = base^(-2i/r), i in [0, r/2), r = rotary_dim,
  * for a context `factor` times longer than the original_len tokens they were made for. */
@@ -492,12 +494,17 @@ int kvg_rotate_axes(const kvg_rotary* rotary, const kvg_axes* axes, int32_t dtyp
                     int32_t n_heads, const void* x_dev, int64_t x_stride, void* y_dev, int64_t y_stride, void* stream);
 
 /* kvg_norm_append at positions with several axes: token row t of the packed tensors is at axes->positions[.][t]
- * (seqs->start_pos is not read).  Blocks of such a cache graft at their own position: their header is
- * kvg_artifact_header_init's with rope_pairing set to KVG_ROPE_OTHER.  Errors: as kvg_norm_append, KVG_E_INVAL (axes),
- * KVG_E_SHAPE (pairs). */
+ * (seqs->start_pos is not read).  Blocks of such a cache have kvg_artifact_header_init_axes' headers.  Errors: as
+ * kvg_norm_append, KVG_E_INVAL (axes), KVG_E_SHAPE (pairs). */
 int kvg_norm_append_axes(const kvg_cache* cache, const kvg_seqs* seqs, const kvg_packed* packed, const kvg_rotary* rotary,
                          const kvg_axes* axes, const kvg_head_norm* norm, int32_t layer0, int32_t n_layers,
                          const void* q_raw_dev, const void* k_raw_dev, const void* v_raw_dev, void* q_out_dev, void* stream);
+
+/* kvg_artifact_header_init for a block whose keys were rotated at positions with several axes.  One distance turns no such
+ * token right, so its rope_pairing is KVG_ROPE_OTHER, which no kvg_graft relocates, and own_pos is any number that names where
+ * the block belongs.  axes->positions is not read and may be NULL.  Errors: KVG_E_INVAL, KVG_E_SHAPE, KVG_E_DTYPE. */
+int kvg_artifact_header_init_axes(const kvg_cache* cache, int32_t n_tokens, int64_t own_pos, const kvg_rotary* rotary,
+                                  const kvg_axes* axes, kvg_artifact_hdr* hdr_out);
 
 /* ---------------------------------------------------------------------------------
  * Caches of 8-bit integers: a stored value is n * scale, n in [-127, 127], with a scale for the keys and one for the

@@ -77,6 +77,18 @@ int kvg_artifact_header_init_rotary(const kvg_cache* cache, int32_t n_tokens, in
   return st;
 }
 
+int kvg_artifact_header_init_axes(const kvg_cache* cache, int32_t n_tokens, int64_t own_pos, const kvg_rotary* rotary,
+                                  const kvg_axes* axes, kvg_artifact_hdr* hdr) {
+  int st = check_cache(cache);
+  if (st != KVG_OK) return st;
+  if ((st = check_rotary(rotary, cache->head_dim)) != KVG_OK) return st;
+  if ((st = check_axes(rotary, cache->head_dim, axes, 0)) != KVG_OK) return st;
+  const kvg_rope rope = {rotary->base, rotary->pairing, 0};
+  st = kvg_artifact_header_init(cache, n_tokens, own_pos, &rope, hdr);
+  if (st == KVG_OK) hdr->rope_pairing = KVG_ROPE_OTHER;
+  return st;
+}
+
 int kvg_rotate(const kvg_rotary* rotary, int32_t dtype, int32_t head_dim, int32_t n_tokens, int32_t n_heads,
                const int64_t* positions, const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream) {
   return rotate(rotary, nullptr, dtype, head_dim, n_tokens, n_heads, positions, x, x_stride, y, y_stride, stream);

@@ -127,6 +127,7 @@ _SIGS = {
     "kvg_rotate": (ctypes.c_int, [_P(kvg_rotary), _i32, _i32, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _vp]),
     "kvg_norm_append": (ctypes.c_int, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_packed), _P(kvg_rotary), _P(kvg_head_norm),
                                        _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
+    "kvg_artifact_header_init_axes": (ctypes.c_int, [_P(kvg_cache), _i32, _i64, _P(kvg_rotary), _P(kvg_axes), _P(kvg_artifact_hdr)]),
     "kvg_rotate_axes": (ctypes.c_int, [_P(kvg_rotary), _P(kvg_axes), _i32, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp]),
     "kvg_norm_append_axes": (ctypes.c_int, [_P(kvg_cache), _P(kvg_seqs), _P(kvg_packed), _P(kvg_rotary), _P(kvg_axes),
                                             _P(kvg_head_norm), _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
@@ -499,6 +500,15 @@ class Axes:
         # packed in one step: a ctypes array and nine fields took half of a small call's marshalling
         return kvg_axes.from_buffer_copy(_AXES.pack(pos.data_ptr(), n, self.order, int(self.own_frequencies), 0, *self.pairs,
                                                     *(0,) * (KVG_MAX_AXES - n)))
+
+
+def kvg_artifact_header_init_axes(cache: Cache, n_tokens: int, own_pos: int, rt: kvg_rotary, axes: Axes) -> kvg_artifact_hdr:
+    """Header of a block of n_tokens tokens at positions with several axes (which it does not read: those of any call do)."""
+    hdr = kvg_artifact_hdr()
+    _check(_lib.kvg_artifact_header_init_axes(ctypes.byref(cache.struct()), n_tokens, own_pos, ctypes.byref(rt),
+                                              ctypes.byref(axes.struct(axes.positions.shape[-1])), ctypes.byref(hdr)),
+           "kvg_artifact_header_init_axes")
+    return hdr
 
 
 def _rotate_strides(where: str, x: torch.Tensor, y: torch.Tensor):
