@@ -27,7 +27,8 @@ def attend(q, index, kn, ks, vn, vs, scale, window=0):
     tol: the query is rounded to multiples of 2^(e - 14), 2^e > max |q| >= 2^(e - 1), so each component is off by at most 2^-14 max
     |q|; the integer products are exact; the scores' conversion, scales and difference to the reference round a few times
     each (8 u of the score's size and 24 u), the exponential 2 u.  A score off by d moves a row by w d |v - out|.  A weight times
-    its scale rounds to fp16: 2^-11 of itself, or 2^-24 of the row's largest where it is below 2^-13 of that; the sum of
+    its scale rounds to fp16, in units in which the largest of its segment of keys is above 2^6: 2^-11 of itself, or below 2^-14 of
+    them half of fp16's last step, 2^-25, which is 2^-31 of the row's largest; the sum of
     the weights does not, so it moves a row by that part of w |v|.  Sums of n terms add n u.  The result rounds to bf16."""
     T, Hq, D = q.shape
     S, Hkv = ks.shape
@@ -53,7 +54,7 @@ def attend(q, index, kn, ks, vn, vs, scale, window=0):
             mass = wt @ np.abs(vt)
             top = (wt * vs[seen, g]).max()
             moved = (wt * off[t, seen]) @ np.abs(vt - out)
-            small = 2.0 ** -24 * top * np.abs(vn[seen, g]).sum(axis=0)
+            small = 2.0 ** -31 * top * np.abs(vn[seen, g]).sum(axis=0)
             err = 1.02 * moved + (2.0 ** -11 + 4 * U) * mass + small + (seen.sum() + 8) * U * (mass + np.abs(out))
             want[t, h] = out
             tol[t, h] = err + 2.0 ** -8 * (np.abs(out) + err) + 1e-37

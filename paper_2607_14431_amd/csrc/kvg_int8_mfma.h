@@ -3,8 +3,8 @@
 //   scores   S = (q . n_j) qstep sk: the query is an integer of 15 bits times a power of two, its upper and lower byte multiply
 //            the cached integers n_j on v_mfma_i32_32x32x32_i8, exactly (|S| <= 2^14 127 256 < 2^30); a pair of these steps takes as long
 //            as the one bf16 step of the same 32 dimensions would, and the cached bytes go in as they are
-//   weights  w_j = p_j sv 2^x, p_j = 2^(s_j - m), rounded to fp16; x puts the row's largest weight between 2^-1 and
-//            2^15, so that only weights below 2^-13 of it lose bits.  The integers m_j are exact in fp16.
+//   weights  w_j = p_j sv 2^x, p_j = 2^(s_j - m), rounded to fp16; x puts the row's largest weight between 2^6 and
+//            2^15 (see Int8State), so that only weights below 2^-20 of it lose bits.  The integers m_j are exact in fp16.
 #pragma once
 
 #include "kvg_int8.h"

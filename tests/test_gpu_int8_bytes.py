@@ -1,9 +1,11 @@
-"""Int8 attention: a row's bytes where its value reference is at the point of rising."""
+"""Int8 attention: a row's bytes where its value reference is at the point of rising, and weights far below a row's largest."""
 
 import numpy as np
 import pytest
 import torch
 
+from oracle import int8 as oracle
+from tests.packed_helpers import host
 from tests.test_gpu_packed import bits, kvg  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -87,3 +89,31 @@ def test_a_row_at_its_references_rise(kvg, D):  # noqa: F811
             # every row has the first one's query, and the tokens between weigh nothing
             wrong = (got != want).any(dim=3).nonzero()
             assert len(wrong) == 0, f"room {room}, {n} rows, raising {list(raising)}: (layer, row, KV head) {wrong[:8].tolist()} of {len(wrong)}"
+
+
+@pytest.mark.parametrize("heads", [(2, 2, 64), (4, 2, 128), (8, 4, 256)])
+@pytest.mark.parametrize("n", [1, 40])
+def test_weights_far_below_the_largest(kvg, heads, n):  # noqa: F811
+    """Equal scores, one page of values of scale 1 and the others of 2^-18 to 2^-20: the former has no values in half of the dimensions, where
+    the result is that of the light pages.  Their scales lie between fp16's steps for a largest weight of 1 or less, by 1/32 of themselves."""
+    Hq, Hkv, D = heads
+    rng = np.random.default_rng(8)
+    pages, ctx = 24, 16 * 24 - n
+    kn, vn = rng.integers(-127, 128, (pages * 16, Hkv, D)), rng.integers(64, 128, (pages * 16, Hkv, D))
+    vn[:16, :, D // 2:] = 0
+    vs = np.tile((1 + 3 / 32) * np.exp2(-20.0 + np.arange(Hkv) % 3), (pages, 1))
+    vs[0] = 1.0
+    ks = np.ones((pages, Hkv))
+    cache = kvg.Int8Cache.allocate(1, pages, *heads)
+    for pool, x in ((cache.k_pool, kn), (cache.v_pool, vn)):
+        pool[0].copy_(torch.from_numpy(x.reshape(pages, 16, Hkv, D).transpose(0, 2, 1, 3).astype(np.int8)))
+    for scale, x in ((cache.k_scale, ks), (cache.v_scale, vs)):
+        scale[0].copy_(torch.from_numpy(x))
+    seqs = kvg.Seqs(torch.arange(pages, dtype=torch.int32, device="cuda")[None].contiguous(), torch.tensor([ctx], dtype=torch.int32, device="cuda"),
+                    torch.zeros(1, dtype=torch.int64, device="cuda"), ctx)
+    packed = kvg.Packed(torch.tensor([0, n], dtype=torch.int32, device="cuda"), n, n)
+    q = torch.zeros(1, n, Hq, D, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty_like(q)
+    kvg.kvg_int8_attn(cache, seqs, packed, 0, 1, q, 0.1, out, kvg.int8_attn_workspace(cache, seqs, packed, 1))
+    want, tol = oracle.attend(host(q[0]), ctx + np.arange(n), kn, np.repeat(ks, 16, axis=0), vn, np.repeat(vs, 16, axis=0), 0.1)
+    assert np.all(np.abs(host(out[0]) - want) <= tol)
