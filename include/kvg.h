@@ -510,7 +510,8 @@ int kvg_artifact_header_init_axes(const kvg_cache* cache, int32_t n_tokens, int6
  * Caches of 8-bit integers: a stored value is n * scale, n in [-127, 127], with a scale for the keys and one for the
  * values of every page (block of 16 tokens) and KV head.  Half the bytes of a bf16 cache, as an fp8 one; for rows without
  * outliers a third of its rounding (half a step is 1/254 of a block's largest value, where E4M3 rounds each value by up to
- * 2^-4 of it).  Raw rows, queries and outputs are bf16.  Other entry points refuse such a cache (KVG_E_DTYPE). */
+ * 2^-4 of it).  Scales are 0 or at least 2^-126, never negative.  Raw rows, queries and outputs are bf16.  Other entry points
+ * refuse such a cache (KVG_E_DTYPE). */
 typedef struct {
   kvg_cache pages;              /* dtype KVG_INT8 */
   float* k_scale;               /* device [n_layers][n_pages][n_kv_heads] */

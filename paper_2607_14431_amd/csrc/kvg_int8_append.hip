@@ -9,7 +9,8 @@
 // Bound: 14,100 tokens of 32 + 2 x 16 heads x 128 take 101 us (406 MB, 4.0 TB/s), the vector unit busy for 62 of them: 21 instructions
 // for 64 values, of which the norm has nine, the rotation five and the integers three (with a clamp, a conversion and shifts for each
 // integer it was eight, and 108 us).  One to six workgroups a page take 100 to 103 us, eight 111; 16 single tokens of 16 + 2 x 8 heads x
-// 256, a page each, 7 us with a wave for every head, 18 with four for all.
+// 256, a page each, 7 us with a wave for every head, 18 with four for all: metadata, the fp64 angles behind their barrier, and only then
+// the raw rows, head after head (kvg_rotary.hip requests its first rows before the angles, this kernel does not).
 #include "kvg_int8.h"
 #include "kvg_launch.h"
 #include "kvg_rotary.h"

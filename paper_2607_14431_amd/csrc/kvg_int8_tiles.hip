@@ -13,8 +13,8 @@
 //                   each wave takes one page of the next tile through registers into LDS, once for the four waves that read it
 //                   (widened beside the reads, every wave spent 160 vector instructions a tile of head_dim 128 on it instead of 40)
 //
-// Bound: vector instructions beside the matrix ones (the two add up: head_dim 128 has the vector unit busy 66% of the time, the matrix
-// cores 32%), so the loop is counted in them: ids and scales once a segment, references seldom raised.  Eight prompts of up to 4,096
+// Bound: vector instructions beside the matrix ones (head_dim 128 has the vector unit busy 66% of the time, the matrix cores 32%; how far the
+// two overlap these counters do not say), so the loop is counted in them: ids and scales once a segment, references seldom raised.  Eight prompts of up to 4,096
 // tokens, 32 heads on 16, head_dim 128: 540 us (714 TFLOP/s; ids and scales loaded a page at a time 616).  head_dim 256 has one wave a
 // SIMD and copies accumulators between the two register files: one prompt of 12,288 tokens, 16 heads on 8, 2.39 ms (518 TFLOP/s).
 #include "kvg_int8_mfma.h"

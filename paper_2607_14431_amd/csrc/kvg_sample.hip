@@ -7,7 +7,9 @@
 // of weights reaches its share, min-p at a weight.  So what is kept is `code >= cut && e^x >= min_p`, and the token is the first in
 // index order whose running sum of kept weights passes the random number's.
 //
-// Rows of up to kSampleListed tokens: a workgroup holds the row's codes.  Longer ones in passes over the row, by many workgroups:
+// Rows of up to kSampleListed tokens: a workgroup holds the row's codes (4,096 tokens, us, without limits / top-k / top-p / both: one row 8 / 11 / 17 /
+// 19, 256 rows 8 / 12 / 30 / 32: the chain of select()'s passes, each a round over LDS with five barriers).  Longer ones in passes over the row, by
+// many workgroups:
 //   top     the largest logit of every part of the row
 //   bins    count and weight of the row's tokens by weight (1,024 equal steps of the exponent down to weight 0), where a top-k or
 //           top-p may end inside the row.  The bins tell in which of them the two limits end.  Weights are left out where top-p is 1
@@ -19,8 +21,12 @@
 // additions of the rows with a top-p alone), 18 for the parts, 24 for the longest lists.  A bitonic sort of a list of 1,400 codes
 // took 20 us, select() about 5.
 //
-// Where the list would be too long (thousands of tokens of nearly equal logits) the cut is found digit by digit instead (11, 11, 10
-// bits of the logit, twice 12 of the index): count or weight of the tokens that share the digits so far, by their next digit.
+// Where the list would be too long the cut is found digit by digit instead (11, 11, 10 bits of the logit, twice 12 of the index): count or
+// weight of the tokens that share the digits so far, by their next digit.  One workgroup makes these passes over the row, five for each
+// limit.  That takes more than 4,096 tokens in the bins where the limits end, (bits + 2) ln 2 / 1,024 wide in x each (0.031 at 262,144
+// tokens): equal logits, but flat rows too, normal ones of sigma / T below about 0.65 with a top-p of 0.9, wider ones of longer
+// vocabularies.  262,144 tokens with that top-p, us, at sigma / T of 3 / 0.75 / 0.5 / equal logits: one row 33 / 37 / 641 / 1,289, 64 rows 103 / 109 /
+// 925 / 2,687; 32,000 tokens, 3 / 0.3 / equal: one row 24 / 29 / 198, 64 rows 39 / 45 / 348; one row of 2,097,152, 3 / 0.5: 64 / 6,489.
 #include "kvg_exp.h"
 #include "kvg_sample.h"
 
