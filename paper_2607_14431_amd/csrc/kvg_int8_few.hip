@@ -254,8 +254,8 @@ __global__ __launch_bounds__(64 * kWaves) void int8_few_kernel(const PackedAttnA
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4)
         *reinterpret_cast<uint2*>(op + d * 32 + r4 * 8 + half * 4) =
-            make_uint2(pack_bf16_rne(o[d][r4 * 4] * inv, o[d][r4 * 4 + 1] * inv),
-                       pack_bf16_rne(o[d][r4 * 4 + 2] * inv, o[d][r4 * 4 + 3] * inv));
+            make_uint2(pack_bf16_rne(row_result(o[d][r4 * 4], inv), row_result(o[d][r4 * 4 + 1], inv)),
+                       pack_bf16_rne(row_result(o[d][r4 * 4 + 2], inv), row_result(o[d][r4 * 4 + 3], inv)));
   }
 }
 

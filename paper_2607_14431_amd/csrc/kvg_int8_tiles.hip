@@ -289,7 +289,7 @@ __global__ __launch_bounds__(64 * kWaves, DV == 256 ? 1 : D == 64 ? (kSplitKeys 
     }
   };
   // end of a segment: its sums taken to the reference of p, its state folded into the running one, which packed_fold_kernel does with
-  // the same operations (the power of two in the factor would give a few zeros another sign)
+  // the same operations (the power of two in the factor would round sums below fp32's range otherwise)
   auto end_segment = [&]() {
     const int e = end_exponent(st);
 #pragma unroll
@@ -343,8 +343,8 @@ __global__ __launch_bounds__(64 * kWaves, DV == 256 ? 1 : D == 64 ? (kSplitKeys 
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4)
         *reinterpret_cast<uint2*>(op + d * 32 + r4 * 8 + half * 4) =
-            make_uint2(pack_bf16_rne(o_run[d][r4 * 4] * inv, o_run[d][r4 * 4 + 1] * inv),
-                       pack_bf16_rne(o_run[d][r4 * 4 + 2] * inv, o_run[d][r4 * 4 + 3] * inv));
+            make_uint2(pack_bf16_rne(row_result(o_run[d][r4 * 4], inv), row_result(o_run[d][r4 * 4 + 1], inv)),
+                       pack_bf16_rne(row_result(o_run[d][r4 * 4 + 2], inv), row_result(o_run[d][r4 * 4 + 3], inv)));
   }
 }
 

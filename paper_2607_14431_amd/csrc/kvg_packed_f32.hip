@@ -279,7 +279,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_f32_kernel(const Packed
     for (int j = 0; j < ND; ++j) {            // dims ND f_i + 4 j + 0..3
       Floats<4> v;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v.x[i] = kSplitKeys ? run[(4 * j + i) % ND][(4 * j + i) / ND] : run[(4 * j + i) % ND][(4 * j + i) / ND] * inv;
+      for (int i = 0; i < 4; ++i) v.x[i] = kSplitKeys ? run[(4 * j + i) % ND][(4 * j + i) / ND] : row_result(run[(4 * j + i) % ND][(4 * j + i) / ND], inv);
       const int x = ND * f_i + 4 * j;
       float* dst = kSplitKeys ? a.part.acc + block * (32 * D) + part_at(f_pair, x) : static_cast<float*>(a.out) + row_of(f_pair) * D + x;
       *reinterpret_cast<Floats<4>*>(dst) = v;

@@ -206,8 +206,8 @@ __global__ __launch_bounds__(64 * kWaves) void packed_few_kernel(const PackedAtt
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4)
           *reinterpret_cast<uint2*>(op + d * 32 + r4 * 8 + half * 4) =
-              make_uint2(pack_bf16_rne(o[d][r4 * 4] * inv, o[d][r4 * 4 + 1] * inv),
-                         pack_bf16_rne(o[d][r4 * 4 + 2] * inv, o[d][r4 * 4 + 3] * inv));
+              make_uint2(pack_bf16_rne(row_result(o[d][r4 * 4], inv), row_result(o[d][r4 * 4 + 1], inv)),
+                         pack_bf16_rne(row_result(o[d][r4 * 4 + 2], inv), row_result(o[d][r4 * 4 + 3], inv)));
     }
   }
   if (s_bad != 0) {                                  // the values that are not finite, to the rows that see them
@@ -250,7 +250,7 @@ __device__ __forceinline__ void fold_few(const PackedAttnArgs& a, const PackedPa
     o_run = fmaf(acc[(int64_t)s * D], f.part, o_run * f.run);
   }
   const int64_t row = (int64_t)l * a.seqs.n_tokens + u.range.row0 + u.at;
-  static_cast<__bf16*>(a.out)[(row * a.Hq + h) * D + x] = (__bf16)(o_run * (1.0f / l_run));
+  static_cast<__bf16*>(a.out)[(row * a.Hq + h) * D + x] = (__bf16)row_result(o_run, 1.0f / l_run);
 }
 
 // Tiles: a workgroup takes 32 dims of a block of 32 pairs, a wave 8 of them, a lane a pair and 4 dims.  Segments that the
@@ -307,7 +307,7 @@ __device__ __forceinline__ void fold_tiles(const PackedAttnArgs& a, const Packed
     T x[4];
   };
   *reinterpret_cast<Four*>(static_cast<T*>(a.out) + row * D + chunk * 8 + (lane >> 5) * 4) = {
-      {(T)(o_run[0] * inv), (T)(o_run[1] * inv), (T)(o_run[2] * inv), (T)(o_run[3] * inv)}};
+      {(T)row_result(o_run[0], inv), (T)row_result(o_run[1], inv), (T)row_result(o_run[2], inv), (T)row_result(o_run[3], inv)}};
 }
 
 // Both in one launch: the few kernel's rows first, in few_workgroups workgroups (none beside fp32 caches, which it does not take).

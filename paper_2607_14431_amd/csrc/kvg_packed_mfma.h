@@ -224,6 +224,10 @@ __device__ __forceinline__ FoldFactors fold_factors(float& m_run, float& l_run, 
   l_run = fmaf(l, f.part, l_run * f.run);
   return f;
 }
+// A row's result from a sum of weighted values and the inverse sum of weights.  A sum that leaves fp32 on the negative side is -0, and
+// becomes +0 with the next block or segment that has no weight for the row, which its neighbours may bring: a zero is
+// always stored as +0.
+__device__ __forceinline__ float row_result(float o, float inv) { return fmaf(o, inv, 0.0f); }
 
 }  // namespace
 
